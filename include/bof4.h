@@ -71,6 +71,13 @@ extern "C" {
 #define BOF4_METRIC_MSE_NORMALIZED 2
 #define BOF4_METRIC_MAE_NORMALIZED 3
 
+/* Activations of bof4_linear, bof4_linear_backward and bof4_moe, in fp32 */
+#define BOF4_ACT_NONE 0
+#define BOF4_ACT_RELU 1
+#define BOF4_ACT_GELU 2      /* z * Phi(z), Phi the normal distribution function */
+#define BOF4_ACT_GELU_TANH 3 /* z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) */
+#define BOF4_ACT_SILU 4      /* z / (1 + exp(-z)) */
+
 #define BOF4_OP_EM 0  /* bof4_em_step, and a bof4_fit_codebook that streams its data */
 #define BOF4_OP_OPQ 1 /* opq_split / bof4_quantize_opq workspace    */
 #define BOF4_OP_EM_BF16 2 /* bof4_fit_codebook over bf16 tensors, any number of iterations */
@@ -373,6 +380,58 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
                  int64_t cols, int block_size, const float* d_codebook, const void* d_x, int n_rhs,
                  const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity,
                  float* d_y, int* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Linear layer over the 4-bit matrix, for any number of tokens:
+ *   z[t, r] = sum_c W^[r, c] x[t, c] + bias[r],   y[t, r] = act(z[t, r]) + residual[t, r]
+ * with W rows x cols as for bof4_gemv (a block never straddles two rows).  Reading: W^ is the dequantised weight rounded to
+ * bf16, bit for bit what bof4_dequantize writes, and the stored value where the outlier list has an entry; products are exact
+ * and added up in fp32 (in an order that depends on shapes and types alone, so two calls on the same inputs give the same
+ * bits); bias, activation and residual are applied in fp32; y is rounded once.  (bof4_gemv keeps the unrounded product
+ * scale * level instead.)
+ *   d_codes     device, rows * cols / 2 bytes, 32-byte aligned;  d_scales, d_codebook as for bof4_gemv
+ *   d_x         device, bf16, token t at d_x + t * ldx, 16-byte aligned; ldx a multiple of 8
+ *   d_bias      device, rows values of bias_dtype, or NULL
+ *   d_residual  device, values of y_dtype, token t at t * ld_residual, or NULL; may be d_y itself (with ld_residual = ldy)
+ *   activation  BOF4_ACT_*
+ *   d_out_idx / d_out_val / d_n_out / capacity   outlier list as for bof4_dequantize (ascending, distinct indices), or all
+ *               NULL; with a list, rows * cols must fit 32-bit indices
+ *   d_y         device, out, y_dtype (BOF4_BF16 or BOF4_F32), token t at t * ldy
+ *   d_pre       device, out, bf16, token t at t * ld_pre: z, as bof4_linear_backward wants it where there is an
+ *               activation; or NULL
+ *   d_status    device int, written: 0, or 1 when a bounded wait inside the kernel ran out (y is then undefined)
+ *   d_ws        device workspace of bof4_linear_workspace_bytes(rows, cols, n_tokens, 0, capacity) bytes, 256-byte aligned,
+ *               any contents; two calls that may run at the same time must not share one
+ * Row strides are in elements and do not matter where n_tokens is 1.  Outputs must not overlap inputs but as said.
+ * No host synchronisation.
+ */
+BOF4_API int bof4_linear(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size,
+                         const float* d_codebook, const void* d_x, int64_t ldx, int64_t n_tokens, const void* d_bias, int bias_dtype,
+                         const void* d_residual, int64_t ld_residual, int activation, const int32_t* d_out_idx, const void* d_out_val,
+                         const int64_t* d_n_out, int64_t capacity, void* d_y, int y_dtype, int64_t ldy, void* d_pre, int64_t ld_pre,
+                         int* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward pass of bof4_linear with the quantised weights held fixed (adapters trained beside a frozen 4-bit matrix):
+ *   dz[t, r] = dy[t, r] * act'(z[t, r]),   dx[t, c] = sum_r dz[t, r] W^[r, c],   dbias[r] = sum_t dz[t, r]
+ * (the gradient of the residual is dy itself).  dz is formed in fp32; the product takes it rounded to bf16, the operand type
+ * of the tensor cores (dy in bf16 without an activation is taken as it is), the sums of dbias take it unrounded.
+ *   d_dy      device, dy_dtype (BOF4_BF16 or BOF4_F32), token t at t * ld_dy
+ *   d_pre     device, bf16, z as bof4_linear left it, token t at t * ld_pre; ignored without an activation
+ *   d_dx      device, out, bf16, token t at t * ld_dx, or NULL: not wanted
+ *   d_dbias   device, out, fp32 [rows], or NULL
+ *   d_ws      device workspace of bof4_linear_workspace_bytes(rows, cols, n_tokens, 1, capacity) bytes, as for bof4_linear
+ * The derivative of BOF4_ACT_RELU at zero is 0.  Other arguments as for bof4_linear.
+ */
+BOF4_API int bof4_linear_backward(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size,
+                                  const float* d_codebook, const void* d_dy, int dy_dtype, int64_t ld_dy, int64_t n_tokens,
+                                  const void* d_pre, int64_t ld_pre, int activation, const int32_t* d_out_idx, const void* d_out_val,
+                                  const int64_t* d_n_out, int64_t capacity, void* d_dx, int64_t ld_dx, float* d_dbias, int* d_status,
+                                  void* d_ws, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace for the two calls above (backward != 0: for the second).  capacity: that of the outlier list, 0 without
+ * one.  Host function, no CUDA call.  0 for invalid or too large shapes. */
+BOF4_API size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, int backward, int64_t capacity);
 
 /*
  * Data-free codebook for unit-variance Gaussian weights (Sec. 3.2 Eq. 5 / Eq. 7; App. B.2): `iters`

@@ -27,6 +27,7 @@ NORM_ABS, NORM_SIGNED = 0, 1
 METRIC_MSE, METRIC_MAE = 0, 1
 METRIC_MSE_NORMALIZED, METRIC_MAE_NORMALIZED = 2, 3  # App. D: errors of the normalised weights
 OP_EM, OP_OPQ, OP_EM_BF16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 LEVELS = 16
 
 # kernels one MAE iteration enqueues: setup, 2 x (data pass + bin selection), then 2 data passes
@@ -55,7 +56,8 @@ EXPORTS = ("bof4_workspace_bytes", "bof4_fit_workspace_bytes", "bof4_em_step", "
            "opq_split", "opq_split_static", "bof4_quantize_opq", "bof4_dequantize", "bof4_opq_threshold",
            "bof4_default_init", "bof4_last_error", "bof4_theoretical_codebook", "bof4_theoretical_codebook_batch",
            "bof4_gemv", "bof4_outlier_count", "bof4_scales_compress", "bof4_scales_expand",
-           "bof4_theoretical_codebook_general", "bof4_quantize_batch", "bof4_dequantize_batch", "bof4_m_step", "bof4_gemm_tc")
+           "bof4_theoretical_codebook_general", "bof4_quantize_batch", "bof4_dequantize_batch", "bof4_m_step", "bof4_gemm_tc",
+           "bof4_linear", "bof4_linear_backward", "bof4_linear_workspace_bytes")
 
 
 class Bof4Error(RuntimeError):
@@ -119,6 +121,14 @@ def lib() -> ctypes.CDLL:
         L.bof4_dequantize_batch.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, i32, vp]
         L.bof4_gemm_tc.restype = i32
         L.bof4_gemm_tc.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i32, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.bof4_linear_workspace_bytes.restype = sz
+        L.bof4_linear_workspace_bytes.argtypes = [i64, i64, i64, i32, i64]
+        L.bof4_linear.restype = i32
+        L.bof4_linear.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i64, i64, vp, i32, vp, i64, i32, vp, vp, vp, i64, vp, i32, i64,
+                                  vp, i64, vp, vp, sz, vp]
+        L.bof4_linear_backward.restype = i32
+        L.bof4_linear_backward.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i32, i64, i64, vp, i64, i32, vp, vp, vp, i64, vp, i64,
+                                           vp, vp, vp, sz, vp]
         L.bof4_m_step.restype = i32
         L.bof4_m_step.argtypes = [vp, i32, i32, vp, ctypes.c_uint32, vp, vp, vp]
         L.bof4_scales_compress.restype = i32
@@ -458,6 +468,33 @@ def bof4_gemm_tc(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int
     """Y fp32 [rows, n_rhs] = W_q X^T on the tensor cores for x bf16 [n_rhs, cols].
     -> (y, status int32[1]); status 0 unless a bounded wait inside the kernel ran out."""
     return _native().gemm_tc(codes, scales, rows, cols, block_size, levels, x, workspace, split, outliers)
+
+
+def bof4_linear_workspace_bytes(rows: int, cols: int, n_tokens: int, backward: bool = False, capacity: int = 0) -> int:
+    """Bytes of the workspace of bof4_linear (backward: of bof4_linear_backward), which the calls otherwise allocate themselves."""
+    return int(lib().bof4_linear_workspace_bytes(rows, cols, n_tokens, int(backward), capacity))
+
+
+def bof4_linear(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, block_size: int, levels, x: torch.Tensor,
+                bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
+                out_dtype: int = BF16, pre: Optional[torch.Tensor] = None,
+                outliers: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """y [n_tokens, rows] = act(x W^T + bias) + residual for x bf16 [n_tokens, cols] (rows of x, residual, pre and out may be
+    apart from one another).  `pre` (bf16 [n_tokens, rows]) receives x W^T + bias, which bof4_linear_backward wants where there
+    is an activation.  -> (y, status int32[1]); status 0 unless a bounded wait inside the kernel ran out."""
+    return _native().linear(codes, scales, rows, cols, block_size, levels, x, bias, residual, activation, out_dtype, pre, outliers, out,
+                            workspace)
+
+
+def bof4_linear_backward(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, block_size: int, levels, dy: torch.Tensor,
+                         pre: Optional[torch.Tensor] = None, activation: int = ACT_NONE, want_dx: bool = True, want_dbias: bool = False,
+                         outliers: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None,
+                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of bof4_linear for dy [n_tokens, rows] with the weights held fixed -> (dx bf16 [n_tokens, cols] or None,
+    dbias fp32 [rows] or None, status int32[1])."""
+    return _native().linear_backward(codes, scales, rows, cols, block_size, levels, dy, pre, activation, want_dx, want_dbias, outliers,
+                                     out, workspace)
 
 
 def bof4_outlier_count(n_out: torch.Tensor, capacity: int) -> int:

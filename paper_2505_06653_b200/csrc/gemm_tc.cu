@@ -42,13 +42,9 @@
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, and the kernel frees its tensor
 // memory and returns.
-#include <atomic>
-#include <chrono>
 #include <type_traits>
 
-#include <cuda.h>
-
-#include "common.cuh"
+#include "tc.cuh"
 
 namespace bof4 {
 
@@ -75,70 +71,15 @@ constexpr int kTcLineBytes = kTcM * 128;         // 16 KiB
 constexpr int kTcPairBytes = 256 * 32 * 8;       // level pairs per code byte, a column per lane
 constexpr int kTcXBytes = 64 * 1024;                  // all stages of X
 constexpr int kTcSmem = kTcXBytes + kTcLines * kTcLineBytes + kTcPairBytes + 1024;  // + slack to align to 1024 bytes
-constexpr uint32_t kTcSpinLimit = 1u << 16;      // try_wait calls before a wait gives up (a k-block takes microseconds)
 // warps: 0 ... 15 produce, then issuers, X, constants and codes, results
 constexpr int kTcIssue = kTcGroups * 4, kTcX = kTcIssue + kTcIssuers, kTcCodes = kTcX + 1, kTcEpilogue = kTcCodes + 1;
 constexpr int kTcThreads = 32 * (kTcEpilogue + 4);  // 24 warps: 80 registers each
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-// Shared-memory matrix descriptor of a K-major tile in the 128-byte swizzled layout: start
-// address and offsets in units of 16 bytes, leading offset 1 (unused for swizzled K-major), stride
-// between 8-row groups 1024 bytes, descriptor version 1, layout type 2 (128-byte swizzle).
-__device__ __forceinline__ uint64_t tc_smem_desc(uint32_t addr)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((addr >> 4) & 0x3fffu);
-    d |= (uint64_t)1 << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
 
 // Instruction descriptor: fp32 accumulator, bf16 x bf16, both K-major, M = 128, N = n.
 __host__ __device__ inline uint32_t tc_instr_desc(int n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTcM >> 4) << 24);
 }
-
-__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity)
-{
-    for (uint32_t it = 0; it < kTcSpinLimit; ++it) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(1000u)  // suspended for up to a microsecond instead of polling
-            : "memory");
-        if (ok) return true;
-    }
-    return false;
-}
-
-// A block constant as it is in memory; widened where it is used, so that nothing waits for the load before.
-template <class ST>
-struct TcConst;
-template <>
-struct TcConst<F32> {
-    float v;
-    __device__ __forceinline__ void load(const void* scales, int64_t b)
-    {
-        asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(static_cast<const float*>(scales) + b));
-    }
-    __device__ __forceinline__ float value() const { return v; }
-};
-template <>
-struct TcConst<BF16> {
-    uint16_t v;
-    __device__ __forceinline__ void load(const void* scales, int64_t b)
-    {
-        asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(v) : "l"(static_cast<const uint16_t*>(scales) + b));
-    }
-    __device__ __forceinline__ float value() const { return __uint_as_float((uint32_t)v << 16); }
-};
 
 // Eight codes (even element in the high nibble of its byte) to eight bf16 values (Eq. 3, round to nearest even).
 __device__ __forceinline__ void tc_lookup8(uint32_t w, float2 mm, uint32_t pairs, uint32_t lane8, uint32_t* o)
@@ -173,19 +114,6 @@ __device__ __forceinline__ int2 tc_bracket(const int32_t* __restrict__ idx, int 
     return make_int2(lo, hi);
 }
 
-__device__ __forceinline__ void tc_arrive(unsigned long long* bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_load_box(uint32_t dst, const CUtensorMap* map, unsigned long long* bar, uint32_t bytes, int x, int y)
-{
-    const uint32_t b = smem_u32(bar);
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 :
-                 : "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(b), "r"(x), "r"(y)
-                 : "memory");
-}
 // Sixteen 32-bit columns of the warp's 32 rows in tensor memory.
 __device__ __forceinline__ void tc_store16(uint32_t addr, const uint32_t (&v)[16])
 {
@@ -194,24 +122,6 @@ __device__ __forceinline__ void tc_store16(uint32_t addr, const uint32_t (&v)[16
         :
         : "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
           "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-        : "memory");
-}
-
-// Eight 32-bit columns of the warp's 32 rows from tensor memory.
-__device__ __forceinline__ void tc_load8(uint32_t addr, uint32_t (&v)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-                 : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-// The tensor-core instructions that the lane with lead = 1 has issued arrive on `bar` when they have completed.
-__device__ __forceinline__ void tc_commit(unsigned long long* bar, uint32_t lead)
-{
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %1, 0;\n\t"
-        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(lead)
         : "memory");
 }
 
@@ -237,18 +147,6 @@ __host__ __device__ inline size_t tc_ticket_bytes(int64_t tiles) { return ((size
 __host__ __device__ inline size_t tc_ws_bytes(int64_t tiles, int64_t ctas, int n_rhs)
 {
     return tc_ticket_bytes(tiles) + (size_t)ctas * 2 * kTcM * n_rhs * 4;  // a CTA has at most two parts of tiles
-}
-
-// A tile's ticket.  The cell needs no preparation: every CTA that has a part of the tile first makes sure that
-// it carries the launch's 56-bit epoch (with no arrivals yet), long before it arrives; the last arrival clears it.
-__device__ __forceinline__ void tc_ticket_open(unsigned long long* cell, unsigned long long epoch)
-{
-    unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(cell);
-    while ((old & ~255ull) != epoch) {
-        const unsigned long long seen = atomicCAS(cell, old, epoch);
-        if (seen == old) break;
-        old = seen;  // somebody else opened it or arrived: at most `ctas` rounds
-    }
 }
 
 template <class ST, bool HALF, bool OPQ, bool WIDE>  // HALF: blocks of 32 weights, two constants per row and k-block
@@ -745,57 +643,6 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap code_map, const void* __restr
 
 using namespace bof4;
 
-namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// Tensor map of a row-major matrix of 2-byte or 1-byte elements with a box of 128 bytes x box_rows and the
-// 128-byte swizzle: X lands in the layout that the tcgen05 descriptor of the B operand names, a code
-// line in one that sixteen-byte reads of neighbouring rows find without bank conflicts.
-int make_map(const void* p, bool bytes, int64_t cols, int64_t rows, int box_rows, CUtensorMap* map)
-{
-    static std::atomic<EncodeTiledFn> known{nullptr};
-    EncodeTiledFn fn = known.load(std::memory_order_relaxed);
-    if (!fn) {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        BOF4_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q));
-        if (!f || q != cudaDriverEntryPointSuccess) {
-            set_error("bof4_gemm_tc: the driver does not provide cuTensorMapEncodeTiled");
-            return BOF4_ERR_CUDA;
-        }
-        fn = reinterpret_cast<EncodeTiledFn>(f);
-        known.store(fn, std::memory_order_relaxed);
-    }
-    const int esize = bytes ? 1 : 2;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)cols * esize};
-    const cuuint32_t box[2] = {(cuuint32_t)(128 / esize), (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims,
-                          strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        set_error("bof4_gemm_tc: cuTensorMapEncodeTiled failed with code %d", (int)r);
-        return BOF4_ERR_CUDA;
-    }
-    return BOF4_OK;
-}
-
-// A name for every launch, no two alike: 56 bits that mix a counter with the time the library was loaded.
-unsigned long long next_epoch()
-{
-    static std::atomic<unsigned long long> counter{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count()};
-    unsigned long long z = counter.fetch_add(1) * 0x9e3779b97f4a7c15ull;  // odd: distinct values stay distinct
-    z ^= z >> 29;
-    z &= ~255ull;
-    return z ? z : 256ull;
-}
-
-}  // namespace
-
 extern "C" int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols,
                             int block_size, const float* d_codebook, const void* d_x, int n_rhs,
                             const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity,
@@ -861,11 +708,12 @@ extern "C" int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int sc
     work.ctas = (int)ctas;
     work.each = (int)(lines / work.unit / ctas);
     work.extra = (int)(lines / work.unit % ctas);
-    work.epoch = next_epoch();
+    work.epoch = tc_next_epoch();
     int rc, block_shift = 0;
     while ((1 << block_shift) < block_size) ++block_shift;
     CUtensorMap x_map, code_map;
-    if ((rc = make_map(d_x, false, cols, n_rhs, n_rhs, &x_map)) || (rc = make_map(d_codes, true, cols / 2, rows, kTcM, &code_map)))
+    if ((rc = tc_make_map(fn, d_x, 2, cols, n_rhs, cols * 2, 128, n_rhs, &x_map)) ||
+        (rc = tc_make_map(fn, d_codes, 1, cols / 2, rows, cols / 2, 128, kTcM, &code_map)))
         return rc;
     const bool list = opq && capacity > 0;
     const uint16_t* val = static_cast<const uint16_t*>(d_out_val);

@@ -1,0 +1,527 @@
+// Products of a 4-bit matrix with any number of tokens on the tensor cores (tcgen05), forward and backward:
+//
+//   forward   z[t, r] = sum_c W^[r, c] x[t, c]          M = 128 rows r,    K = columns c
+//   backward  dx[t, c] = sum_r dz[t, r] W^[r, c]         M = 128 columns c, K = rows r
+//
+// W^ is the dequantised weight rounded to bf16, bit for bit what bof4_dequantize writes (Eq. 3), with the stored values of
+// the outliers in their places; products are exact, sums fp32 in tensor memory.  A tile is 128 of M by up to 256 tokens (N),
+// so that a decoded weight is used for up to 256 tokens.
+//
+// The codes of both directions are decoded row by row as they are stored: a thread takes 64 consecutive codes of one row of
+// W, which share a block constant, and writes the 128 bytes of their bf16 values as one row of the A tile.  Forward that row
+// is a row of M with 64 of K (a K-major operand), backward it is one of K with 64 of M (an M-major operand): the tile in
+// shared memory is the same, only the matrix descriptor and the order in which code bytes are fetched differ.
+//
+// Decoding.  A thread forms the 16 possible products constant * level of its block once (eight packed multiplications and
+// conversions for 64 weights) and keeps them in eight registers, the low bytes of the 16 bf16 values in four and the high
+// bytes in four.  A code is then looked up by byte permutes: four codes take two permutes of the lower and the upper eight
+// entries and one that picks between them by bit 3, for the low and for the high bytes, and two that put the bytes together.
+// That is 2.6 instructions per weight of the integer pipe and no shared memory; a table of level pairs in shared memory
+// (gemm_tc.cu) takes 4 bytes of its data path per weight, which the tensor cores need here for their own operands.
+//
+// The work is dealt as in gemm_tc.cu: lines (four k-blocks of 64 of K) of all tiles, tile after tile, in equal contiguous
+// parts to one CTA per SM; a tile that several CTAs share is summed in their order by the one that completes it last (a
+// ticket: nobody waits).  Warps with one job each, coupled by mbarriers:
+//
+//   16 producers  four groups of four warps, a k-block of the line each.  (Every line has four, so that a group is never
+//                 more than four k-blocks behind its next one: with four stages or more a barrier's parity is then
+//                 unambiguous.)
+//   1 issuer      four tcgen05.mma (M = 128, N = tokens, K = 16) per k-block, tcgen05.commit hands the stages back
+//   1 tokens, 1 codes   TMA loads of the B operand and of the code lines
+//   4 results     read a finished accumulator (there are two) while the next tile runs
+//
+// Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
+#include "linear.cuh"
+#include "tc.cuh"
+
+namespace bof4 {
+
+constexpr int kLtGroups = 4;                 // producer groups, a k-block of a line each
+constexpr int kLtM = 128, kLtK = 64;
+constexpr int kLtMaxN = 256;                 // tokens of a tile; columns of an accumulator
+constexpr int kLtABytes = kLtM * kLtK * 2;   // 16 KiB
+constexpr int kLtLineBytes = 16384;          // forward 128 rows x 128 bytes, backward 256 rows x 64 bytes
+constexpr int kLtMaxA = 6, kLtMaxB = 8, kLtMaxLines = 4;
+constexpr int kLtSmem = 214 * 1024;          // rings, with slack to align them to 1024 bytes
+constexpr int kLtIssue = 16, kLtTokens = 17, kLtCodes = 18, kLtResults = 20;  // warp 19 has no job: the results start at a multiple of 4
+constexpr int kLtThreads = 32 * (kLtResults + 4);
+
+struct LtWork {
+    int tiles, tiles_n, per_tile;  // tiles, those along the tokens, lines of a tile
+    int box_n;                     // tokens of a tile, a multiple of 16
+    int sa, sb, sl;                // stages of A, of B, code lines
+    int each, extra;               // lines per CTA, and the remainder
+    unsigned long long epoch;
+    __host__ __device__ int start(int i) const { return i * each + (i < extra ? i : extra); }
+    __device__ int owner(int l) const
+    {
+        const uint32_t longer = (uint32_t)extra * (uint32_t)(each + 1);
+        return (uint32_t)l < longer ? (int)((uint32_t)l / (uint32_t)(each + 1)) : extra + (int)(((uint32_t)l - longer) / (uint32_t)each);
+    }
+};
+
+// Eight products by byte permutes.  lo[0..1], hi[0..1]: bytes of entries 0 ... 7, lo[2..3], hi[2..3]: of 8 ... 15.
+__device__ __forceinline__ void lt_lookup8(uint32_t w, const uint32_t (&lo)[4], const uint32_t (&hi)[4], uint32_t* o)
+{
+    // bits 0 ... 2 of each code select within eight entries; bit 3 selects between the two results of a byte
+    uint32_t s = w & 0x77777777u, t = ((w >> 1) & 0x44444444u) | 0x32103210u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        // result bytes: elements 1, 0, 3, 2 (the even element of a byte is its high nibble)
+        const uint32_t l = __byte_perm(__byte_perm(lo[0], lo[1], s), __byte_perm(lo[2], lo[3], s), t);
+        const uint32_t u = __byte_perm(__byte_perm(hi[0], hi[1], s), __byte_perm(hi[2], hi[3], s), t);
+        o[2 * h] = __byte_perm(l, u, 0x4051);
+        o[2 * h + 1] = __byte_perm(l, u, 0x6273);
+        s >>= 16, t >>= 16;
+    }
+}
+// The 16 products m * level, rounded to bf16, as planes of bytes.
+__device__ __forceinline__ void lt_table(float m, const float2* levels, uint32_t (&lo)[4], uint32_t (&hi)[4])
+{
+    uint32_t p[8];
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const float4 l = reinterpret_cast<const float4*>(levels)[k / 2];
+        const float2 a = __fmul2_rn(make_float2(m, m), make_float2(l.x, l.y)), b = __fmul2_rn(make_float2(m, m), make_float2(l.z, l.w));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(a.y), "f"(a.x));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k + 1]) : "f"(b.y), "f"(b.x));
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        lo[k] = __byte_perm(p[2 * k], p[2 * k + 1], 0x6420);
+        hi[k] = __byte_perm(p[2 * k], p[2 * k + 1], 0x7531);
+    }
+}
+
+__device__ __forceinline__ void lt_load16(uint32_t addr, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr));
+}
+
+// Outliers of a launch, as lists per k-block of a tile and producer warp: a node is {next, place in the warp's 32 x 64
+// weights of the tile << 16 | value}.  Positions are distinct, so the order within a list does not matter.
+__global__ void __launch_bounds__(256)
+linear_outlier_lists(const int32_t* __restrict__ idx, const uint16_t* __restrict__ val, const int64_t* __restrict__ n_out, int64_t capacity,
+                     int64_t rows, int64_t cols, bool backward, int blocks, int* __restrict__ heads, int2* __restrict__ nodes)
+{
+    if (!after_previous()) return;
+    int64_t end = *n_out;
+    if (end > capacity) end = capacity;
+    const int64_t n = rows * cols;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < end; k += (int64_t)gridDim.x * 256) {
+        const int64_t i = idx[k];
+        if (i < 0 || i >= n) continue;
+        const int r = (int)(i / cols), c = (int)(i - (int64_t)r * cols);
+        const int thread = backward ? (c >> 6 & 1) * 64 + (r & 63) : r & 127;
+        const int64_t tile = backward ? c >> 7 : r >> 7, block = backward ? r >> 6 : c >> 6;
+        const int next = atomicExch(heads + (tile * blocks + block) * 4 + (thread >> 5), (int)k);
+        nodes[k] = make_int2(next, (int)((uint32_t)((thread & 31) << 6 | (c & 63)) << 16 | val[k]));
+    }
+}
+
+template <bool BWD, class ST, bool HALF, bool OPQ>  // HALF: blocks of 32 weights, two constants per thread and k-block
+__global__ void __launch_bounds__(kLtThreads, 1)
+linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap token_map, const void* __restrict__ scales,
+                 int64_t cols, int block_shift, int64_t last_scale, const float* __restrict__ levels, const LinearOut out,
+                 int* __restrict__ status, const int* __restrict__ heads, const int2* __restrict__ nodes, const LtWork work,
+                 unsigned char* __restrict__ ws, float* __restrict__ parts)
+{
+    extern __shared__ unsigned char s_dyn[];
+    __shared__ __align__(8) unsigned long long s_a_full[kLtMaxA], s_a_empty[kLtMaxA], s_b_full[kLtMaxB], s_b_empty[kLtMaxB],
+        s_line_full[kLtMaxLines], s_line_empty[kLtMaxLines], s_acc_full[2], s_acc_empty[2];
+    __shared__ __align__(16) float2 s_levels[8];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_fail, s_sums, s_sum[2];
+    if (!after_previous()) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per_tile = work.per_tile, box_n = work.box_n;
+    const uint32_t b_stage = (uint32_t)box_n * 128u;  // a multiple of 2048
+    const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)work.sa * kLtABytes;
+    const uint32_t b_ring = code_ring + (uint32_t)work.sl * kLtLineBytes;
+    const int begin = work.start((int)blockIdx.x), finish = work.start((int)blockIdx.x + 1), lines = finish - begin;
+    const int tile0 = (int)((uint32_t)begin / (uint32_t)per_tile), in0 = begin - tile0 * per_tile;
+    const int segs = lines ? (in0 + lines - 1) / per_tile + 1 : 0;
+    auto warp_wait = [&](unsigned long long* bar, uint32_t parity) -> bool {
+        if (__all_sync(kFull, tc_wait(smem_u32(bar), parity))) return true;
+        if (lane == 0) s_fail = 1;
+        return false;
+    };
+    auto init = [&](unsigned long long* bar, int count) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
+    };
+    if (tid == 0) {
+        if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
+        s_fail = s_sums = 0;
+        for (int s = 0; s < work.sa; ++s) init(&s_a_full[s], 4), init(&s_a_empty[s], 1);
+        for (int s = 0; s < work.sb; ++s) init(&s_b_full[s], 1), init(&s_b_empty[s], 1);
+        for (int s = 0; s < work.sl; ++s) init(&s_line_full[s], 1), init(&s_line_empty[s], 4 * kLtGroups);
+        for (int b = 0; b < 2; ++b) init(&s_acc_full[b], 1), init(&s_acc_empty[b], 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid >= 32 && tid < 40) s_levels[tid - 32] = make_float2(__ldg(levels + 2 * (tid - 32)), __ldg(levels + 2 * (tid - 32) + 1));
+    if (warp == kLtIssue) {  // tensor memory: two accumulators of 256 columns
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(2 * kLtMaxN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+
+    if (warp < kLtIssue) {
+        // ---- producers
+        const int group = warp >> 2, thread = (warp & 3) * 32 + lane;
+        const int row = BWD ? thread & 63 : thread, half = BWD ? thread >> 6 : 0;  // of W within the k-block (backward), the tile (forward)
+        int tile = tile0, in = in0, ct = tile0, ci = in0;
+        // block constants three lines ahead (past the end: the last ones again; outside the matrix: its last one)
+        TcConst<ST> c0, c1, c2, d0, d1, d2;
+        auto constants = [&](TcConst<ST>& c, TcConst<ST>& d) {
+            const int64_t tm = (uint32_t)ct / (uint32_t)work.tiles_n, k = (int64_t)ci * kLtGroups + group;
+            const int64_t i = BWD ? (k * kLtK + row) * cols + tm * kLtM + half * 64 : (tm * kLtM + row) * cols + k * kLtK;
+            const int64_t b = i >> block_shift;
+            c.load(scales, b < last_scale ? b : last_scale);
+            if (HALF) d.load(scales, b + 1 < last_scale ? b + 1 : last_scale);
+            if (ct * per_tile + ci + 1 < finish && ++ci == per_tile) ci = 0, ++ct;
+        };
+        if (lines) constants(c0, d0), constants(c1, d1), constants(c2, d2);
+        int line = 0, s = 0;
+        uint32_t line_par = 0, par = 0;
+        for (int n = 0; n < lines; ++n) {
+            if (!warp_wait(&s_line_full[line], line_par)) break;
+            uint32_t w[8];
+            {
+                const int r = BWD ? group * 64 + row : row;  // row of the line
+                const uint32_t at = code_ring + (uint32_t)line * kLtLineBytes + (uint32_t)r * (BWD ? 64u : 128u);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int chunk = BWD ? (2 * half + h) ^ ((r >> 1) & 3) : (2 * group + h) ^ (r & 7);
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
+                                 : "r"(at + (uint32_t)chunk * 16u));
+                }
+            }
+            const float m = c0.value(), m2 = HALF ? d0.value() : m;
+            c0 = c1, c1 = c2;
+            if (HALF) d0 = d1, d1 = d2;
+            constants(c2, d2);
+            int head = -1;
+            if (OPQ) head = __ldg(heads + (((int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * per_tile + in) * kLtGroups + group) * 4 + (warp & 3));
+            uint32_t lo[4], hi[4], v[16];
+            lt_table(m, s_levels, lo, hi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
+            int st = s + group;
+            uint32_t p = par;
+            if (st >= work.sa) st -= work.sa, p ^= 1u;
+            if (!warp_wait(&s_a_empty[st], p ^ 1u)) break;
+            const uint32_t at = a_ring + (uint32_t)st * kLtABytes + (uint32_t)thread * 128u, x = (uint32_t)(thread & 7);
+            auto store = [&](int j, const uint32_t* q) {
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((uint32_t)j ^ x) << 4)), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
+            };
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store(j, v + 4 * j);
+            if (HALF) lt_table(m2, s_levels, lo, hi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lt_lookup8(w[4 + j], lo, hi, v + 4 * j);
+                store(4 + j, v + 4 * j);
+            }
+            if (OPQ) {
+                while (head >= 0) {  // the same list for all lanes; a lane patches its own row
+                    const int2 e = __ldg(nodes + head);
+                    const uint32_t place = (uint32_t)e.y >> 16;
+                    if ((int)(place >> 6) == lane) {
+                        const uint32_t c = place & 63u;
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + (((c >> 3) ^ x) << 4) + (c & 7u) * 2u), "h"((uint16_t)e.y) : "memory");
+                    }
+                    head = e.x;
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                tc_arrive(&s_line_empty[line]);
+                tc_arrive(&s_a_full[st]);
+            }
+            if ((s += kLtGroups) >= work.sa) s -= work.sa, par ^= 1u;
+            if (++line == work.sl) line = 0, line_par ^= 1u;
+            if (++in == per_tile) in = 0, ++tile;
+        }
+    } else if (warp == kLtIssue) {
+        // ---- the issuing warp
+        const uint32_t lead = lane == 0 ? 1u : 0u;
+        const uint64_t da0 = tc_smem_desc(a_ring, BWD ? 8192u : 16u), db0 = tc_smem_desc(b_ring);
+        // fp32 accumulator, bf16 x bf16, A M-major (backward) or K-major, B K-major, M = 128, N
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (BWD ? 1u << 15 : 0u) | ((uint32_t)(box_n >> 3) << 17) | ((uint32_t)(kLtM >> 4) << 24);
+        constexpr uint64_t a_step = BWD ? 2048 >> 4 : 32 >> 4;  // 16 of K
+        int in = in0, seg = 0, sa = 0, sb = 0;
+        uint32_t acc = 0u, pa = 0, pb = 0;
+        bool ok = true;
+        for (int n = 0; ok && n < lines; ++n) {
+            const int buf = seg & 1;
+            if (acc == 0u && !(ok = warp_wait(&s_acc_empty[buf], (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
+            for (int j = 0; j < kLtGroups; ++j) {
+                if (!(ok = warp_wait(&s_b_full[sb], pb) && warp_wait(&s_a_full[sa], pa))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t da = da0 + (uint64_t)(sa * (kLtABytes >> 4)), db = db0 + (uint64_t)(sb * (b_stage >> 4));
+#pragma unroll
+                for (int kk = 0; kk < kLtK / 16; ++kk) {
+                    asm volatile(
+                        "{\n\t.reg .pred p, q;\n\t"
+                        "setp.ne.b32 p, %4, 0;\n\t"
+                        "setp.ne.b32 q, %5, 0;\n\t"
+                        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                        :
+                        : "r"(tmem + (uint32_t)(buf * kLtMaxN)), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc), "r"(lead)
+                        : "memory");
+                    acc = 1u;
+                }
+                tc_commit(&s_a_empty[sa], lead);
+                tc_commit(&s_b_empty[sb], lead);
+                if (++sa == work.sa) sa = 0, pa ^= 1u;
+                if (++sb == work.sb) sb = 0, pb ^= 1u;
+            }
+            if (ok && (++in == per_tile || n + 1 == lines)) {  // the end of a part of a tile
+                tc_commit(&s_acc_full[buf], lead);
+                in = 0, ++seg, acc = 0u;
+            }
+        }
+    } else if (warp == kLtTokens) {
+        // ---- the B operand: 64 of K of the tile's tokens
+        int tile = tile0, in = in0, sb = 0;
+        uint32_t pb = 0;
+        bool ok = true;
+        for (int n = 0; ok && n < lines; ++n) {
+            const int t0 = (int)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
+            for (int j = 0; ok && j < kLtGroups; ++j) {
+                if (!(ok = warp_wait(&s_b_empty[sb], pb ^ 1u))) break;
+                if (lane == 0) tc_load_box(b_ring + (uint32_t)sb * b_stage, &token_map, &s_b_full[sb], b_stage, (in * kLtGroups + j) * kLtK, t0);
+                __syncwarp();
+                if (++sb == work.sb) sb = 0, pb ^= 1u;
+            }
+            if (++in == per_tile) in = 0, ++tile;
+        }
+    } else if (warp == kLtCodes) {
+        // ---- code lines
+        int tile = tile0, in = in0, line = 0;
+        uint32_t par = 0;
+        for (int n = 0; n < lines; ++n) {
+            if (!warp_wait(&s_line_empty[line], par ^ 1u)) break;
+            const int tm = (int)((uint32_t)tile / (uint32_t)work.tiles_n);
+            if (lane == 0)
+                tc_load_box(code_ring + (uint32_t)line * kLtLineBytes, &code_map, &s_line_full[line], kLtLineBytes, BWD ? tm * 64 : in * 128, BWD ? in * 256 : tm * kLtM);
+            __syncwarp();
+            if (++line == work.sl) line = 0, par ^= 1u;
+            if (++in == per_tile) in = 0, ++tile;
+        }
+    } else if (warp >= kLtResults) {
+        // ---- results of the parts of tiles
+        const int f = tid - kLtResults * 32, m = (warp & 3) * 32 + lane;
+        unsigned long long* const tickets = reinterpret_cast<unsigned long long*>(ws);
+        if (f == 0 && segs) {
+            if (in0 || lines < per_tile) tc_ticket_open(tickets + tile0, work.epoch);
+            if (segs > 1 && (in0 + lines) % per_tile) tc_ticket_open(tickets + tile0 + segs - 1, work.epoch);
+        }
+        auto sync = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+        auto all4 = [](bool ok) -> bool {
+            uint32_t r;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(ok ? 1u : 0u) : "memory");
+            return r != 0u;
+        };
+        for (int seg = 0; seg < segs; ++seg) {
+            const int buf = seg & 1;
+            if (!all4(warp_wait(&s_acc_full[buf], (uint32_t)(seg >> 1) & 1u))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const int tile = tile0 + seg, t0 = tile * per_tile;
+            const int64_t o = (int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * kLtM + m, token0 = (int64_t)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
+            const int count = (int)(out.tokens - token0 < box_n ? out.tokens - token0 : box_n);
+            const bool all = begin <= t0 && finish >= t0 + per_tile, live = o < out.n;
+            const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * kLtMaxN);
+            float* const part = parts + (2 * (int64_t)blockIdx.x + (begin <= t0 ? 1 : 0)) * kLtM * box_n;
+            const float b = all && live ? out.bias_at(o) : 0.0f;
+            for (int q = 0; q < count; q += 16) {
+                uint32_t a[16];
+                __syncwarp();
+                lt_load16(src + (uint32_t)q, a);
+                float r[16];
+                if (all && live) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) r[k] = q + k < count ? out.residual_at(token0 + q + k, o) : 0.0f;
+                }
+                __syncwarp();
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                if (!all) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (q + k < count) part[(q + k) * kLtM + m] = __uint_as_float(a[k]);
+                } else if (live) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (q + k < count) out.store(__uint_as_float(a[k]), b, r[k], token0 + q + k, o);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) tc_arrive(&s_acc_empty[buf]);
+            if (all) continue;
+            const int others = work.owner(t0 + per_tile - 1) - work.owner(t0);
+            __threadfence();
+            sync();
+            if (f == 0 && (int)(atomicAdd(tickets + tile, 1ull) & 255ull) == others) {
+                tickets[tile] = 0ull;
+                s_sum[s_sums++] = tile;
+            }
+        }
+    }
+    // Every loop above is bounded, so every warp gets here.
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (s_fail) {
+        // copies and tensor-core instructions issued before the time-out may still be under way: they take
+        // microseconds; give them a bounded 100 before shared and tensor memory go away
+        if (tid == 0) atomicExch(status, 1);
+        for (int i = 0; i < 100; ++i) __nanosleep(1000);
+    }
+    for (int k = 0; k < s_sums; ++k) {  // the parts in the order of the CTAs; all but the first begin inside the tile
+        const int tile = s_sum[k], t0 = tile * per_tile, i0 = work.owner(t0), more = work.owner(t0 + per_tile - 1) - i0;
+        const int64_t o0 = (int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * kLtM, token0 = (int64_t)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
+        const int count = (int)(out.tokens - token0 < box_n ? out.tokens - token0 : box_n);
+        const int64_t slab = (int64_t)(kLtM / 4) * box_n;
+        __threadfence();
+        const float4* head = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + (work.start(i0) <= t0 ? 1 : 0)) * slab;
+        const float4* next = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + 2) * slab;
+        for (int e = tid; e < count * (kLtM / 4); e += kLtThreads) {
+            float4 sum = __ldcg(head + e);
+            for (int i = 0; i < more; i += 4) {
+                float4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = i + u < more ? __ldcg(next + (int64_t)(2 * (i + u)) * slab + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
+            }
+            const float z[4] = {sum.x, sum.y, sum.z, sum.w};
+            const int64_t o = o0 + (e & 31) * 4, t = token0 + (e >> 5);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (o + u < out.n) out.store(z[u], out.bias_at(o + u), out.residual_at(t, o + u), t, o + u);
+        }
+    }
+    if (warp == kLtIssue)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kLtMaxN) : "memory");
+}
+
+// ---------------------------------------------------------------- host side
+
+namespace {
+
+struct LtPlan {
+    LtWork work{};
+    int ctas = 0, blocks = 0;
+    int64_t tiles_m = 0;
+    size_t parts = 0, heads = 0, nodes = 0, total = 0;  // byte offsets (the tickets are at 0), and the bytes of all
+};
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// False: too large for 32-bit line numbers.
+bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t capacity, LtPlan* p)
+{
+    const int64_t m = backward ? cols : rows, k = backward ? rows : cols;
+    // (k-blocks past the end of K have zeros for the tokens)
+    const int64_t tiles_m = (m + kLtM - 1) / kLtM, per_tile = (k + kLtK * kLtGroups - 1) / (kLtK * kLtGroups), blocks = per_tile * kLtGroups;
+    const int64_t most_n = (tokens + kLtMaxN - 1) / kLtMaxN;
+    // the tokens are dealt evenly over the tiles, in multiples of 16
+    const int64_t box = ((tokens + most_n - 1) / most_n + 15) & ~(int64_t)15, tiles_n = (tokens + box - 1) / box, tiles = tiles_m * tiles_n;
+    if (tiles_m > (1 << 24) || tokens > 0x7fffff00 || k > 0x7fffff00 || tiles > 0x3fffffff || tiles * per_tile > 0x3fffffff) return false;
+    LtWork& w = p->work;
+    w.tiles = (int)tiles;
+    w.tiles_n = (int)tiles_n;
+    w.per_tile = (int)per_tile;
+    w.box_n = (int)box;
+    w.sl = box > 128 ? 3 : 4;
+    w.sa = box > 128 ? 4 : 6;
+    w.sb = (int)((kLtSmem - 1024 - w.sl * kLtLineBytes - w.sa * kLtABytes) / (box * 128));
+    if (w.sb > kLtMaxB) w.sb = kLtMaxB;
+    // One CTA per SM, each with an equal part of the lines.  A tile is cut into at most so many parts that summing them
+    // stays short beside the product: 16384 / tokens.
+    const int64_t lines = tiles * per_tile, most = tiles * (16384 / box < 64 ? 16384 / box : 64);
+    int64_t ctas = lines < kSMs ? lines : kSMs;
+    if (ctas > most) ctas = most;
+    p->ctas = (int)ctas;
+    w.each = (int)(lines / ctas);
+    w.extra = (int)(lines % ctas);
+    p->blocks = (int)blocks;
+    p->tiles_m = tiles_m;
+    p->parts = up256((size_t)tiles * 8);
+    p->heads = p->parts + up256((size_t)ctas * 2 * kLtM * box * 4);
+    p->nodes = p->heads + (capacity > 0 ? up256((size_t)tiles_m * blocks * 16) : 0);
+    p->total = p->nodes + (capacity > 0 ? up256((size_t)capacity * 8) : 0);
+    return true;
+}
+
+}  // namespace
+
+size_t linear_tc_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t capacity)
+{
+    LtPlan p;
+    return lt_plan(rows, cols, tokens, backward, capacity, &p) ? p.total : 0;
+}
+
+int linear_tc(const char* who, const LinearW& w, bool backward, const void* operand, int64_t ld, const LinearOut& out, int* status,
+              void* ws, size_t ws_bytes, cudaStream_t st)
+{
+    LtPlan p;
+    const bool opq = w.out_idx && w.capacity > 0;
+    if (!lt_plan(w.rows, w.cols, out.tokens, backward, opq ? w.capacity : 0, &p)) {
+        set_error("%s: matrix or batch too large", who);
+        return BOF4_ERR_SHAPE;
+    }
+    if (ws_bytes < p.total) {
+        set_error("%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes, p.total);
+        return BOF4_ERR_WORKSPACE;
+    }
+    unsigned char* const base = static_cast<unsigned char*>(ws);
+    p.work.epoch = tc_next_epoch();
+    CUtensorMap code_map, token_map;
+    int rc;
+    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, backward ? 64 : 128, backward ? 256 : kLtM, &code_map)) ||
+        (rc = tc_make_map(who, operand, 2, backward ? w.rows : w.cols, out.tokens, ld * 2, 128, p.work.box_n, &token_map)))
+        return rc;
+    int* heads = nullptr;
+    int2* nodes = nullptr;
+    if (opq) {
+        heads = reinterpret_cast<int*>(base + p.heads);
+        nodes = reinterpret_cast<int2*>(base + p.nodes);
+        BOF4_CUDA_TRY(cudaMemsetAsync(heads, 0xff, (size_t)p.tiles_m * p.blocks * 16, st));
+        const int64_t want = (w.capacity + 255) / 256;
+        launch_after(linear_outlier_lists, (int)(want < 4 * kSMs ? want : 4 * kSMs), 256, 0, st, w.out_idx, w.out_val, w.n_out, w.capacity, w.rows,
+                     w.cols, backward, p.blocks, heads, nodes);
+        BOF4_CUDA_TRY(cudaGetLastError());
+    }
+    const int64_t last_scale = w.rows * w.cols / w.block_size - 1;
+    float* const parts = reinterpret_cast<float*>(base + p.parts);
+#define BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_)                                                                                                        \
+    {                                                                                                                                             \
+        constexpr auto kern = linear_tc_kernel<BWD_, ST_, HALF_, OPQ_>;                                                                           \
+        if ((rc = ensure_dynamic_smem<kern>(kLtSmem))) return rc;                                                                                 \
+        launch_after(kern, p.ctas, kLtThreads, kLtSmem, st, code_map, token_map, w.scales, w.cols, w.block_shift, last_scale, w.levels, out,      \
+                     status, heads, nodes, p.work, base, parts);                                                                                  \
+    }
+#define BOF4_LT_O(BWD_, ST_, HALF_) { if (opq) BOF4_LT_GO(BWD_, ST_, HALF_, true) else BOF4_LT_GO(BWD_, ST_, HALF_, false) }
+#define BOF4_LT_H(BWD_, ST_) { if (w.block_size == 32) BOF4_LT_O(BWD_, ST_, true) else BOF4_LT_O(BWD_, ST_, false) }
+#define BOF4_LT_S(BWD_) { if (w.scale_dtype == BOF4_F32) BOF4_LT_H(BWD_, F32) else BOF4_LT_H(BWD_, BF16) }
+    if (backward) BOF4_LT_S(true) else BOF4_LT_S(false)
+#undef BOF4_LT_S
+#undef BOF4_LT_H
+#undef BOF4_LT_O
+#undef BOF4_LT_GO
+    BOF4_CUDA_TRY(cudaGetLastError());
+    return BOF4_OK;
+}
+
+}  // namespace bof4

@@ -19,6 +19,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <optional>
 #include <vector>
 
 #include "../../include/bof4.h"
@@ -410,6 +411,137 @@ PyObject* gemm_tc(PyObject* const* a)
     return PyTuple_Pack(2, ry.p, rs.p);
 }
 
+// A CUDA tensor [n, cols] whose rows may be apart from one another, of type dt.
+struct Rows {
+    at::Tensor t;  // owned: other threads may run before it is used
+    int64_t ld = 0;
+    Rows(PyObject* o, const char* name, int64_t n, int64_t cols, at::ScalarType dt, at::Device d) : t(tensor(o, name))
+    {
+        if (!t.is_cuda() || t.device() != d) failf(PyExc_ValueError, "%s must be a CUDA tensor on the device of the weights", name);
+        if (t.scalar_type() != dt) failf(PyExc_TypeError, "%s must be %s, got %s", name, c10::toString(dt), c10::toString(t.scalar_type()));
+        if (t.dim() != 2 || t.size(0) != n || t.size(1) != cols)
+            failf(PyExc_ValueError, "%s must have shape [%lld, %lld]", name, (long long)n, (long long)cols);
+        if (cols > 1 && n > 0 && t.stride(1) != 1) failf(PyExc_ValueError, "the values of a row of %s must be contiguous", name);
+        ld = n > 1 ? t.stride(0) : cols;
+        if (n > 1 && ld < cols) failf(PyExc_ValueError, "the rows of %s must not overlap", name);
+    }
+    void* ptr() const { return t.data_ptr(); }
+};
+// A workspace given by the caller: a contiguous CUDA tensor of bytes on the device of the call.
+at::Tensor given_workspace(PyObject* o, at::Device d)
+{
+    const at::Tensor& t = dev(o, "workspace");
+    if (t.scalar_type() != at::kByte || t.device() != d) fail(PyExc_ValueError, "workspace must be a uint8 tensor on the device of the weights");
+    return t;
+}
+void check_matrix(const at::Tensor& codes, const at::Tensor& scales, int64_t rows, int64_t cols, int64_t block)
+{
+    int64_t n = 0;
+    if (rows < 0 || cols < 0 || __builtin_mul_overflow(rows, cols, &n) || codes.scalar_type() != at::kByte || codes.numel() * 2 != n)
+        fail(PyExc_ValueError, "codes must be uint8 and hold rows * cols weights");
+    if (block < 1 || scales.numel() != n / block || scales.device() != codes.device())
+        fail(PyExc_ValueError, "scales must hold one constant per block, on the device of the codes");
+}
+void check_outliers(const Outliers& o, at::Device d)
+{
+    if (!o.idx) return;
+    if (o.own[0].scalar_type() != at::kInt || o.own[1].scalar_type() != at::kBFloat16 || o.own[2].scalar_type() != at::kLong ||
+        o.own[1].numel() < o.cap || o.own[2].numel() != 1 || o.own[0].device() != d || o.own[1].device() != d || o.own[2].device() != d)
+        fail(PyExc_ValueError, "outliers must be (idx int32, val bfloat16, n_out int64[1]) on the device of the weights");
+}
+
+// (codes, scales, rows, cols, block_size, levels, x, bias, residual, activation, out_dtype, pre, outliers, out, workspace)
+PyObject* linear(PyObject* const* a)
+{
+    const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
+    const int64_t rows = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
+    check_matrix(codes, scales, rows, cols, block);
+    const at::Device d = codes.device();
+    if (tensor(a[6], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, cols]");
+    const int64_t n = tensor(a[6], "x").size(0);
+    const Rows x(a[6], "x", n, cols, at::kBFloat16, d);
+    const int od = (int)integer(a[10]), act = (int)integer(a[9]), sd = dtype_code(scales);
+    if (od != BOF4_F32 && od != BOF4_BF16) fail(PyExc_ValueError, "out_dtype must be F32 or BF16");
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[5], d);
+    const Outliers o(a[12]);
+    check_outliers(o, d);
+    at::Tensor bias;
+    int bd = BOF4_F32;
+    if (!none(a[7])) {
+        bias = dev(a[7], "bias");
+        bd = dtype_code(bias);
+        if (bias.numel() != rows || bias.device() != d) fail(PyExc_ValueError, "bias must hold one value per row, on the device of the weights");
+    }
+    std::optional<Rows> res, pre, out;
+    if (!none(a[8])) res.emplace(a[8], "residual", n, rows, torch_dtype(od), d);
+    if (!none(a[11])) pre.emplace(a[11], "pre", n, rows, at::kBFloat16, d);
+    if (!none(a[13])) out.emplace(a[13], "out", n, rows, torch_dtype(od), d);
+    at::Tensor made[3], ws;  // the status (written by the call), the workspace, the result
+    Spec spec[3];
+    size_t k = 0;
+    spec[k++] = {1, at::kInt};
+    const size_t i_ws = k;
+    if (none(a[14])) spec[k++] = {(int64_t)bof4_linear_workspace_bytes(rows, cols, n, 0, o.idx ? o.cap : 0), at::kByte};
+    else ws = given_workspace(a[14], d);
+    const size_t i_y = k;
+    if (!out) spec[k++] = {n * rows, torch_dtype(od)};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        return bof4_linear(static_cast<const uint8_t*>(codes.const_data_ptr()), scales.const_data_ptr(), sd, rows, cols, (int)block, levels_ptr(cb),
+                           x.ptr(), x.ld, n, bias.defined() ? bias.const_data_ptr() : nullptr, bd, res ? res->ptr() : nullptr, res ? res->ld : 0,
+                           act, o.idx, o.val, o.cnt, o.cap, out ? out->ptr() : made[i_y].data_ptr(), od, out ? out->ld : rows,
+                           pre ? pre->ptr() : nullptr, pre ? pre->ld : 0, static_cast<int*>(made[0].data_ptr()), w.data_ptr(), (size_t)w.numel(),
+                           stream_of(d));
+    });
+    Ref rs(wrap(made[0])), ry(out ? Py_NewRef(a[13]) : wrap(made[i_y].view({n, rows})));
+    return PyTuple_Pack(2, ry.p, rs.p);
+}
+
+// (codes, scales, rows, cols, block_size, levels, dy, pre, activation, want_dx, want_dbias, outliers, out, workspace)
+PyObject* linear_backward(PyObject* const* a)
+{
+    const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
+    const int64_t rows = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
+    check_matrix(codes, scales, rows, cols, block);
+    const at::Device d = codes.device();
+    if (tensor(a[6], "dy").dim() != 2) fail(PyExc_ValueError, "dy must be [n_tokens, rows]");
+    const int dd = dtype_code(tensor(a[6], "dy")), act = (int)integer(a[8]), sd = dtype_code(scales);
+    const int64_t n = tensor(a[6], "dy").size(0);
+    const Rows dy(a[6], "dy", n, rows, torch_dtype(dd), d);
+    const bool want_dx = PyObject_IsTrue(a[9]) == 1, want_db = PyObject_IsTrue(a[10]) == 1;
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[5], d);
+    const Outliers o(a[11]);
+    check_outliers(o, d);
+    std::optional<Rows> pre, out;
+    if (!none(a[7])) pre.emplace(a[7], "pre", n, rows, at::kBFloat16, d);
+    if (!none(a[12])) out.emplace(a[12], "out", n, cols, at::kBFloat16, d);
+    at::Tensor made[4], ws;
+    Spec spec[4];
+    size_t k = 0;
+    spec[k++] = {1, at::kInt};
+    const size_t i_db = k;
+    if (want_db) spec[k++] = {rows, at::kFloat};
+    const size_t i_ws = k;
+    if (none(a[13])) spec[k++] = {(int64_t)bof4_linear_workspace_bytes(rows, cols, n, 1, o.idx ? o.cap : 0), at::kByte};
+    else ws = given_workspace(a[13], d);
+    const size_t i_dx = k;
+    if (want_dx && !out) spec[k++] = {n * cols, at::kBFloat16};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        void* const dx = !want_dx ? nullptr : out ? out->ptr() : made[i_dx].data_ptr();
+        return bof4_linear_backward(static_cast<const uint8_t*>(codes.const_data_ptr()), scales.const_data_ptr(), sd, rows, cols, (int)block,
+                                    levels_ptr(cb), dy.ptr(), dd, dy.ld, n, pre ? pre->ptr() : nullptr, pre ? pre->ld : 0, act, o.idx, o.val,
+                                    o.cnt, o.cap, dx, out ? out->ld : cols, want_db ? static_cast<float*>(made[i_db].data_ptr()) : nullptr,
+                                    static_cast<int*>(made[0].data_ptr()), w.data_ptr(), (size_t)w.numel(), stream_of(d));
+    });
+    Ref rs(wrap(made[0]));
+    Ref rdx(!want_dx ? Py_NewRef(Py_None) : out ? Py_NewRef(a[12]) : wrap(made[i_dx].view({n, cols})));
+    Ref rdb(want_db ? wrap(made[i_db]) : Py_NewRef(Py_None));
+    return PyTuple_Pack(3, rdx.p, rdb.p, rs.p);
+}
+
 // (w, block_size, norm, levels, tau, capacity, scale_dtype, workspace, out)
 PyObject* quantize_opq(PyObject* const* a)
 {
@@ -662,7 +794,7 @@ PyMethodDef g_methods[] = {
     BOF4_ENTRY(set_hooks, 2), BOF4_ENTRY(set_allocator, 1), BOF4_ENTRY(quantize, 6), BOF4_ENTRY(dequantize, 8),
     BOF4_ENTRY(gemv, 9), BOF4_ENTRY(gemm_tc, 10), BOF4_ENTRY(quantize_opq, 9), BOF4_ENTRY(outlier_count, 2),
     BOF4_ENTRY(quantize_batch, 6), BOF4_ENTRY(dequantize_batch, 7), BOF4_ENTRY(scales_compress, 2), BOF4_ENTRY(scales_expand, 3),
-    BOF4_ENTRY(fit_codebook, 10), {nullptr, nullptr, 0, nullptr}};
+    BOF4_ENTRY(fit_codebook, 10), BOF4_ENTRY(linear, 15), BOF4_ENTRY(linear_backward, 14), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bof4_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
