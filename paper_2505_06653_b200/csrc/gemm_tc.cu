@@ -44,6 +44,7 @@
 // memory and returns.
 #include <type_traits>
 
+#include "decode.cuh"
 #include "tc.cuh"
 
 namespace bof4 {
@@ -79,20 +80,6 @@ constexpr int kTcThreads = 32 * (kTcEpilogue + 4);  // 24 warps: 80 registers ea
 __host__ __device__ inline uint32_t tc_instr_desc(int n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTcM >> 4) << 24);
-}
-
-// Eight codes (even element in the high nibble of its byte) to eight bf16 values (Eq. 3, round to nearest even).
-__device__ __forceinline__ void tc_lookup8(uint32_t w, float2 mm, uint32_t pairs, uint32_t lane8, uint32_t* o)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        // byte * 256 + lane * 8 in one permute
-        const uint32_t off = __byte_perm(w, lane8, 0x5504u | ((uint32_t)k << 4));
-        float2 l;
-        asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l.x), "=f"(l.y) : "r"(pairs + off));
-        const float2 v = __fmul2_rn(mm, l);
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[k]) : "f"(v.y), "f"(v.x));
-    }
 }
 
 // Brackets the first entry of the ascending list with idx >= key to 32 places, by one warp: a guess from the

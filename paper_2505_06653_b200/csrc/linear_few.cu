@@ -1,0 +1,267 @@
+// bof4_linear for one to sixteen tokens: a product that is bound by its codes.
+//
+// A CTA holds `groups` row groups of `stripes` warps.  Warp s of a group owns 256 columns of a slice of the columns for every
+// row tile (16 rows) that the group visits, its tokens in registers (decode.cuh).  The parts of a row tile are added up over
+// the stripes in shared memory, in a fixed order, a few row tiles at a time (two buffers, one barrier per kFewDefer tiles).
+// A matrix with more columns than a CTA has warps for is cut into slices of equal numbers of stripes; the CTAs of a slice
+// take the same row tiles as their counterparts in the others, leave their sums in the workspace, and the one that is last
+// (a ticket: nobody waits) adds the slices up in order.
+#include "decode.cuh"
+#include "linear.cuh"
+#include "tc.cuh"
+
+namespace bof4 {
+
+constexpr int kFewDefer = 4;
+template <int NT>
+struct FewGeo {
+    // a lane keeps 32 registers of tokens per eight of them: 128 registers a thread for 8 tokens, 255 for 16
+    static constexpr int warps = NT == 1 ? 16 : 8, threads = 32 * warps;
+    static constexpr int part = 16 * 8 * NT;  // sums of a warp and row tile
+    static constexpr int smem = kPairBytes + 2 * kFewDefer * warps * part * 4;
+};
+
+struct FewWork {
+    int stripes, groups, slices, peers;  // stripes of a slice; CTAs of a slice
+    int tiles;
+    unsigned long long epoch;
+};
+
+template <int NT, class ST, bool HALF>
+__global__ void __launch_bounds__(FewGeo<NT>::threads, 1)
+linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
+                  const float* __restrict__ levels, const uint16_t* __restrict__ x, int64_t ldx, const LinearOut out,
+                  const float* __restrict__ correction, int* __restrict__ status, const FewWork work, unsigned long long* __restrict__ tickets,
+                  float* __restrict__ sums)
+{
+    if (!after_previous()) return;
+    constexpr int W = FewGeo<NT>::warps, P = FewGeo<NT>::part, D = kFewDefer;
+    extern __shared__ __align__(256) unsigned char s_dyn[];
+    float2* const s_pairs = reinterpret_cast<float2*>(s_dyn);
+    float* const s_part = reinterpret_cast<float*>(s_dyn + kPairBytes);  // [2][D][W][P]
+    __shared__ __align__(16) float2 s_levels[8];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
+    const int group = warp / work.stripes, stripe = warp - group * work.stripes;
+    const int slice = (int)blockIdx.x / work.peers, peer = (int)blockIdx.x - slice * work.peers;
+    const int64_t c0 = (int64_t)(slice * work.stripes + stripe) * kFewStripe + 64 * q;
+    const bool busy = group < work.groups, live0 = busy && c0 < cols, live1 = busy && c0 + 32 < cols;
+    const int first = peer * work.groups + group, step = work.peers * work.groups;  // row tiles of this group
+    const int rounds = (work.tiles - peer * work.groups + step - 1) / step;         // of the CTA: its first group has the most
+    const int tokens = (int)out.tokens;
+    if (tid == 0) {
+        if (blockIdx.x == 0) *status = 0;
+        if (work.slices > 1) tc_ticket_open(tickets + peer, work.epoch);
+    }
+    FewCodes code;
+    float m[4];
+    auto fetch = [&](int i, FewCodes& c, float (&s)[4]) {
+        const int64_t r0 = ((int64_t)first + (int64_t)i * step) * 16 + g, r1 = r0 + 8;
+        const bool a = r0 < rows, b = r1 < rows;
+        const int64_t ia = r0 * cols + c0, ib = r1 * cols + c0;
+        few_load(c, codes + (ia >> 1), codes + (ib >> 1), live0 && a, live1 && a, live0 && b, live1 && b);
+        s[0] = few_scale<ST>(scales, ia >> block_shift, live0 && a);
+        s[2] = few_scale<ST>(scales, ib >> block_shift, live0 && b);
+        s[1] = HALF ? few_scale<ST>(scales, (ia + 32) >> block_shift, live1 && a) : 0.0f;
+        s[3] = HALF ? few_scale<ST>(scales, (ib + 32) >> block_shift, live1 && b) : 0.0f;
+    };
+    fetch(0, code, m);
+    uint32_t xr[NT][32];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int t = 8 * n + g;
+        few_tokens(xr[n], x + (int64_t)(t < tokens ? t : 0) * ldx + c0, live0 && t < tokens, live1 && t < tokens);
+    }
+    if (tid < 8) s_levels[tid] = make_float2(__ldg(levels + 2 * tid), __ldg(levels + 2 * tid + 1));
+    fill_pairs(s_pairs, levels, tid, FewGeo<NT>::threads);
+    __syncthreads();
+    const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
+    int k = 0, buf = 0;
+    for (int i = 0; i < rounds; ++i) {
+        FewCodes next;
+        float mn[4];
+        fetch(i + 1, next, mn);
+        float acc[NT][4] = {};
+        if (busy) few_multiply<HALF, NT>(code, m, xr, acc, pairs, lane8, s_levels);
+        float* const mine = s_part + ((buf * D + k) * W + warp) * P;  // [16][8 NT]
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            *reinterpret_cast<float2*>(mine + g * 8 * NT + 8 * n + 2 * q) = make_float2(acc[n][0], acc[n][1]);
+            *reinterpret_cast<float2*>(mine + (g + 8) * 8 * NT + 8 * n + 2 * q) = make_float2(acc[n][2], acc[n][3]);
+        }
+        if (k == D - 1 || i + 1 == rounds) {
+            __syncthreads();
+            // the k + 1 row tiles of each group since the last time; rows fastest, so that neighbours write neighbours
+            const int per = work.groups * 16, total = (k + 1) * per * tokens;
+            for (int e = tid; e < total; e += FewGeo<NT>::threads) {
+                const int row = e & 15, rest = e >> 4, gr = rest % work.groups, rest2 = rest / work.groups, t = rest2 % tokens, j = rest2 / tokens;
+                const int64_t tile = (int64_t)peer * work.groups + gr + (int64_t)(i - k + j) * step, r = tile * 16 + row;
+                if (r >= rows) continue;
+                const float* p = s_part + ((buf * D + j) * W + gr * work.stripes) * P + row * 8 * NT + t;
+                float sum = 0.0f;
+                for (int s = 0; s < work.stripes; ++s) sum += p[s * P];
+                if (work.slices > 1)
+                    sums[((int64_t)slice * tokens + t) * rows + r] = sum;
+                else
+                    out.store(sum + (correction ? correction[(int64_t)t * rows + r] : 0.0f), out.bias_at(r), out.residual_at(t, r), t, r);
+            }
+            buf ^= 1;
+            k = 0;
+        } else {
+            ++k;
+        }
+        code = next;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) m[u] = mn[u];
+    }
+    if (work.slices == 1) return;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+        s_last = (int)(atomicAdd(tickets + peer, 1ull) & 255ull) == work.slices - 1;
+        if (s_last) tickets[peer] = 0ull;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    for (int e = tid; e < rounds * work.groups * 16 * tokens; e += FewGeo<NT>::threads) {
+        const int row = e & 15, rest = e >> 4, gr = rest % work.groups, rest2 = rest / work.groups, i = rest2 % rounds, t = rest2 / rounds;
+        const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)i * step) * 16 + row;
+        if (r >= rows) continue;
+        float sum = 0.0f;
+        for (int s = 0; s < work.slices; ++s) sum += __ldcg(sums + ((int64_t)s * tokens + t) * rows + r);
+        out.store(sum + (correction ? correction[(int64_t)t * rows + r] : 0.0f), out.bias_at(r), out.residual_at(t, r), t, r);
+    }
+}
+
+// Outliers: correction[t, r] = sum over the entries of row r of (val - W^) x[t, c], zero elsewhere (set before).  A thread per entry
+// forms its terms, and the one with a row's first entry adds the row's up, in the order of the list; a row that runs past the
+// CTA's 256 entries is finished from global memory.
+constexpr int kFewTokens = 16;
+template <class ST>
+__global__ void __launch_bounds__(256)
+few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
+                      const float* __restrict__ levels, const uint16_t* __restrict__ x, int64_t ldx, int tokens, const int32_t* __restrict__ idx,
+                      const uint16_t* __restrict__ val, const int64_t* __restrict__ n_out, int64_t capacity, float* __restrict__ correction)
+{
+    if (!after_previous()) return;
+    __shared__ float s_term[256][kFewTokens + 1];
+    __shared__ int s_row[256];
+    int64_t k_end = *n_out;
+    if (k_end > capacity) k_end = capacity;
+    const int64_t n = rows * cols;
+    auto row_of = [&](int64_t k) -> int {  // -1 for an index outside the matrix
+        const int64_t i = idx[k];
+        return (i < 0 || i >= n) ? -1 : (int)(i / cols);
+    };
+    auto change_of = [&](int64_t k) -> float {
+        const int64_t i = idx[k];
+        const uint32_t byte = codes[i >> 1], c = (i & 1) ? (byte & 15u) : (byte >> 4);
+        return bf16_value(val[k]) - bf16_value(bf16_round(__fmul_rn(few_scale<ST>(scales, i >> block_shift, true), __ldg(levels + c))));
+    };
+    const int tid = threadIdx.x;
+    for (int64_t base = (int64_t)blockIdx.x * 256; base < k_end; base += (int64_t)gridDim.x * 256) {
+        const int64_t k = base + tid;
+        const int r = k < k_end ? row_of(k) : -1;
+        s_row[tid] = r;
+        if (r >= 0) {
+            const float d = change_of(k);
+            const int64_t c = idx[k] - (int64_t)r * cols;
+            for (int t = 0; t < tokens; ++t) s_term[tid][t] = d * bf16_value(x[t * ldx + c]);
+        }
+        __syncthreads();
+        if (r >= 0 && (tid > 0 ? s_row[tid - 1] : (k > 0 ? row_of(k - 1) : -1)) != r) {  // first outlier of its row
+            int end = tid;
+            while (end < 256 && s_row[end] == r) ++end;
+            for (int t = 0; t < tokens; ++t) {
+                float sum = 0.0f;
+                for (int j = tid; j < end; ++j) sum += s_term[j][t];
+                if (end == 256)
+                    for (int64_t kk = base + 256; kk < k_end && row_of(kk) == r; ++kk) sum += change_of(kk) * bf16_value(x[t * ldx + idx[kk] - (int64_t)r * cols]);
+                correction[(int64_t)t * rows + r] = sum;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+namespace {
+
+struct FewPlan {
+    FewWork work{};
+    int grid = 0;
+    size_t sums = 0, correction = 0, total = 0;  // byte offsets (the tickets are at 0), and the bytes of all
+};
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
+{
+    FewPlan p;
+    const int warps = tokens > 8 ? FewGeo<2>::warps : FewGeo<1>::warps;
+    const int64_t stripes = (cols + kFewStripe - 1) / kFewStripe, tiles = (rows + 15) / 16;
+    const int64_t slices = (stripes + warps - 1) / warps;
+    FewWork& w = p.work;
+    w.slices = (int)slices;
+    w.stripes = (int)((stripes + slices - 1) / slices);
+    w.groups = warps / w.stripes;
+    if (w.groups > tiles) w.groups = (int)tiles;
+    w.tiles = (int)tiles;
+    const int64_t want = (tiles + w.groups - 1) / w.groups, have = kSMs / slices;
+    w.peers = (int)(want < have ? want : have);
+    p.grid = w.peers * w.slices;
+    p.sums = up256((size_t)w.peers * 8);
+    p.correction = p.sums + (slices > 1 ? up256((size_t)slices * tokens * rows * 4) : 0);
+    p.total = p.correction + (list ? up256((size_t)tokens * rows * 4) : 0);
+    return p;
+}
+
+}  // namespace
+
+bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens)
+{
+    return tokens <= kFewTokens && cols <= 32768 && rows <= (1 << 26);
+}
+
+size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity) { return few_plan(rows, cols, tokens, capacity > 0).total; }
+
+int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, const LinearOut& out, int* status, void* ws, size_t ws_bytes, cudaStream_t st)
+{
+    const bool list = w.out_idx && w.capacity > 0;
+    FewPlan p = few_plan(w.rows, w.cols, out.tokens, list);
+    if (ws_bytes < p.total) {
+        set_error("%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes, p.total);
+        return BOF4_ERR_WORKSPACE;
+    }
+    unsigned char* const base = static_cast<unsigned char*>(ws);
+    const uint16_t* const xb = static_cast<const uint16_t*>(x);
+    float* correction = nullptr;
+    if (list) {
+        correction = reinterpret_cast<float*>(base + p.correction);
+        BOF4_CUDA_TRY(cudaMemsetAsync(correction, 0, (size_t)out.tokens * w.rows * 4, st));
+        const int64_t want = (w.capacity + 255) / 256;
+        launch_after(w.scale_dtype == BOF4_F32 ? few_correction_kernel<F32> : few_correction_kernel<BF16>, (int)(want < 4 * kSMs ? want : 4 * kSMs), 256,
+                     0, st, w.codes, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb, ldx, (int)out.tokens, w.out_idx, w.out_val, w.n_out,
+                     w.capacity, correction);
+        BOF4_CUDA_TRY(cudaGetLastError());
+    }
+    p.work.epoch = tc_next_epoch();
+    int rc;
+#define BOF4_FEW_GO(NT_, ST_, HALF_)                                                                                                              \
+    {                                                                                                                                             \
+        constexpr auto kern = linear_few_kernel<NT_, ST_, HALF_>;                                                                                 \
+        if ((rc = ensure_dynamic_smem<kern>(FewGeo<NT_>::smem))) return rc;                                                                       \
+        launch_after(kern, p.grid, FewGeo<NT_>::threads, FewGeo<NT_>::smem, st, w.codes, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
+                     ldx, out, correction, status, p.work, reinterpret_cast<unsigned long long*>(base), reinterpret_cast<float*>(base + p.sums)); \
+    }
+#define BOF4_FEW_S(NT_, ST_) { if (w.block_size == 32) BOF4_FEW_GO(NT_, ST_, true) else BOF4_FEW_GO(NT_, ST_, false) }
+#define BOF4_FEW_N(NT_) { if (w.scale_dtype == BOF4_F32) BOF4_FEW_S(NT_, F32) else BOF4_FEW_S(NT_, BF16) }
+    if (out.tokens > 8) BOF4_FEW_N(2) else BOF4_FEW_N(1)
+#undef BOF4_FEW_N
+#undef BOF4_FEW_S
+#undef BOF4_FEW_GO
+    BOF4_CUDA_TRY(cudaGetLastError());
+    return BOF4_OK;
+}
+
+}  // namespace bof4

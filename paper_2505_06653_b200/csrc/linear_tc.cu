@@ -31,6 +31,7 @@
 //   4 results     read a finished accumulator (there are two) while the next tile runs
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
+#include "decode.cuh"
 #include "linear.cuh"
 #include "tc.cuh"
 
@@ -59,39 +60,6 @@ struct LtWork {
         return (uint32_t)l < longer ? (int)((uint32_t)l / (uint32_t)(each + 1)) : extra + (int)(((uint32_t)l - longer) / (uint32_t)each);
     }
 };
-
-// Eight products by byte permutes.  lo[0..1], hi[0..1]: bytes of entries 0 ... 7, lo[2..3], hi[2..3]: of 8 ... 15.
-__device__ __forceinline__ void lt_lookup8(uint32_t w, const uint32_t (&lo)[4], const uint32_t (&hi)[4], uint32_t* o)
-{
-    // bits 0 ... 2 of each code select within eight entries; bit 3 selects between the two results of a byte
-    uint32_t s = w & 0x77777777u, t = ((w >> 1) & 0x44444444u) | 0x32103210u;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        // result bytes: elements 1, 0, 3, 2 (the even element of a byte is its high nibble)
-        const uint32_t l = __byte_perm(__byte_perm(lo[0], lo[1], s), __byte_perm(lo[2], lo[3], s), t);
-        const uint32_t u = __byte_perm(__byte_perm(hi[0], hi[1], s), __byte_perm(hi[2], hi[3], s), t);
-        o[2 * h] = __byte_perm(l, u, 0x4051);
-        o[2 * h + 1] = __byte_perm(l, u, 0x6273);
-        s >>= 16, t >>= 16;
-    }
-}
-// The 16 products m * level, rounded to bf16, as planes of bytes.
-__device__ __forceinline__ void lt_table(float m, const float2* levels, uint32_t (&lo)[4], uint32_t (&hi)[4])
-{
-    uint32_t p[8];
-#pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-        const float4 l = reinterpret_cast<const float4*>(levels)[k / 2];
-        const float2 a = __fmul2_rn(make_float2(m, m), make_float2(l.x, l.y)), b = __fmul2_rn(make_float2(m, m), make_float2(l.z, l.w));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(a.y), "f"(a.x));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k + 1]) : "f"(b.y), "f"(b.x));
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        lo[k] = __byte_perm(p[2 * k], p[2 * k + 1], 0x6420);
-        hi[k] = __byte_perm(p[2 * k], p[2 * k + 1], 0x7531);
-    }
-}
 
 __device__ __forceinline__ void lt_load16(uint32_t addr, uint32_t (&v)[16])
 {

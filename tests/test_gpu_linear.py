@@ -394,7 +394,8 @@ def test_refusals(bof4):
     bad(bof4.Bof4Error, activation=5)
     bad(bof4.Bof4Error, activation=-1)
     bad(ValueError, out_dtype=7)
-    bad(bof4.Bof4Error, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda"))
+    need = bof4.bof4_linear_workspace_bytes(rows, cols, 2)
+    bad(bof4.Bof4Error, workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
     bad(ValueError, workspace=torch.zeros(1 << 20, dtype=torch.uint8))
     wide = torch.zeros(2, cols + 4, dtype=torch.bfloat16, device="cuda")
     bad(bof4.Bof4Error, x=wide[:, :cols])            # rows 264 bytes apart: not a multiple of 16
