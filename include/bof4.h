@@ -78,6 +78,10 @@ extern "C" {
 #define BOF4_ACT_GELU_TANH 3 /* z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) */
 #define BOF4_ACT_SILU 4      /* z / (1 + exp(-z)) */
 
+/* What bof4_moe makes of a router's logits */
+#define BOF4_SCORE_SOFTMAX 0 /* over all experts */
+#define BOF4_SCORE_SIGMOID 1 /* each by itself   */
+
 #define BOF4_OP_EM 0  /* bof4_em_step, and a bof4_fit_codebook that streams its data */
 #define BOF4_OP_OPQ 1 /* opq_split / bof4_quantize_opq workspace    */
 #define BOF4_OP_EM_BF16 2 /* bof4_fit_codebook over bf16 tensors, any number of iterations */
@@ -432,6 +436,36 @@ BOF4_API int bof4_linear_backward(const uint8_t* d_codes, const void* d_scales, 
 /* Bytes of workspace for the two calls above (backward != 0: for the second).  capacity: that of the outlier list, 0 without
  * one.  Host function, no CUDA call.  0 for invalid or too large shapes. */
 BOF4_API size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, int backward, int64_t capacity);
+
+/*
+ * A whole mixture-of-experts layer for a few tokens, its experts' matrices in 4 bits:
+ *   s[t, e] = sum_c x[t, c] R[e, c];   score = softmax_e(s) or 1 / (1 + exp(-s))
+ *   the top_k experts of token t: the largest s, descending (equal ones: lowest index first);  w[t, j] = scale * score, divided
+ *   by the sum of the token's top_k scores where renormalize != 0
+ *   h = act(G_e x) * (U_e x);   y[t] = sum_j w[t, j] D_e h
+ * with the dequantised weights in bf16 as for bof4_linear and fp32 everywhere else but in h, of which 16 bits enter the product
+ * with D_e (2^-17 relative).  Every sum is taken in an order that depends on the shapes and the choice of experts alone.  Only
+ * the experts that some token chose are read.
+ *   d_x         device, bf16, n_tokens (0 ... 64) rows of `hidden`, token t at t * ldx; 16-byte aligned, ldx a multiple of 8
+ *   d_router    device, [n_experts][hidden] of router_dtype, 16-byte aligned;  n_experts 1 ... 512, top_k 1 ... 16
+ *   d_gate_up_codes / d_gate_up_scales   [n_experts][2 * ffn][hidden], quantised as one flat tensor: an expert's `ffn` rows of
+ *               G, then its rows of U;  d_down_codes / d_down_scales   [n_experts][hidden][ffn].  Codes 32-byte aligned;
+ *               block_size divides hidden and ffn; one codebook for all
+ *   d_y         device, out, y_dtype, token t at t * ldy
+ *   d_ids, d_weights   device, out, [n_tokens][top_k] int32 and fp32: the experts and w
+ *   d_status    device int, written: 0, or 1 when a bounded wait inside the kernel ran out (y is then undefined)
+ *   d_ws        device workspace of bof4_moe_workspace_bytes bytes, 256-byte aligned, any contents; two calls that may run
+ *               at the same time must not share one
+ * One cooperative launch (a CTA on every SM) on `stream`; no host synchronisation.
+ */
+BOF4_API int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t hidden, const void* d_router, int router_dtype, int n_experts,
+                      int top_k, int score, int renormalize, float scale, const uint8_t* d_gate_up_codes, const void* d_gate_up_scales,
+                      const uint8_t* d_down_codes, const void* d_down_scales, int scale_dtype, int64_t ffn, int block_size,
+                      const float* d_codebook, int activation, void* d_y, int y_dtype, int64_t ldy, int32_t* d_ids, float* d_weights,
+                      int* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Bytes of its workspace.  Host function, no CUDA call.  0 for invalid sizes. */
+BOF4_API size_t bof4_moe_workspace_bytes(int64_t n_tokens, int64_t hidden, int64_t ffn, int n_experts, int top_k);
 
 /*
  * Data-free codebook for unit-variance Gaussian weights (Sec. 3.2 Eq. 5 / Eq. 7; App. B.2): `iters`

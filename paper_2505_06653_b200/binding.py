@@ -27,6 +27,7 @@ NORM_ABS, NORM_SIGNED = 0, 1
 METRIC_MSE, METRIC_MAE = 0, 1
 METRIC_MSE_NORMALIZED, METRIC_MAE_NORMALIZED = 2, 3  # App. D: errors of the normalised weights
 OP_EM, OP_OPQ, OP_EM_BF16 = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 LEVELS = 16
 
@@ -57,7 +58,7 @@ EXPORTS = ("bof4_workspace_bytes", "bof4_fit_workspace_bytes", "bof4_em_step", "
            "bof4_default_init", "bof4_last_error", "bof4_theoretical_codebook", "bof4_theoretical_codebook_batch",
            "bof4_gemv", "bof4_outlier_count", "bof4_scales_compress", "bof4_scales_expand",
            "bof4_theoretical_codebook_general", "bof4_quantize_batch", "bof4_dequantize_batch", "bof4_m_step", "bof4_gemm_tc",
-           "bof4_linear", "bof4_linear_backward", "bof4_linear_workspace_bytes")
+           "bof4_linear", "bof4_linear_backward", "bof4_linear_workspace_bytes", "bof4_moe", "bof4_moe_workspace_bytes")
 
 
 class Bof4Error(RuntimeError):
@@ -129,6 +130,11 @@ def lib() -> ctypes.CDLL:
         L.bof4_linear_backward.restype = i32
         L.bof4_linear_backward.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i32, i64, i64, vp, i64, i32, vp, vp, vp, i64, vp, i64,
                                            vp, vp, vp, sz, vp]
+        L.bof4_moe_workspace_bytes.restype = sz
+        L.bof4_moe_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.bof4_moe.restype = i32
+        L.bof4_moe.argtypes = [vp, i64, i64, i64, vp, i32, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, i32, i64, i32, vp, i32,
+                               vp, i32, i64, vp, vp, vp, vp, sz, vp]
         L.bof4_m_step.restype = i32
         L.bof4_m_step.argtypes = [vp, i32, i32, vp, ctypes.c_uint32, vp, vp, vp]
         L.bof4_scales_compress.restype = i32
@@ -495,6 +501,22 @@ def bof4_linear_backward(codes: torch.Tensor, scales: torch.Tensor, rows: int, c
     dbias fp32 [rows] or None, status int32[1])."""
     return _native().linear_backward(codes, scales, rows, cols, block_size, levels, dy, pre, activation, want_dx, want_dbias, outliers,
                                      out, workspace)
+
+
+def bof4_moe_workspace_bytes(n_tokens: int, hidden: int, ffn: int, n_experts: int, top_k: int) -> int:
+    """Bytes of the workspace of bof4_moe, which the call otherwise allocates itself."""
+    return int(lib().bof4_moe_workspace_bytes(n_tokens, hidden, ffn, n_experts, top_k))
+
+
+def bof4_moe(x: torch.Tensor, router: torch.Tensor, gate_up: Tuple[torch.Tensor, torch.Tensor], down: Tuple[torch.Tensor, torch.Tensor],
+             ffn: int, block_size: int, levels, top_k: int, activation: int = ACT_SILU, score: int = SCORE_SOFTMAX,
+             renormalize: bool = True, scale: float = 1.0, out_dtype: int = BF16, out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None):
+    """A mixture-of-experts layer for up to 64 tokens x bf16 [n_tokens, hidden]: router [n_experts, hidden], the experts'
+    matrices as (codes, scales) of flat tensors [n_experts, 2 ffn, hidden] (gate rows, then up rows) and [n_experts, hidden, ffn].
+    -> (y [n_tokens, hidden], ids int32 [n_tokens, top_k], weights fp32 [n_tokens, top_k], status int32[1])."""
+    return _native().moe(x, router, gate_up, down, ffn, block_size, levels, top_k, activation, score, renormalize, scale, out_dtype, out,
+                         workspace)
 
 
 def bof4_outlier_count(n_out: torch.Tensor, capacity: int) -> int:

@@ -1,0 +1,512 @@
+// A whole mixture-of-experts layer for a few tokens, in one launch: router, choice of experts, gated products with the 4-bit
+// matrices of the chosen experts, weighted sum.
+//
+//   s[t, e] = sum_c x[t, c] R[e, c];  p = softmax_e(s) or sigmoid(s);  the top_k experts of a token by s (ties: lowest index)
+//   h = act(G_e x) * (U_e x);  y[t] = sum_j weight[t, j] * D_e(j) h
+//
+// W^ as in bof4_linear: constant * level rounded to bf16.  h is kept as the sum of two bf16 values (16 bits of it reach the
+// product, 2^-17 relative), everything else is fp32.
+//
+// With a few tokens the layer is bound by reading the codes of the experts that were chosen, once.  One cooperative launch of
+// a CTA per SM goes through four phases with a barrier over the grid between them (1.2 us each; a launch of their own would
+// cost more, and would have to build the table of level pairs anew):
+//
+//   router   a warp per expert and four tokens
+//   gate/up  every CTA works the choice out for itself (a warp per token), then lists the chosen experts with their tokens.
+//            Units of eight rows of G with the same eight of U (one 16-row product of decode.cuh, so that a lane holds
+//            both halves of h) are dealt in equal contiguous runs over the row groups of the grid
+//   down     units of 16 rows of D, the two halves of h as separate columns of the product
+//   sum      y[t] over the token's experts, in the order of its list
+//
+// A unit's columns are split over the stripes of a row group (a warp each, 256 columns; several stripes a warp where a row is
+// longer than a CTA has warps for) and its parts are added up in shared memory in a fixed order: no sum depends on scheduling.
+//
+// The waits on the barrier are bounded: a time-out sets the status word and everybody leaves.
+#include <type_traits>
+
+#include "decode.cuh"
+#include "linear.cuh"
+#include "tc.cuh"
+
+namespace bof4 {
+
+constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
+constexpr int kMoeTokens = 64, kMoeExperts = 512, kMoeTop = 16;
+constexpr int kMoePart = 128;      // sums of a warp and unit: 16 rows, 8 columns
+constexpr int kMoeDefer = 4;       // units between two additions over the stripes
+constexpr int kMoeSmem = kPairBytes + 2 * kMoeDefer * kMoeWarps * kMoePart * 4;
+constexpr int kMoeChoices = kMoeTokens * kMoeTop;
+constexpr uint32_t kMoeSpin = 1u << 22;
+
+struct MoeArgs {
+    const uint16_t* x;
+    int64_t ldx, hidden, ffn;
+    int tokens, experts, top, score, act, block_shift;
+    bool renormalize, router_bf16, y_bf16;
+    float scale;
+    const void* router;
+    const uint8_t *codes1, *codes2;  // gate and up [experts][2 ffn][hidden], down [experts][hidden][ffn]
+    const void *scales1, *scales2;
+    const float* levels;
+    void* y;
+    int64_t ldy;
+    int32_t* ids;
+    float* weights;
+    int* status;
+    unsigned long long* cells;  // barriers
+    unsigned long long epoch;
+    float* logits;              // [tokens][experts]
+    uint16_t *h_hi, *h_lo;      // [tokens * top][ffn]
+    float* out;                 // [tokens * top][hidden]
+};
+
+// Order-preserving map of a finite or infinite fp32 value to an unsigned integer (a NaN goes to one end).
+__device__ __forceinline__ uint32_t moe_key(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);  // -0 counts as +0
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+template <class ST, bool HALF>
+__global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const MoeArgs p)
+{
+    extern __shared__ __align__(256) unsigned char s_dyn[];
+    float2* const s_pairs = reinterpret_cast<float2*>(s_dyn);
+    float* const s_part = reinterpret_cast<float*>(s_dyn + kPairBytes);  // [2][kMoeDefer][kMoeWarps][kMoePart]
+    __shared__ __align__(16) float2 s_levels[8];
+    __shared__ uint16_t s_id[kMoeChoices];       // expert of choice t * top + j
+    __shared__ uint16_t s_list[kMoeChoices];     // choices, by expert
+    __shared__ uint16_t s_first[kMoeExperts + 1], s_expert[kMoeExperts];  // of the chosen experts: first place in the list, which
+    __shared__ int s_units[2][kMoeExperts + 1];  // units before a chosen expert, gate/up and down
+    __shared__ int s_warp[2][kMoeWarps + 1];
+    __shared__ int s_chosen, s_fail;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
+    const int grid = (int)gridDim.x;
+    const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
+    if (tid == 0) {
+        s_fail = 0;
+        if (blockIdx.x == 0) *p.status = 0;
+        tc_ticket_open(p.cells + 0, p.epoch), tc_ticket_open(p.cells + 1, p.epoch), tc_ticket_open(p.cells + 2, p.epoch), tc_ticket_open(p.cells + 3, p.epoch);
+    }
+    // All CTAs of the grid meet; false: a time-out.  What they wrote before is visible after.
+    auto meet = [&](int which) -> bool {
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            atomicAdd(p.cells + which, 1ull);
+            const unsigned long long all = p.epoch | (unsigned long long)grid;
+            uint32_t spin = 0;
+            while (*reinterpret_cast<volatile unsigned long long*>(p.cells + which) != all && ++spin < kMoeSpin) __nanosleep(20);
+            if (spin >= kMoeSpin) {
+                s_fail = 1;
+                atomicExch(p.status, 1);
+            }
+        }
+        __syncthreads();
+        __threadfence();
+        return s_fail == 0;
+    };
+
+    // ---- router
+    {
+        const int quads = (p.tokens + 3) / 4;
+        for (int job = (int)blockIdx.x + grid * warp; job < p.experts * quads; job += grid * kMoeWarps) {
+            const int e = job / quads, t0 = (job - e * quads) * 4, n = min(4, p.tokens - t0);
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int64_t c = lane * 8; c < p.hidden; c += 256) {
+                float r[8];
+                if (p.router_bf16) {
+                    const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.router) + e * p.hidden + c));
+                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) r[2 * k] = __uint_as_float(w[k] << 16), r[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                } else {
+                    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p.router) + e * p.hidden + c);
+                    const float4 a = __ldg(f), b = __ldg(f + 1);
+                    r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if (t < n) {
+                        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.x + (t0 + t) * p.ldx + c));
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            sum[t] = fmaf(r[2 * k], __uint_as_float(w[k] << 16), sum[t]);
+                            sum[t] = fmaf(r[2 * k + 1], __uint_as_float(w[k] & 0xffff0000u), sum[t]);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int o = 16; o >= 1; o >>= 1) sum[t] += __shfl_xor_sync(kFull, sum[t], o);
+                if (lane == 0 && t < n) p.logits[(t0 + t) * p.experts + e] = sum[t];
+            }
+        }
+    }
+    if (tid < 8) s_levels[tid] = make_float2(__ldg(p.levels + 2 * tid), __ldg(p.levels + 2 * tid + 1));
+    fill_pairs(s_pairs, p.levels, tid, kMoeThreads);
+    if (!meet(0)) return;
+
+    // ---- the choice, by every CTA for itself
+    for (int t = warp; t < p.tokens; t += kMoeWarps) {
+        constexpr int R = kMoeExperts / 32;
+        float s[R];
+        uint32_t free = 0u;  // experts of this lane that have not been taken
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int e = k * 32 + lane;
+            s[k] = e < p.experts ? __ldcg(p.logits + t * p.experts + e) : 0.0f;
+            if (e < p.experts) free |= 1u << k, most = fmaxf(most, s[k]);
+        }
+        float total = 0.0f;
+        if (p.score == BOF4_SCORE_SOFTMAX) {
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (k * 32 + lane < p.experts) total += expf(s[k] - most);
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
+        }
+        float mine = 0.0f, chosen_sum = 0.0f;  // lane j: the score of choice j
+        for (int j = 0; j < p.top; ++j) {
+            // the largest remaining logit, then the lowest index
+            unsigned long long best = 0ull;
+            float value = 0.0f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const unsigned long long key = (unsigned long long)moe_key(s[k]) << 32 | (0xffffffffu - (uint32_t)(k * 32 + lane));
+                if ((free >> k & 1u) && key > best) best = key, value = s[k];
+            }
+            unsigned long long top = best;
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) {
+                const unsigned long long other = __shfl_xor_sync(kFull, top, o);
+                if (other > top) top = other;
+            }
+            const int e = (int)(0xffffffffu - (uint32_t)top);
+            value = __shfl_sync(kFull, value, e & 31);
+            if ((e & 31) == lane) free &= ~(1u << (e >> 5));
+            const float score = p.score == BOF4_SCORE_SOFTMAX ? expf(value - most) / total : 1.0f / (1.0f + expf(-value));
+            chosen_sum += score;
+            if (lane == j) mine = score, s_id[t * p.top + j] = (uint16_t)e;
+        }
+        if (p.renormalize) mine /= chosen_sum;
+        if (blockIdx.x == 0 && lane < p.top) {
+            p.ids[t * p.top + lane] = s_id[t * p.top + lane];
+            p.weights[t * p.top + lane] = mine * p.scale;
+        }
+    }
+    __syncthreads();
+    // ---- the chosen experts in ascending order, their choices, and the units before each
+    const int choices = p.tokens * p.top;
+    const int tiles1 = (int)(p.ffn / 8), tiles2 = (int)((p.hidden + 15) / 16);
+    {
+        int count = 0;
+        if (tid < p.experts)
+            for (int a = 0; a < choices; ++a) count += s_id[a] == tid;
+        // running numbers over the threads: choices, and chosen experts
+        int before = count, which = count > 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int b = __shfl_up_sync(kFull, before, o), w = __shfl_up_sync(kFull, which, o);
+            if (lane >= o) before += b, which += w;
+        }
+        if (lane == 31) s_warp[0][warp] = before, s_warp[1][warp] = which;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) before += s_warp[0][w], which += s_warp[1][w];
+        if (count > 0) {
+            const int at = before - count, i = which - 1;
+            s_expert[i] = (uint16_t)tid;
+            s_first[i] = (uint16_t)at;
+            int k = at;
+            for (int a = 0; a < choices; ++a)
+                if (s_id[a] == tid) s_list[k++] = (uint16_t)a;
+            // passes of eight tokens (gate/up) and of four (down)
+            s_units[0][i] = (count + 7) / 8 * tiles1;
+            s_units[1][i] = (count + 3) / 4 * tiles2;
+        }
+        if (tid == kMoeThreads - 1) s_chosen = which, s_first[which] = (uint16_t)choices;
+    }
+    __syncthreads();
+    const int chosen = s_chosen;
+    if (warp < 2) {  // exclusive sums over the chosen experts, by a warp each
+        int carry = 0;
+        for (int i0 = 0; i0 < chosen; i0 += 32) {
+            const int i = i0 + lane, v = i < chosen ? s_units[warp][i] : 0;
+            int sum = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int b = __shfl_up_sync(kFull, sum, o);
+                if (lane >= o) sum += b;
+            }
+            if (i < chosen) s_units[warp][i] = carry + sum - v;
+            carry += __shfl_sync(kFull, sum, 31);
+        }
+        if (lane == 0) s_units[warp][chosen] = carry;
+    }
+    __syncthreads();
+
+    // ---- gate/up and down: the same walk over units
+    auto walk = [&](auto second_c) {
+        constexpr bool SECOND = decltype(second_c)::value;
+        constexpr int PASS = SECOND ? 4 : 8;
+        const int* const units = s_units[SECOND ? 1 : 0];
+        const int64_t cols = SECOND ? p.ffn : p.hidden;
+        const int tiles = SECOND ? tiles2 : tiles1;
+        const uint8_t* const codes = SECOND ? p.codes2 : p.codes1;
+        const void* const scales = SECOND ? p.scales2 : p.scales1;
+        const int stripes = (int)((cols + kFewStripe - 1) / kFewStripe), rounds = (stripes + kMoeWarps - 1) / kMoeWarps;
+        const int wide = (stripes + rounds - 1) / rounds, groups = kMoeWarps / wide;  // stripes side by side, row groups of the CTA
+        const int group = warp / wide, stripe = warp - group * wide;
+        const bool busy = group < groups;
+        const int total = units[chosen], all = grid * groups, each = total / all, extra = total % all;
+        auto start_of = [&](int k) { return k * each + min(k, extra); };  // first unit of row group k of the grid
+        const int group0 = (int)blockIdx.x * groups, steps = each + (group0 < extra);  // the CTA's first group has the most
+        const int begin = busy ? start_of(group0 + group) : 0, finish = busy ? start_of(group0 + group + 1) : 0;
+        // where a unit lies: chosen expert, pass, tile
+        auto place = [&](int u, int& i, int& pass, int& tile) {
+            while (u >= units[i + 1]) ++i;
+            const int in = u - units[i];
+            pass = in / tiles, tile = in - pass * tiles;
+        };
+        auto fetch = [&](int u, int i0, int round, FewCodes& c, float (&m)[4]) {
+            const bool ok = u < finish;
+            int i = i0, pass = 0, tile = 0;
+            if (ok) place(u, i, pass, tile);
+            const int64_t e = s_expert[ok ? i : 0], c0 = (int64_t)(round * wide + stripe) * kFewStripe + 64 * q;
+            const int64_t r0 = SECOND ? e * p.hidden + tile * 16 + g : e * 2 * p.ffn + tile * 8 + g, r1 = SECOND ? r0 + 8 : r0 + p.ffn;
+            const bool a = ok && (!SECOND || tile * 16 + g < p.hidden), b = ok && (!SECOND || tile * 16 + 8 + g < p.hidden);
+            const bool l0 = c0 < cols, l1 = c0 + 32 < cols;
+            const int64_t ia = r0 * cols + c0, ib = r1 * cols + c0;
+            few_load(c, codes + (ia >> 1), codes + (ib >> 1), l0 && a, l1 && a, l0 && b, l1 && b);
+            m[0] = few_scale<ST>(scales, ia >> p.block_shift, l0 && a);
+            m[2] = few_scale<ST>(scales, ib >> p.block_shift, l0 && b);
+            m[1] = HALF ? few_scale<ST>(scales, (ia + 32) >> p.block_shift, l1 && a) : 0.0f;
+            m[3] = HALF ? few_scale<ST>(scales, (ib + 32) >> p.block_shift, l1 && b) : 0.0f;
+        };
+        int at = 0, k = 0, buf = 0;         // chosen expert of the current unit; units since the last addition
+        int have_i = -1, have_pass = -1;    // whose tokens xr holds
+        uint32_t xr[1][32];
+        FewCodes code;
+        float m[4];
+        fetch(begin, 0, 0, code, m);
+        for (int s = 0; s < steps; ++s) {
+            const int u = begin + s;
+            float acc[1][4] = {};
+            for (int round = 0; round < rounds; ++round) {
+                FewCodes next;
+                float mn[4];
+                const bool more = round + 1 < rounds;
+                fetch(more ? u : u + 1, at, more ? round + 1 : 0, next, mn);
+                if (u < finish) {
+                    int pass, tile;
+                    place(u, at, pass, tile);
+                    if (rounds > 1 || at != have_i || pass != have_pass) {
+                        have_i = at, have_pass = pass;
+                        const int64_t c0 = (int64_t)(round * wide + stripe) * kFewStripe + 64 * q;
+                        const int n = s_first[at + 1] - s_first[at] - pass * PASS, col = SECOND ? g & 3 : g;
+                        const bool live = col < n;
+                        const int a = live ? s_list[s_first[at] + pass * PASS + col] : 0;
+                        const uint16_t* src = SECOND ? (g < 4 ? p.h_hi : p.h_lo) + (int64_t)a * p.ffn : p.x + (int64_t)(a / p.top) * p.ldx;
+                        few_tokens(xr[0], src + c0, live && c0 < cols, live && c0 + 32 < cols);
+                    }
+                    few_multiply<HALF, 1>(code, m, xr, acc, pairs, lane8, s_levels);
+                }
+                code = next;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) m[v] = mn[v];
+            }
+            float* const mine = s_part + ((buf * kMoeDefer + k) * kMoeWarps + warp) * kMoePart;  // [16][8]
+            *reinterpret_cast<float2*>(mine + g * 8 + 2 * q) = make_float2(acc[0][0], acc[0][1]);
+            *reinterpret_cast<float2*>(mine + (g + 8) * 8 + 2 * q) = make_float2(acc[0][2], acc[0][3]);
+            if (k == kMoeDefer - 1 || s + 1 == steps) {
+                __syncthreads();
+                // results of k + 1 units of each group: gate/up 8 rows x 8 tokens, down 16 rows x 4 tokens, rows fastest
+                for (int e = tid; e < (k + 1) * groups * 64; e += kMoeThreads) {
+                    const int row = SECOND ? e & 15 : e & 7, col = SECOND ? (e >> 4) & 3 : (e >> 3) & 7, rest = e >> 6, gr = rest % groups, j = rest / groups;
+                    const int v = start_of(group0 + gr) + s - k + j;
+                    if (v >= start_of(group0 + gr + 1)) continue;
+                    int i = 0, pass, tile;
+                    place(v, i, pass, tile);
+                    if (col >= s_first[i + 1] - s_first[i] - pass * PASS) continue;
+                    const int64_t a = s_list[s_first[i] + pass * PASS + col];
+                    const float* part = s_part + ((buf * kMoeDefer + j) * kMoeWarps + gr * wide) * kMoePart;
+                    float v0 = 0.0f, v1 = 0.0f;
+                    const int i0 = row * 8 + col, i1 = SECOND ? i0 + 4 : i0 + 64;
+                    for (int w = 0; w < wide; ++w) v0 += part[w * kMoePart + i0], v1 += part[w * kMoePart + i1];
+                    if (SECOND) {
+                        const int64_t o = tile * 16 + row;
+                        if (o < p.hidden) p.out[a * p.hidden + o] = v0 + v1;
+                    } else {
+                        const float h = activate(v0, p.act) * v1;
+                        const uint16_t hi = bf16_round(h);
+                        const int64_t o = a * p.ffn + tile * 8 + row;
+                        p.h_hi[o] = hi;
+                        p.h_lo[o] = bf16_round(isfinite(h) ? h - bf16_value(hi) : 0.0f);
+                    }
+                }
+                buf ^= 1;
+                k = 0;
+            } else {
+                ++k;
+            }
+        }
+    };
+    walk(std::false_type{});
+    if (!meet(1)) return;
+    walk(std::true_type{});
+    if (!meet(2)) return;
+
+    // ---- the weighted sums
+    for (int64_t i = (int64_t)blockIdx.x * kMoeThreads + tid; i < p.tokens * p.hidden; i += (int64_t)grid * kMoeThreads) {
+        const int64_t t = i / p.hidden, o = i - t * p.hidden;
+        float sum = 0.0f;
+        for (int j = 0; j < p.top; ++j) sum = fmaf(__ldcg(p.weights + t * p.top + j), __ldcg(p.out + (t * p.top + j) * p.hidden + o), sum);
+        if (p.y_bf16) static_cast<uint16_t*>(p.y)[t * p.ldy + o] = bf16_round(sum);
+        else static_cast<float*>(p.y)[t * p.ldy + o] = sum;
+    }
+    // the last to leave clears the barriers: a replayed launch has the same epoch
+    if (tid == 0 && (int)(atomicAdd(p.cells + 3, 1ull) & 255ull) == grid - 1) p.cells[0] = p.cells[1] = p.cells[2] = p.cells[3] = 0ull;
+}
+
+namespace {
+
+struct MoePlan {
+    size_t logits, hi, lo, out, total;  // byte offsets (the barriers are at 0), and the bytes of all
+};
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+MoePlan moe_plan(int64_t tokens, int64_t hidden, int64_t ffn, int64_t experts, int64_t top)
+{
+    MoePlan p;
+    p.logits = 256;
+    p.hi = p.logits + up256((size_t)(tokens * experts * 4));
+    p.lo = p.hi + up256((size_t)(tokens * top * ffn * 2));
+    p.out = p.lo + up256((size_t)(tokens * top * ffn * 2));
+    p.total = p.out + up256((size_t)(tokens * top * hidden * 4));
+    return p;
+}
+bool moe_sizes(int64_t tokens, int64_t hidden, int64_t ffn, int64_t experts, int64_t top)
+{
+    return tokens >= 0 && tokens <= kMoeTokens && experts >= 1 && experts <= kMoeExperts && top >= 1 && top <= kMoeTop && top <= experts && hidden >= 32 &&
+           hidden <= (1 << 20) && ffn >= 32 && ffn <= (1 << 20) && hidden % 32 == 0 && ffn % 32 == 0;
+}
+
+}  // namespace
+}  // namespace bof4
+
+using namespace bof4;
+
+extern "C" size_t bof4_moe_workspace_bytes(int64_t n_tokens, int64_t hidden, int64_t ffn, int n_experts, int top_k)
+{
+    return moe_sizes(n_tokens, hidden, ffn, n_experts, top_k) ? moe_plan(n_tokens, hidden, ffn, n_experts, top_k).total : 0;
+}
+
+extern "C" int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t hidden, const void* d_router, int router_dtype, int n_experts,
+                        int top_k, int score, int renormalize, float scale, const uint8_t* d_gate_up_codes, const void* d_gate_up_scales,
+                        const uint8_t* d_down_codes, const void* d_down_scales, int scale_dtype, int64_t ffn, int block_size,
+                        const float* d_codebook, int activation, void* d_y, int y_dtype, int64_t ldy, int32_t* d_ids, float* d_weights,
+                        int* d_status, void* d_ws, size_t ws_bytes, void* stream)
+{
+    const char* fn = "bof4_moe";
+    if (!moe_sizes(n_tokens, hidden, ffn, n_experts, top_k) || !valid_block_size(block_size) || hidden % block_size || ffn % block_size) {
+        set_error("%s: 0 ... 64 tokens, 1 ... 512 experts, top_k 1 ... 16 and at most n_experts, block_size a power of two in 32 ... 4096 that "
+                  "divides hidden and ffn (at most 2^20)", fn);
+        return BOF4_ERR_SHAPE;
+    }
+    if ((scale_dtype != BOF4_F32 && scale_dtype != BOF4_BF16) || (router_dtype != BOF4_F32 && router_dtype != BOF4_BF16) ||
+        (y_dtype != BOF4_F32 && y_dtype != BOF4_BF16)) {
+        set_error("%s: unknown dtype", fn);
+        return BOF4_ERR_DTYPE;
+    }
+    if (activation < BOF4_ACT_NONE || activation > BOF4_ACT_SILU || (score != BOF4_SCORE_SOFTMAX && score != BOF4_SCORE_SIGMOID)) {
+        set_error("%s: unknown activation or score", fn);
+        return BOF4_ERR_INVALID_ARG;
+    }
+    if (n_tokens > 1 && (ldx < hidden || ldy < hidden)) {
+        set_error("%s: a row stride is smaller than its row", fn);
+        return BOF4_ERR_SHAPE;
+    }
+    if (n_tokens <= 1) ldx = ldy = hidden;
+    if (!d_status || (n_tokens > 0 && (!d_x || !d_router || !d_gate_up_codes || !d_gate_up_scales || !d_down_codes || !d_down_scales || !d_codebook ||
+                                       !d_y || !d_ids || !d_weights))) {
+        set_error("%s: NULL pointer", fn);
+        return BOF4_ERR_INVALID_ARG;
+    }
+    auto odd = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
+    if (n_tokens > 0 && (odd(d_gate_up_codes, 32) || odd(d_down_codes, 32) || odd(d_x, 16) || odd(d_router, 16) || ldx % 8)) {
+        set_error("%s: codes must be 32-byte aligned, d_x and d_router 16-byte aligned and ldx a multiple of 8", fn);
+        return BOF4_ERR_INVALID_ARG;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (n_tokens == 0) {
+        BOF4_CUDA_TRY(cudaMemsetAsync(d_status, 0, sizeof(int), st));
+        return BOF4_OK;
+    }
+    const MoePlan plan = moe_plan(n_tokens, hidden, ffn, n_experts, top_k);
+    if (!d_ws || odd(d_ws, 256) || ws_bytes < plan.total) {
+        set_error("%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, plan.total);
+        return BOF4_ERR_WORKSPACE;
+    }
+    unsigned char* const base = static_cast<unsigned char*>(d_ws);
+    MoeArgs a{};
+    a.x = static_cast<const uint16_t*>(d_x);
+    a.ldx = ldx;
+    a.hidden = hidden;
+    a.ffn = ffn;
+    a.tokens = (int)n_tokens;
+    a.experts = n_experts;
+    a.top = top_k;
+    a.score = score;
+    a.act = activation;
+    while ((1 << a.block_shift) < block_size) ++a.block_shift;
+    a.renormalize = renormalize != 0;
+    a.router_bf16 = router_dtype == BOF4_BF16;
+    a.y_bf16 = y_dtype == BOF4_BF16;
+    a.scale = scale;
+    a.router = d_router;
+    a.codes1 = d_gate_up_codes;
+    a.codes2 = d_down_codes;
+    a.scales1 = d_gate_up_scales;
+    a.scales2 = d_down_scales;
+    a.levels = d_codebook;
+    a.y = d_y;
+    a.ldy = ldy;
+    a.ids = d_ids;
+    a.weights = d_weights;
+    a.status = d_status;
+    a.cells = reinterpret_cast<unsigned long long*>(base);
+    a.epoch = tc_next_epoch();
+    a.logits = reinterpret_cast<float*>(base + plan.logits);
+    a.h_hi = reinterpret_cast<uint16_t*>(base + plan.hi);
+    a.h_lo = reinterpret_cast<uint16_t*>(base + plan.lo);
+    a.out = reinterpret_cast<float*>(base + plan.out);
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeCooperative;  // all CTAs are resident at once: they meet at barriers
+    attr.val.cooperative = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(kSMs);
+    cfg.blockDim = dim3(kMoeThreads);
+    cfg.dynamicSmemBytes = kMoeSmem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int rc;
+#define BOF4_MOE_GO(ST_, HALF_)                                                  \
+    {                                                                            \
+        constexpr auto kern = moe_kernel<ST_, HALF_>;                            \
+        if ((rc = ensure_dynamic_smem<kern>(kMoeSmem))) return rc;               \
+        BOF4_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, static_cast<MoeArgs>(a)));  \
+    }
+    if (scale_dtype == BOF4_F32) {
+        if (block_size == 32) BOF4_MOE_GO(F32, true) else BOF4_MOE_GO(F32, false)
+    } else {
+        if (block_size == 32) BOF4_MOE_GO(BF16, true) else BOF4_MOE_GO(BF16, false)
+    }
+#undef BOF4_MOE_GO
+    return BOF4_OK;
+}

@@ -542,6 +542,56 @@ PyObject* linear_backward(PyObject* const* a)
     return PyTuple_Pack(3, rdx.p, rdb.p, rs.p);
 }
 
+// (x, router, gate_up, down, ffn, block_size, levels, top_k, activation, score, renormalize, scale, out_dtype, out, workspace)
+PyObject* moe(PyObject* const* a)
+{
+    const at::Tensor router = dev(a[1], "router");
+    const at::Device d = router.device();
+    if (router.dim() != 2 || tensor(a[0], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, hidden] and router [n_experts, hidden]");
+    const int64_t experts = router.size(0), hidden = router.size(1), n = tensor(a[0], "x").size(0), ffn = integer(a[4]), block = integer(a[5]);
+    const Rows x(a[0], "x", n, hidden, at::kBFloat16, d);
+    if (ffn < 1 || ffn > (1 << 20) || hidden > (1 << 20) || experts > 512) fail(PyExc_ValueError, "at most 512 experts, hidden and ffn of at most 2^20");
+    at::Tensor m[4];  // codes and constants of gate/up and down
+    for (int k = 0; k < 2; ++k) {
+        Ref pair(items(a[2 + k], "gate_up and down must be (codes, scales)"));
+        if (PyTuple_GET_SIZE(pair.p) != 2) fail(PyExc_ValueError, "gate_up and down must be (codes, scales)");
+        m[2 * k] = dev(PyTuple_GET_ITEM(pair.p, 0), "codes");
+        m[2 * k + 1] = dev(PyTuple_GET_ITEM(pair.p, 1), "scales");
+        check_matrix(m[2 * k], m[2 * k + 1], experts * (k ? hidden : 2 * ffn), k ? ffn : hidden, block);
+        if (m[2 * k].device() != d) fail(PyExc_ValueError, "all tensors must be on one device");
+    }
+    const int sd = dtype_code(m[1]), od = (int)integer(a[12]), rd = dtype_code(router);
+    if (dtype_code(m[3]) != sd) fail(PyExc_TypeError, "the constants of gate_up and down must share a dtype");
+    if (od != BOF4_F32 && od != BOF4_BF16) fail(PyExc_ValueError, "out_dtype must be F32 or BF16");
+    const int64_t top = integer(a[7]);
+    if (top < 1 || top > 16) fail(PyExc_ValueError, "top_k must be 1 ... 16");
+    const int act = (int)integer(a[8]), score = (int)integer(a[9]), renorm = PyObject_IsTrue(a[10]) == 1;
+    const float scale = (float)real(a[11]);
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[6], d);
+    std::optional<Rows> out;
+    if (!none(a[13])) out.emplace(a[13], "out", n, hidden, torch_dtype(od), d);
+    at::Tensor made[5], ws;
+    Spec spec[5] = {{1, at::kInt}, {n * top, at::kInt}, {n * top, at::kFloat}};
+    size_t k = 3;
+    const size_t i_ws = k;
+    if (none(a[14])) spec[k++] = {(int64_t)bof4_moe_workspace_bytes(n, hidden, ffn, (int)experts, (int)top), at::kByte};
+    else ws = given_workspace(a[14], d);
+    const size_t i_y = k;
+    if (!out) spec[k++] = {n * hidden, torch_dtype(od)};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        return bof4_moe(x.ptr(), x.ld, n, hidden, router.const_data_ptr(), rd, (int)experts, (int)top, score, renorm, scale,
+                        static_cast<const uint8_t*>(m[0].const_data_ptr()), m[1].const_data_ptr(), static_cast<const uint8_t*>(m[2].const_data_ptr()),
+                        m[3].const_data_ptr(), sd, ffn, (int)block, levels_ptr(cb), act, out ? out->ptr() : made[i_y].data_ptr(), od,
+                        out ? out->ld : hidden, static_cast<int32_t*>(made[1].data_ptr()), static_cast<float*>(made[2].data_ptr()),
+                        static_cast<int*>(made[0].data_ptr()), w.data_ptr(), (size_t)w.numel(), stream_of(d));
+    });
+    Ref rs(wrap(made[0])), ri(wrap(made[1].view({n, top}))), rw(wrap(made[2].view({n, top})));
+    Ref ry(out ? Py_NewRef(a[13]) : wrap(made[i_y].view({n, hidden})));
+    return PyTuple_Pack(4, ry.p, ri.p, rw.p, rs.p);
+}
+
 // (w, block_size, norm, levels, tau, capacity, scale_dtype, workspace, out)
 PyObject* quantize_opq(PyObject* const* a)
 {
@@ -794,7 +844,7 @@ PyMethodDef g_methods[] = {
     BOF4_ENTRY(set_hooks, 2), BOF4_ENTRY(set_allocator, 1), BOF4_ENTRY(quantize, 6), BOF4_ENTRY(dequantize, 8),
     BOF4_ENTRY(gemv, 9), BOF4_ENTRY(gemm_tc, 10), BOF4_ENTRY(quantize_opq, 9), BOF4_ENTRY(outlier_count, 2),
     BOF4_ENTRY(quantize_batch, 6), BOF4_ENTRY(dequantize_batch, 7), BOF4_ENTRY(scales_compress, 2), BOF4_ENTRY(scales_expand, 3),
-    BOF4_ENTRY(fit_codebook, 10), BOF4_ENTRY(linear, 15), BOF4_ENTRY(linear_backward, 14), {nullptr, nullptr, 0, nullptr}};
+    BOF4_ENTRY(fit_codebook, 10), BOF4_ENTRY(linear, 15), BOF4_ENTRY(moe, 15), BOF4_ENTRY(linear_backward, 14), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bof4_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
