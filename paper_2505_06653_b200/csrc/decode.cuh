@@ -2,7 +2,7 @@
 // different units of an SM, and the warp-wide product of sixteen rows with a few tokens that is built on them.
 #pragma once
 
-#include "common.cuh"
+#include "tc.cuh"
 
 namespace bof4 {
 
@@ -55,14 +55,23 @@ __device__ __forceinline__ void lt_table(float m, const float2* levels, uint32_t
 
 constexpr int kPairBytes = 256 * 32 * 8;
 
-// Fills the table of level pairs; all threads of the CTA (whole warps) take part.
+// Fills the table of level pairs; all warps of the CTA take part.  A row of the table is the same pair 32 times: a warp
+// writes rows in turn, the levels in its registers.
 __device__ __forceinline__ void fill_pairs(float2* pairs, const float* __restrict__ levels, int tid, int threads)
 {
-    const float mine = __ldg(levels + (tid & 15));  // level l sits in the lanes with (lane & 15) == l
-#pragma unroll 4
-    for (int e = tid; e < 256 * 32; e += threads) {
-        const int byte = e >> 5;
-        pairs[e] = make_float2(__shfl_sync(kFull, mine, byte >> 4), __shfl_sync(kFull, mine, byte & 15));
+    float lv[16];
+#pragma unroll
+    for (int l = 0; l < 16; l += 4) {
+        const float4 v = make_float4(__ldg(levels + l), __ldg(levels + l + 1), __ldg(levels + l + 2), __ldg(levels + l + 3));
+        lv[l] = v.x, lv[l + 1] = v.y, lv[l + 2] = v.z, lv[l + 3] = v.w;
+    }
+    for (int hi = tid >> 5; hi < 16; hi += threads >> 5) {
+        float h = lv[15];
+#pragma unroll
+        for (int l = 14; l >= 0; --l) h = hi == l ? lv[l] : h;
+        float2* const row = pairs + hi * (16 * 32) + (tid & 31);
+#pragma unroll
+        for (int l = 0; l < 16; ++l) row[l * 32] = make_float2(h, lv[l]);
     }
 }
 
@@ -75,41 +84,55 @@ __device__ __forceinline__ void fill_pairs(float2* pairs, const float* __restric
 // words give the row's part of A for two instructions each, one block constant per row (two for blocks of 32), and of B the
 // 64 values of token g, which stay in 32 registers for as many rows as the warp visits.
 //
-// Decoding is what an SM has to do most here: HBM delivers 43 codes per clock and SM.  Row g goes through the table in
-// shared memory (4 bytes of its data path per code: 32 codes per clock at most), row 8 + g through byte permutes (2.8 instructions
-// of the integer pipe per code: 23 per clock); together they could take 39.
+// Decoding is what an SM has to do most here: HBM delivers 43 codes per clock and SM.  The table in shared memory takes 4
+// bytes of its data path per code (32 codes per clock at most) and one instruction of the integer pipe, byte permutes take 2.9 of
+// that pipe (22 per clock).  Three quarters of the codes go through the table, the last 32 columns of row 8 + g
+// through permutes: 42 per clock for the one, 40 for the other.
 
 constexpr int kFewStripe = 256;
 
 struct FewCodes {
     uint4 v[4];  // row g: 64 codes, row 8 + g: 64 codes
 };
-// a, b: the lane's first byte in rows g and 8 + g; live0, live1: the lane's first and last 32 columns exist (and the row does)
-__device__ __forceinline__ void few_load(FewCodes& c, const uint8_t* a, const uint8_t* b, bool a0, bool a1, bool b0, bool b1)
+// Codes travel to shared memory by TMA, kFewAhead units ahead, into a ring that the warp owns: one lane requests a unit (16 rows of 128
+// bytes, in the 128-byte swizzle, zeros outside the matrix), and every lane reads the 32 bytes of its columns from rows g and
+// 8 + g without meeting a bank twice.  Loads and addresses of the lanes' own took 40 % of the instructions of a unit.
+constexpr int kFewUnit = 2048, kFewAhead = 2, kFewSlots = kFewAhead + 1;
+__device__ __forceinline__ void few_read(FewCodes& c, uint32_t slot, int lane)
 {
-    const uint8_t* p[4] = {a, a + 16, b, b + 16};
-    const bool live[4] = {a0, a1, b0, b1};
+    const uint32_t g = (uint32_t)lane >> 2, q = (uint32_t)lane & 3u;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        c.v[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (live[k])
-            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(c.v[k].x), "=r"(c.v[k].y), "=r"(c.v[k].z), "=r"(c.v[k].w)
-                         : "l"(p[k]));
+    for (int k = 0; k < 4; ++k)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(c.v[k].x), "=r"(c.v[k].y), "=r"(c.v[k].z), "=r"(c.v[k].w)
+                     : "r"(slot + (g + 8u * (k >> 1)) * 128u + ((2u * q + (k & 1u)) ^ g) * 16u)
+                     : "memory");
+}
+// The lane's block constants of a unit as they are in memory, widened where they are used so that nothing waits for the loads
+// before: row g in [0] (with HALF its first 32 columns in [0], its last in [1]), row 8 + g in [2], [3].  a, b: the constants of
+// the lane's first weights in the two rows; live: bits 0, 1: row g and the lane's first and last 32 columns exist, 2, 3: row 8 + g.
+template <class ST, bool HALF>
+struct FewConst {
+    uint32_t v[4];
+    __device__ __forceinline__ void load(const void* scales, int64_t a, int64_t b, uint32_t live)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; k += HALF ? 1 : 2) {
+            const int64_t i = (k < 2 ? a : b) + (k & 1);
+            v[k] = 0u;
+            if (live >> k & 1u) {
+                if (ST::code == BOF4_F32) {
+                    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v[k]) : "l"(static_cast<const uint32_t*>(scales) + i));
+                } else {
+                    uint16_t h;
+                    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(h) : "l"(static_cast<const uint16_t*>(scales) + i));
+                    v[k] = h;
+                }
+            }
+        }
     }
-}
-template <class ST>
-__device__ __forceinline__ float few_scale(const void* scales, int64_t b, bool live);
-template <>
-__device__ __forceinline__ float few_scale<F32>(const void* scales, int64_t b, bool live)
-{
-    return live ? __ldg(static_cast<const float*>(scales) + b) : 0.0f;
-}
-template <>
-__device__ __forceinline__ float few_scale<BF16>(const void* scales, int64_t b, bool live)
-{
-    return live ? __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(scales) + b) << 16) : 0.0f;
-}
+    __device__ __forceinline__ float value(int k) const { return __uint_as_float(ST::code == BOF4_F32 ? v[k] : v[k] << 16); }
+};
 // The 64 values of a token from the lane's first column, as 32 pairs.
 __device__ __forceinline__ void few_tokens(uint32_t (&x)[32], const uint16_t* p, bool live0, bool live1)
 {
@@ -125,29 +148,37 @@ __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1,
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// acc[n]: rows g (0, 1) and 8 + g (2, 3), tokens 8 n + 2 q and 8 n + 2 q + 1.  m: constants of row g, of row 8 + g; with
-// HALF those of their first 32 columns in m[0], m[2] and of the last 32 in m[1], m[3].
-template <bool HALF, int NT>
-__device__ __forceinline__ void few_multiply(const FewCodes& c, const float (&m)[4], const uint32_t (&x)[NT][32], float (&acc)[NT][4],
+// acc[n]: rows g (0, 1) and 8 + g (2, 3), tokens 8 n + 2 q and 8 n + 2 q + 1.
+template <class ST, bool HALF, int NT>
+__device__ __forceinline__ void few_multiply(const FewCodes& c, const FewConst<ST, HALF>& raw, const uint32_t (&x)[NT][32], float (&acc)[NT][4],
                                              uint32_t pairs, uint32_t lane8, const float2* levels)
 {
+    const float m[4] = {raw.value(0), HALF ? raw.value(1) : 0.0f, raw.value(2), HALF ? raw.value(3) : 0.0f};
     uint32_t lo[4], hi[4];
-    lt_table(m[2], levels, lo, hi);
+    lt_table(HALF ? m[3] : m[2], levels, lo, hi);
+    float more[NT][4] = {};  // a second chain of sums
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (HALF && j == 4) lt_table(m[3], levels, lo, hi);
+    for (int i = 0; i < 8; ++i) {
+        // words of the first and of the last 32 columns in turn: table and permutes next to one another
+        const int j = (i & 1) * 4 + (i >> 1);
         const uint4 va = c.v[j >> 2], vb = c.v[2 + (j >> 2)];
         const uint32_t wa = (j & 3) == 0 ? va.x : (j & 3) == 1 ? va.y : (j & 3) == 2 ? va.z : va.w;
         const uint32_t wb = (j & 3) == 0 ? vb.x : (j & 3) == 1 ? vb.y : (j & 3) == 2 ? vb.z : vb.w;
         const float ma = HALF && j >= 4 ? m[1] : m[0];
         uint32_t a[4], b[4];
         tc_lookup8(wa, make_float2(ma, ma), pairs, lane8, a);
-        lt_lookup8(wb, lo, hi, b);
+        if (j < 4) tc_lookup8(wb, make_float2(m[2], m[2]), pairs, lane8, b);
+        else lt_lookup8(wb, lo, hi, b);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) few_mma(acc[n], a[2 * h], b[2 * h], a[2 * h + 1], b[2 * h + 1], x[n][4 * j + 2 * h], x[n][4 * j + 2 * h + 1]);
+            for (int n = 0; n < NT; ++n)
+                few_mma(j < 4 ? acc[n] : more[n], a[2 * h], b[2 * h], a[2 * h + 1], b[2 * h + 1], x[n][4 * j + 2 * h], x[n][4 * j + 2 * h + 1]);
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[n][k] += more[n][k];
 }
 
 }  // namespace bof4

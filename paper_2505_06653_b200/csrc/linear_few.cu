@@ -2,7 +2,7 @@
 //
 // A CTA holds `groups` row groups of `stripes` warps.  Warp s of a group owns 256 columns of a slice of the columns for every
 // row tile (16 rows) that the group visits, its tokens in registers (decode.cuh).  The parts of a row tile are added up over
-// the stripes in shared memory, in a fixed order, a few row tiles at a time (two buffers, one barrier per kFewDefer tiles).
+// the stripes in shared memory, in a fixed order, a few row tiles at a time (two buffers, one barrier per FewGeo::defer tiles).
 // A matrix with more columns than a CTA has warps for is cut into slices of equal numbers of stripes; the CTAs of a slice
 // take the same row tiles as their counterparts in the others, leave their sums in the workspace, and the one that is last
 // (a ticket: nobody waits) adds the slices up in order.
@@ -12,13 +12,14 @@
 
 namespace bof4 {
 
-constexpr int kFewDefer = 4;
+constexpr int kFewPitch = 20;  // rows of a token, 16, and room that keeps the tokens of a quad in different banks
 template <int NT>
 struct FewGeo {
     // a lane keeps 32 registers of tokens per eight of them: 128 registers a thread for 8 tokens, 255 for 16
     static constexpr int warps = NT == 1 ? 16 : 8, threads = 32 * warps;
-    static constexpr int part = 16 * 8 * NT;  // sums of a warp and row tile
-    static constexpr int smem = kPairBytes + 2 * kFewDefer * warps * part * 4;
+    static constexpr int part = 8 * NT * kFewPitch;  // sums of a warp and row tile, [token][row]
+    static constexpr int defer = 2;                  // row tiles between two additions over the stripes
+    static constexpr int ring = warps * kFewSlots * kFewUnit, smem = ring + kPairBytes + 2 * defer * warps * part * 4 + 1024;  // (the ring is aligned to 1024)
 };
 
 struct FewWork {
@@ -29,17 +30,19 @@ struct FewWork {
 
 template <int NT, class ST, bool HALF>
 __global__ void __launch_bounds__(FewGeo<NT>::threads, 1)
-linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
+linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
                   const float* __restrict__ levels, const uint16_t* __restrict__ x, int64_t ldx, const LinearOut out,
                   const float* __restrict__ correction, int* __restrict__ status, const FewWork work, unsigned long long* __restrict__ tickets,
                   float* __restrict__ sums)
 {
     if (!after_previous()) return;
-    constexpr int W = FewGeo<NT>::warps, P = FewGeo<NT>::part, D = kFewDefer;
-    extern __shared__ __align__(256) unsigned char s_dyn[];
-    float2* const s_pairs = reinterpret_cast<float2*>(s_dyn);
-    float* const s_part = reinterpret_cast<float*>(s_dyn + kPairBytes);  // [2][D][W][P]
+    constexpr int W = FewGeo<NT>::warps, P = FewGeo<NT>::part, D = FewGeo<NT>::defer;
+    extern __shared__ unsigned char s_dyn[];
+    unsigned char* const s_base = s_dyn + ((1024u - (smem_u32(s_dyn) & 1023u)) & 1023u);  // the ring, the table, the sums
+    float2* const s_pairs = reinterpret_cast<float2*>(s_base + FewGeo<NT>::ring);
+    float* const s_part = reinterpret_cast<float*>(s_base + FewGeo<NT>::ring + kPairBytes);  // [2][D][W][P]
     __shared__ __align__(16) float2 s_levels[8];
+    __shared__ __align__(8) unsigned long long s_full[W][kFewSlots];
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int group = warp / work.stripes, stripe = warp - group * work.stripes;
@@ -49,23 +52,29 @@ linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ sc
     const int first = peer * work.groups + group, step = work.peers * work.groups;  // row tiles of this group
     const int rounds = (work.tiles - peer * work.groups + step - 1) / step;         // of the CTA: its first group has the most
     const int tokens = (int)out.tokens;
+    bool failed = false;  // a wait ran out
     if (tid == 0) {
-        if (blockIdx.x == 0) *status = 0;
+        if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
         if (work.slices > 1) tc_ticket_open(tickets + peer, work.epoch);
     }
-    FewCodes code;
-    float m[4];
-    auto fetch = [&](int i, FewCodes& c, float (&s)[4]) {
-        const int64_t r0 = ((int64_t)first + (int64_t)i * step) * 16 + g, r1 = r0 + 8;
-        const bool a = r0 < rows, b = r1 < rows;
-        const int64_t ia = r0 * cols + c0, ib = r1 * cols + c0;
-        few_load(c, codes + (ia >> 1), codes + (ib >> 1), live0 && a, live1 && a, live0 && b, live1 && b);
-        s[0] = few_scale<ST>(scales, ia >> block_shift, live0 && a);
-        s[2] = few_scale<ST>(scales, ib >> block_shift, live0 && b);
-        s[1] = HALF ? few_scale<ST>(scales, (ia + 32) >> block_shift, live1 && a) : 0.0f;
-        s[3] = HALF ? few_scale<ST>(scales, (ib + 32) >> block_shift, live1 && b) : 0.0f;
+    // The group's row tiles in order: codes and constants are requested kFewAhead of them before they are used.
+    const uint32_t ring = smem_u32(s_base) + (uint32_t)(warp * kFewSlots * kFewUnit), lanes = (live0 ? 5u : 0u) | (live1 ? 10u : 0u);
+    const int mine = busy && first < work.tiles ? (work.tiles - 1 - first) / step + 1 : 0;  // row tiles of this group
+    const int64_t per_row = cols >> block_shift, jump = (int64_t)step * 16 * per_row;
+    int64_t at = ((int64_t)first * 16 + g) * per_row + (c0 >> block_shift);
+    int left = (int)(rows - (int64_t)first * 16) - g, row = first * 16, asked = 0;
+    FewConst<ST, HALF> m[kFewAhead + 1];  // of the next units, the oldest first
+    auto request = [&](int slot, FewConst<ST, HALF>& c) {
+        if (asked < mine && lane == 0)
+            tc_load_box(ring + (uint32_t)(slot * kFewUnit), &code_map, &s_full[warp][slot], kFewUnit, (int)(c0 >> 1), row);
+        c.load(scales, at, at + 8 * per_row, ((left > 0 ? 3u : 0u) | (left > 8 ? 12u : 0u)) & lanes);
+        ++asked, row += step * 16, left -= step * 16, at += jump;
     };
-    fetch(0, code, m);
+    if (lane < kFewSlots) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_full[warp][lane])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < kFewAhead; ++k) request(k, m[k]);
     uint32_t xr[NT][32];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -76,29 +85,35 @@ linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ sc
     fill_pairs(s_pairs, levels, tid, FewGeo<NT>::threads);
     __syncthreads();
     const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
-    int k = 0, buf = 0;
+    int k = 0, buf = 0, slot = 0;
+    uint32_t parity = 0;
     for (int i = 0; i < rounds; ++i) {
-        FewCodes next;
-        float mn[4];
-        fetch(i + 1, next, mn);
+        __syncwarp();  // all lanes have read the slot that is asked for now
+        request(slot == 0 ? kFewAhead : slot - 1, m[kFewAhead]);
         float acc[NT][4] = {};
-        if (busy) few_multiply<HALF, NT>(code, m, xr, acc, pairs, lane8, s_levels);
-        float* const mine = s_part + ((buf * D + k) * W + warp) * P;  // [16][8 NT]
+        if (i < mine) {
+            if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
+            FewCodes code;
+            few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
+            few_multiply<ST, HALF, NT>(code, m[0], xr, acc, pairs, lane8, s_levels);
+        }
+        if (++slot == kFewSlots) slot = 0, parity ^= 1u;
+        float* const to0 = s_part + ((buf * D + k) * W + warp) * P + 2 * q * kFewPitch + g;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            *reinterpret_cast<float2*>(mine + g * 8 * NT + 8 * n + 2 * q) = make_float2(acc[n][0], acc[n][1]);
-            *reinterpret_cast<float2*>(mine + (g + 8) * 8 * NT + 8 * n + 2 * q) = make_float2(acc[n][2], acc[n][3]);
+            float* const to = to0 + 8 * n * kFewPitch;
+            to[0] = acc[n][0], to[kFewPitch] = acc[n][1], to[8] = acc[n][2], to[kFewPitch + 8] = acc[n][3];
         }
         if (k == D - 1 || i + 1 == rounds) {
             __syncthreads();
-            // the k + 1 row tiles of each group since the last time; rows fastest, so that neighbours write neighbours
-            const int per = work.groups * 16, total = (k + 1) * per * tokens;
-            for (int e = tid; e < total; e += FewGeo<NT>::threads) {
-                const int row = e & 15, rest = e >> 4, gr = rest % work.groups, rest2 = rest / work.groups, t = rest2 % tokens, j = rest2 / tokens;
-                const int64_t tile = (int64_t)peer * work.groups + gr + (int64_t)(i - k + j) * step, r = tile * 16 + row;
+            // the k + 1 row tiles of each group since the last time; rows along the lanes, so that neighbours write neighbours
+            for (uint32_t w = (uint32_t)tid >> 4; w < (uint32_t)((k + 1) * work.groups * tokens); w += FewGeo<NT>::threads / 16) {
+                const uint32_t rest = w / (uint32_t)tokens, t = w - rest * (uint32_t)tokens, j = rest / (uint32_t)work.groups, gr = rest - j * (uint32_t)work.groups;
+                const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)(i - k + (int)j) * step) * 16 + (lane & 15);
+                const float* p = s_part + ((buf * D + j) * W + gr * work.stripes) * P + t * kFewPitch + (lane & 15);
                 if (r >= rows) continue;
-                const float* p = s_part + ((buf * D + j) * W + gr * work.stripes) * P + row * 8 * NT + t;
                 float sum = 0.0f;
+#pragma unroll 8
                 for (int s = 0; s < work.stripes; ++s) sum += p[s * P];
                 if (work.slices > 1)
                     sums[((int64_t)slice * tokens + t) * rows + r] = sum;
@@ -110,10 +125,10 @@ linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ sc
         } else {
             ++k;
         }
-        code = next;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) m[u] = mn[u];
+        for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
     }
+    if (failed) atomicExch(status, 1);
     if (work.slices == 1) return;
     __threadfence();
     __syncthreads();
@@ -124,11 +139,12 @@ linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ sc
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    for (int e = tid; e < rounds * work.groups * 16 * tokens; e += FewGeo<NT>::threads) {
-        const int row = e & 15, rest = e >> 4, gr = rest % work.groups, rest2 = rest / work.groups, i = rest2 % rounds, t = rest2 / rounds;
-        const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)i * step) * 16 + row;
+    for (uint32_t w = (uint32_t)tid >> 4; w < (uint32_t)(rounds * work.groups * tokens); w += FewGeo<NT>::threads / 16) {
+        const uint32_t rest = w / (uint32_t)tokens, t = w - rest * (uint32_t)tokens, i = rest / (uint32_t)work.groups, gr = rest - i * (uint32_t)work.groups;
+        const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)i * step) * 16 + (lane & 15);
         if (r >= rows) continue;
         float sum = 0.0f;
+#pragma unroll 4
         for (int s = 0; s < work.slices; ++s) sum += __ldcg(sums + ((int64_t)s * tokens + t) * rows + r);
         out.store(sum + (correction ? correction[(int64_t)t * rows + r] : 0.0f), out.bias_at(r), out.residual_at(t, r), t, r);
     }
@@ -138,6 +154,11 @@ linear_few_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ sc
 // forms its terms, and the one with a row's first entry adds the row's up, in the order of the list; a row that runs past the
 // CTA's 256 entries is finished from global memory.
 constexpr int kFewTokens = 16;
+template <class ST>
+__device__ __forceinline__ float scale_at(const void* scales, int64_t b)
+{
+    return ST::code == BOF4_F32 ? __ldg(static_cast<const float*>(scales) + b) : bf16_value(__ldg(static_cast<const uint16_t*>(scales) + b));
+}
 template <class ST>
 __global__ void __launch_bounds__(256)
 few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
@@ -157,7 +178,7 @@ few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict_
     auto change_of = [&](int64_t k) -> float {
         const int64_t i = idx[k];
         const uint32_t byte = codes[i >> 1], c = (i & 1) ? (byte & 15u) : (byte >> 4);
-        return bf16_value(val[k]) - bf16_value(bf16_round(__fmul_rn(few_scale<ST>(scales, i >> block_shift, true), __ldg(levels + c))));
+        return bf16_value(val[k]) - bf16_value(bf16_round(__fmul_rn(scale_at<ST>(scales, i >> block_shift), __ldg(levels + c))));
     };
     const int tid = threadIdx.x;
     for (int64_t base = (int64_t)blockIdx.x * 256; base < k_end; base += (int64_t)gridDim.x * 256) {
@@ -247,11 +268,13 @@ int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, co
     }
     p.work.epoch = tc_next_epoch();
     int rc;
+    CUtensorMap code_map;
+    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 128, 16, &code_map))) return rc;
 #define BOF4_FEW_GO(NT_, ST_, HALF_)                                                                                                              \
     {                                                                                                                                             \
         constexpr auto kern = linear_few_kernel<NT_, ST_, HALF_>;                                                                                 \
         if ((rc = ensure_dynamic_smem<kern>(FewGeo<NT_>::smem))) return rc;                                                                       \
-        launch_after(kern, p.grid, FewGeo<NT_>::threads, FewGeo<NT_>::smem, st, w.codes, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
+        launch_after(kern, p.grid, FewGeo<NT_>::threads, FewGeo<NT_>::smem, st, code_map, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
                      ldx, out, correction, status, p.work, reinterpret_cast<unsigned long long*>(base), reinterpret_cast<float*>(base + p.sums)); \
     }
 #define BOF4_FEW_S(NT_, ST_) { if (w.block_size == 32) BOF4_FEW_GO(NT_, ST_, true) else BOF4_FEW_GO(NT_, ST_, false) }

@@ -32,9 +32,11 @@ namespace bof4 {
 
 constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMoeTokens = 64, kMoeExperts = 512, kMoeTop = 16;
-constexpr int kMoePart = 128;      // sums of a warp and unit: 16 rows, 8 columns
-constexpr int kMoeDefer = 4;       // units between two additions over the stripes
-constexpr int kMoeSmem = kPairBytes + 2 * kMoeDefer * kMoeWarps * kMoePart * 4;
+constexpr int kMoePitch = 20;      // sums of a column, 16 rows, and room that keeps the columns of a quad in different banks
+constexpr int kMoePart = 8 * kMoePitch;  // sums of a warp and unit, [column][row]
+constexpr int kMoeDefer = 2;       // units between two additions over the stripes
+constexpr int kMoeRing = kMoeWarps * kFewSlots * kFewUnit;
+constexpr int kMoeSmem = kMoeRing + kPairBytes + 2 * kMoeDefer * kMoeWarps * kMoePart * 4 + 1024;  // (the ring is aligned to 1024)
 constexpr int kMoeChoices = kMoeTokens * kMoeTop;
 constexpr uint32_t kMoeSpin = 1u << 22;
 
@@ -45,8 +47,7 @@ struct MoeArgs {
     bool renormalize, router_bf16, y_bf16;
     float scale;
     const void* router;
-    const uint8_t *codes1, *codes2;  // gate and up [experts][2 ffn][hidden], down [experts][hidden][ffn]
-    const void *scales1, *scales2;
+    const void *scales1, *scales2;  // of gate and up [experts][2 ffn][hidden], of down [experts][hidden][ffn]
     const float* levels;
     void* y;
     int64_t ldy;
@@ -68,12 +69,16 @@ __device__ __forceinline__ uint32_t moe_key(float v)
 }
 
 template <class ST, bool HALF>
-__global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const MoeArgs p)
+__global__ void __launch_bounds__(kMoeThreads, 1)
+moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUtensorMap map2, const __grid_constant__ MoeArgs p)
 {
-    extern __shared__ __align__(256) unsigned char s_dyn[];
-    float2* const s_pairs = reinterpret_cast<float2*>(s_dyn);
-    float* const s_part = reinterpret_cast<float*>(s_dyn + kPairBytes);  // [2][kMoeDefer][kMoeWarps][kMoePart]
+    extern __shared__ unsigned char s_dyn[];
+    unsigned char* const s_base = s_dyn + ((1024u - (smem_u32(s_dyn) & 1023u)) & 1023u);  // the ring, the table, the sums
+    float2* const s_pairs = reinterpret_cast<float2*>(s_base + kMoeRing);
+    float* const s_part = reinterpret_cast<float*>(s_base + kMoeRing + kPairBytes);  // [2][kMoeDefer][kMoeWarps][kMoePart]
     __shared__ __align__(16) float2 s_levels[8];
+    __shared__ __align__(8) unsigned long long s_full[kMoeWarps][kFewSlots];
+    __shared__ int4 s_what[2][kMoeDefer][kMoeWarps];  // of the units whose parts wait: first row, first place in the list, columns
     __shared__ uint16_t s_id[kMoeChoices];       // expert of choice t * top + j
     __shared__ uint16_t s_list[kMoeChoices];     // choices, by expert
     __shared__ uint16_t s_first[kMoeExperts + 1], s_expert[kMoeExperts];  // of the chosen experts: first place in the list, which
@@ -83,6 +88,8 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const MoeArgs p)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int grid = (int)gridDim.x;
     const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
+    if (lane < kFewSlots) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_full[warp][lane])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (tid == 0) {
         s_fail = 0;
         if (blockIdx.x == 0) *p.status = 0;
@@ -252,100 +259,125 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const MoeArgs p)
     __syncthreads();
 
     // ---- gate/up and down: the same walk over units
+    int slot = 0;            // of the ring, over both walks: nothing is on its way between them
+    uint32_t parity = 0;
+    bool failed = false;     // a wait for codes ran out
+    const uint32_t ring = smem_u32(s_base) + (uint32_t)(warp * kFewSlots * kFewUnit);
     auto walk = [&](auto second_c) {
         constexpr bool SECOND = decltype(second_c)::value;
         constexpr int PASS = SECOND ? 4 : 8;
         const int* const units = s_units[SECOND ? 1 : 0];
-        const int64_t cols = SECOND ? p.ffn : p.hidden;
-        const int tiles = SECOND ? tiles2 : tiles1;
-        const uint8_t* const codes = SECOND ? p.codes2 : p.codes1;
+        const int cols = (int)(SECOND ? p.ffn : p.hidden), hidden = (int)p.hidden, ffn = (int)p.ffn, tiles = SECOND ? tiles2 : tiles1;
         const void* const scales = SECOND ? p.scales2 : p.scales1;
-        const int stripes = (int)((cols + kFewStripe - 1) / kFewStripe), rounds = (stripes + kMoeWarps - 1) / kMoeWarps;
+        const int per_row = cols >> p.block_shift;
+        const int stripes = (cols + kFewStripe - 1) / kFewStripe, rounds = (stripes + kMoeWarps - 1) / kMoeWarps;
         const int wide = (stripes + rounds - 1) / rounds, groups = kMoeWarps / wide;  // stripes side by side, row groups of the CTA
         const int group = warp / wide, stripe = warp - group * wide;
         const bool busy = group < groups;
         const int total = units[chosen], all = grid * groups, each = total / all, extra = total % all;
         auto start_of = [&](int k) { return k * each + min(k, extra); };  // first unit of row group k of the grid
         const int group0 = (int)blockIdx.x * groups, steps = each + (group0 < extra);  // the CTA's first group has the most
-        const int begin = busy ? start_of(group0 + group) : 0, finish = busy ? start_of(group0 + group + 1) : 0;
-        // where a unit lies: chosen expert, pass, tile
-        auto place = [&](int u, int& i, int& pass, int& tile) {
-            while (u >= units[i + 1]) ++i;
-            const int in = u - units[i];
-            pass = in / tiles, tile = in - pass * tiles;
+        const int begin = busy ? start_of(group0 + group) : 0, mine = busy ? start_of(group0 + group + 1) - begin : 0;
+        // a place in the order of units: expert (of the chosen ones), pass over its tokens, tile of its rows, round over the stripes
+        struct Place {
+            int i, pass, tile, round;
         };
-        auto fetch = [&](int u, int i0, int round, FewCodes& c, float (&m)[4]) {
-            const bool ok = u < finish;
-            int i = i0, pass = 0, tile = 0;
-            if (ok) place(u, i, pass, tile);
-            const int64_t e = s_expert[ok ? i : 0], c0 = (int64_t)(round * wide + stripe) * kFewStripe + 64 * q;
-            const int64_t r0 = SECOND ? e * p.hidden + tile * 16 + g : e * 2 * p.ffn + tile * 8 + g, r1 = SECOND ? r0 + 8 : r0 + p.ffn;
-            const bool a = ok && (!SECOND || tile * 16 + g < p.hidden), b = ok && (!SECOND || tile * 16 + 8 + g < p.hidden);
-            const bool l0 = c0 < cols, l1 = c0 + 32 < cols;
-            const int64_t ia = r0 * cols + c0, ib = r1 * cols + c0;
-            few_load(c, codes + (ia >> 1), codes + (ib >> 1), l0 && a, l1 && a, l0 && b, l1 && b);
-            m[0] = few_scale<ST>(scales, ia >> p.block_shift, l0 && a);
-            m[2] = few_scale<ST>(scales, ib >> p.block_shift, l0 && b);
-            m[1] = HALF ? few_scale<ST>(scales, (ia + 32) >> p.block_shift, l1 && a) : 0.0f;
-            m[3] = HALF ? few_scale<ST>(scales, (ib + 32) >> p.block_shift, l1 && b) : 0.0f;
+        auto columns_of = [&](const Place& u) { return s_first[u.i + 1] - s_first[u.i] - u.pass * PASS; };  // tokens left for the pass
+        auto step_on = [&](Place& u) {
+            if (++u.round < rounds) return;
+            u.round = 0;
+            if (++u.tile < tiles) return;
+            u.tile = 0;
+            if (columns_of(u) > PASS) ++u.pass;
+            else ++u.i, u.pass = 0;
         };
-        int at = 0, k = 0, buf = 0;         // chosen expert of the current unit; units since the last addition
-        int have_i = -1, have_pass = -1;    // whose tokens xr holds
+        Place now{0, 0, 0, 0};
+        if (mine) {
+            while (begin >= units[now.i + 1]) ++now.i;
+            const int in = begin - units[now.i];
+            now.pass = in / tiles, now.tile = in - now.pass * tiles;
+        }
+        Place ask = now;
+        int asked = 0;
+        FewConst<ST, HALF> m[kFewAhead + 1];
+        auto request = [&](int k, FewConst<ST, HALF>& c) {
+            const bool ok = asked < mine * rounds;
+            const int e = s_expert[ok ? ask.i : 0], c0 = (ask.round * wide + stripe) * kFewStripe;
+            const int r0 = SECOND ? e * hidden + ask.tile * 16 : e * 2 * ffn + ask.tile * 8, r1 = SECOND ? r0 + 8 : r0 + ffn;
+            if (ok && lane == 0) {
+                const uint32_t bar = smem_u32(&s_full[warp][k]), dst = ring + (uint32_t)(k * kFewUnit);
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)kFewUnit) : "memory");
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                                 :
+                                 : "r"(dst + h * 1024u), "l"(reinterpret_cast<uint64_t>(SECOND ? &map2 : &map1)), "r"(bar), "r"(c0 >> 1), "r"(h ? r1 : r0)
+                                 : "memory");
+            }
+            const int cc = c0 + 64 * q;
+            const uint32_t live = ((ok && cc < cols ? 5u : 0u) | (ok && cc + 32 < cols ? 10u : 0u)) &
+                                  (SECOND ? (ask.tile * 16 + g < hidden ? 3u : 0u) | (ask.tile * 16 + 8 + g < hidden ? 12u : 0u) : 15u);
+            const int64_t col = cc >> p.block_shift;
+            c.load(scales, (int64_t)(r0 + g) * per_row + col, (int64_t)(r1 + g) * per_row + col, live);
+            ++asked;
+            if (ok) step_on(ask);
+        };
+        // (ring slots go on from where the walk before ended)
+        auto slot_after = [&](int k) { return slot + k >= kFewSlots ? slot + k - kFewSlots : slot + k; };
+#pragma unroll
+        for (int k = 0; k < kFewAhead; ++k) request(slot_after(k), m[k]);
+        int k = 0, buf = 0, have_i = -1, have_pass = -1;  // whose tokens xr holds
         uint32_t xr[1][32];
-        FewCodes code;
-        float m[4];
-        fetch(begin, 0, 0, code, m);
         for (int s = 0; s < steps; ++s) {
-            const int u = begin + s;
             float acc[1][4] = {};
-            for (int round = 0; round < rounds; ++round) {
-                FewCodes next;
-                float mn[4];
-                const bool more = round + 1 < rounds;
-                fetch(more ? u : u + 1, at, more ? round + 1 : 0, next, mn);
-                if (u < finish) {
-                    int pass, tile;
-                    place(u, at, pass, tile);
-                    if (rounds > 1 || at != have_i || pass != have_pass) {
-                        have_i = at, have_pass = pass;
-                        const int64_t c0 = (int64_t)(round * wide + stripe) * kFewStripe + 64 * q;
-                        const int n = s_first[at + 1] - s_first[at] - pass * PASS, col = SECOND ? g & 3 : g;
-                        const bool live = col < n;
-                        const int a = live ? s_list[s_first[at] + pass * PASS + col] : 0;
-                        const uint16_t* src = SECOND ? (g < 4 ? p.h_hi : p.h_lo) + (int64_t)a * p.ffn : p.x + (int64_t)(a / p.top) * p.ldx;
+            if (s < mine) {
+                if (stripe == 0 && lane == 0) s_what[buf][k][group] = make_int4(now.tile, s_first[now.i] + now.pass * PASS, columns_of(now), 0);
+                for (int round = 0; round < rounds; ++round) {
+                    __syncwarp();  // all lanes have read the slot that is asked for now
+                    request(slot_after(kFewAhead), m[kFewAhead]);
+                    if (rounds > 1 || now.i != have_i || now.pass != have_pass) {
+                        have_i = now.i, have_pass = now.pass;
+                        const int c0 = (round * wide + stripe) * kFewStripe + 64 * q, col = SECOND ? g & 3 : g;
+                        const bool live = col < columns_of(now);
+                        const int a = live ? s_list[s_first[now.i] + now.pass * PASS + col] : 0;
+                        const uint16_t* src = SECOND ? (g < 4 ? p.h_hi : p.h_lo) + (int64_t)a * ffn : p.x + (int64_t)(a / p.top) * p.ldx;
                         few_tokens(xr[0], src + c0, live && c0 < cols, live && c0 + 32 < cols);
                     }
-                    few_multiply<HALF, 1>(code, m, xr, acc, pairs, lane8, s_levels);
-                }
-                code = next;
+                    if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
+                    FewCodes code;
+                    few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
+                    few_multiply<ST, HALF, 1>(code, m[0], xr, acc, pairs, lane8, s_levels);
+                    if (++slot == kFewSlots) slot = 0, parity ^= 1u;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) m[v] = mn[v];
+                    for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
+                    step_on(now);
+                }
+            } else if (busy && stripe == 0 && lane == 0) {
+                s_what[buf][k][group] = make_int4(0, 0, 0, 0);
             }
-            float* const mine = s_part + ((buf * kMoeDefer + k) * kMoeWarps + warp) * kMoePart;  // [16][8]
-            *reinterpret_cast<float2*>(mine + g * 8 + 2 * q) = make_float2(acc[0][0], acc[0][1]);
-            *reinterpret_cast<float2*>(mine + (g + 8) * 8 + 2 * q) = make_float2(acc[0][2], acc[0][3]);
+            float* const to = s_part + ((buf * kMoeDefer + k) * kMoeWarps + warp) * kMoePart + 2 * q * kMoePitch + g;
+            to[0] = acc[0][0], to[kMoePitch] = acc[0][1], to[8] = acc[0][2], to[kMoePitch + 8] = acc[0][3];
             if (k == kMoeDefer - 1 || s + 1 == steps) {
                 __syncthreads();
-                // results of k + 1 units of each group: gate/up 8 rows x 8 tokens, down 16 rows x 4 tokens, rows fastest
-                for (int e = tid; e < (k + 1) * groups * 64; e += kMoeThreads) {
-                    const int row = SECOND ? e & 15 : e & 7, col = SECOND ? (e >> 4) & 3 : (e >> 3) & 7, rest = e >> 6, gr = rest % groups, j = rest / groups;
-                    const int v = start_of(group0 + gr) + s - k + j;
-                    if (v >= start_of(group0 + gr + 1)) continue;
-                    int i = 0, pass, tile;
-                    place(v, i, pass, tile);
-                    if (col >= s_first[i + 1] - s_first[i] - pass * PASS) continue;
-                    const int64_t a = s_list[s_first[i] + pass * PASS + col];
-                    const float* part = s_part + ((buf * kMoeDefer + j) * kMoeWarps + gr * wide) * kMoePart;
+                // results of k + 1 units of each group, rows along the lanes: gate/up 8 rows x 8 tokens, down 16 rows x 4 tokens
+                for (uint32_t e = (uint32_t)tid; e < (uint32_t)((k + 1) * groups * 64); e += kMoeThreads) {
+                    const uint32_t row = SECOND ? e & 15u : e & 7u, col = SECOND ? (e >> 4) & 3u : (e >> 3) & 7u, rest = e >> 6;
+                    const uint32_t j = rest / (uint32_t)groups, gr = rest - j * (uint32_t)groups;
+                    const int4 what = s_what[buf][j][gr];
+                    if ((int)col >= what.z) continue;
+                    const int a = s_list[what.y + (int)col];
+                    const float* part = s_part + ((buf * kMoeDefer + j) * kMoeWarps + gr * wide) * kMoePart + col * kMoePitch + row;
+                    constexpr int other = SECOND ? 4 * kMoePitch : 8;
                     float v0 = 0.0f, v1 = 0.0f;
-                    const int i0 = row * 8 + col, i1 = SECOND ? i0 + 4 : i0 + 64;
-                    for (int w = 0; w < wide; ++w) v0 += part[w * kMoePart + i0], v1 += part[w * kMoePart + i1];
+#pragma unroll 4
+                    for (int w = 0; w < wide; ++w) v0 += part[w * kMoePart], v1 += part[w * kMoePart + other];
                     if (SECOND) {
-                        const int64_t o = tile * 16 + row;
-                        if (o < p.hidden) p.out[a * p.hidden + o] = v0 + v1;
+                        const int o = what.x * 16 + (int)row;
+                        if (o < hidden) p.out[(int64_t)a * hidden + o] = v0 + v1;
                     } else {
                         const float h = activate(v0, p.act) * v1;
                         const uint16_t hi = bf16_round(h);
-                        const int64_t o = a * p.ffn + tile * 8 + row;
+                        const int64_t o = (int64_t)a * ffn + what.x * 8 + (int)row;
                         p.h_hi[o] = hi;
                         p.h_lo[o] = bf16_round(isfinite(h) ? h - bf16_value(hi) : 0.0f);
                     }
@@ -356,6 +388,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const MoeArgs p)
                 ++k;
             }
         }
+        if (failed) atomicExch(p.status, 1);
     };
     walk(std::false_type{});
     if (!meet(1)) return;
@@ -469,8 +502,6 @@ extern "C" int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t 
     a.y_bf16 = y_dtype == BOF4_BF16;
     a.scale = scale;
     a.router = d_router;
-    a.codes1 = d_gate_up_codes;
-    a.codes2 = d_down_codes;
     a.scales1 = d_gate_up_scales;
     a.scales2 = d_down_scales;
     a.levels = d_codebook;
@@ -496,11 +527,15 @@ extern "C" int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t 
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int rc;
+    CUtensorMap map1, map2;
+    if ((rc = tc_make_map(fn, d_gate_up_codes, 1, hidden / 2, n_experts * 2 * ffn, hidden / 2, 128, 8, &map1)) ||
+        (rc = tc_make_map(fn, d_down_codes, 1, ffn / 2, n_experts * hidden, ffn / 2, 128, 8, &map2)))
+        return rc;
 #define BOF4_MOE_GO(ST_, HALF_)                                                  \
     {                                                                            \
         constexpr auto kern = moe_kernel<ST_, HALF_>;                            \
         if ((rc = ensure_dynamic_smem<kern>(kMoeSmem))) return rc;               \
-        BOF4_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, static_cast<MoeArgs>(a)));  \
+        BOF4_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, map1, map2, static_cast<MoeArgs>(a)));  \
     }
     if (scale_dtype == BOF4_F32) {
         if (block_size == 32) BOF4_MOE_GO(F32, true) else BOF4_MOE_GO(F32, false)
