@@ -148,10 +148,24 @@ __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1,
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The table of level pairs lies at this address of shared memory, so that one permute makes a whole address of a code byte and the
+// lane: byte * 256 + lane * 8 + 0x10000.  What comes before it is the kernel's to use, the ring lies behind it.
+constexpr uint32_t kFewTable = 0x10000u, kFewRing = kFewTable + kPairBytes;
+// Eight codes to bf16 through the table; column = lane * 8 + kFewTable.
+__device__ __forceinline__ void few_lookup8(uint32_t w, float2 mm, uint32_t column, uint32_t* o)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float2 l;
+        asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l.x), "=f"(l.y) : "r"(__byte_perm(w, column, 0x7604u | ((uint32_t)k << 4))));
+        const float2 v = __fmul2_rn(mm, l);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[k]) : "f"(v.y), "f"(v.x));
+    }
+}
 // acc[n]: rows g (0, 1) and 8 + g (2, 3), tokens 8 n + 2 q and 8 n + 2 q + 1.
 template <class ST, bool HALF, int NT>
 __device__ __forceinline__ void few_multiply(const FewCodes& c, const FewConst<ST, HALF>& raw, const uint32_t (&x)[NT][32], float (&acc)[NT][4],
-                                             uint32_t pairs, uint32_t lane8, const float2* levels)
+                                             uint32_t column, const float2* levels)
 {
     const float m[4] = {raw.value(0), HALF ? raw.value(1) : 0.0f, raw.value(2), HALF ? raw.value(3) : 0.0f};
     uint32_t lo[4], hi[4];
@@ -166,8 +180,8 @@ __device__ __forceinline__ void few_multiply(const FewCodes& c, const FewConst<S
         const uint32_t wb = (j & 3) == 0 ? vb.x : (j & 3) == 1 ? vb.y : (j & 3) == 2 ? vb.z : vb.w;
         const float ma = HALF && j >= 4 ? m[1] : m[0];
         uint32_t a[4], b[4];
-        tc_lookup8(wa, make_float2(ma, ma), pairs, lane8, a);
-        if (j < 4) tc_lookup8(wb, make_float2(m[2], m[2]), pairs, lane8, b);
+        few_lookup8(wa, make_float2(ma, ma), column, a);
+        if (j < 4) few_lookup8(wb, make_float2(m[2], m[2]), column, b);
         else lt_lookup8(wb, lo, hi, b);
 #pragma unroll
         for (int h = 0; h < 2; ++h)

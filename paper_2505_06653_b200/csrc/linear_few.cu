@@ -17,14 +17,23 @@ template <int NT>
 struct FewGeo {
     // a lane keeps 32 registers of tokens per eight of them: 128 registers a thread for 8 tokens, 255 for 16
     static constexpr int warps = NT == 1 ? 16 : 8, threads = 32 * warps;
-    static constexpr int part = 8 * NT * kFewPitch;  // sums of a warp and row tile, [token][row]
-    static constexpr int defer = 2;                  // row tiles between two additions over the stripes
-    static constexpr int ring = warps * kFewSlots * kFewUnit, smem = ring + kPairBytes + 2 * defer * warps * part * 4 + 1024;  // (the ring is aligned to 1024)
+    static constexpr int ring = warps * kFewSlots * kFewUnit;
+    // row tiles between two additions over the stripes: as many as two buffers of sums, [tile][warp][token][row], have room for
+    // before the table (the fewer barriers the better: with two of them 28672 x 8192 by one token takes 6 us more than without any)
+    static constexpr int sums = 54 * 1024;
+    static int defer(int tokens)
+    {
+        const int d = sums / (2 * warps * tokens * kFewPitch * 4);
+        return d < 16 ? d : 16;
+    }
+    static_assert(sums + 8192 <= (int)kFewTable, "the sums lie before the table");
 };
+
+constexpr int kFewBegin = 1024;  // dynamic memory begins there or later
 
 struct FewWork {
     int stripes, groups, slices, peers;  // stripes of a slice; CTAs of a slice
-    int tiles;
+    int tiles, defer;
     unsigned long long epoch;
 };
 
@@ -36,11 +45,13 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
                   float* __restrict__ sums)
 {
     if (!after_previous()) return;
-    constexpr int W = FewGeo<NT>::warps, P = FewGeo<NT>::part, D = FewGeo<NT>::defer;
+    constexpr int W = FewGeo<NT>::warps;
+    const int D = work.defer, P = (int)out.tokens * kFewPitch;
     extern __shared__ unsigned char s_dyn[];
-    unsigned char* const s_base = s_dyn + ((1024u - (smem_u32(s_dyn) & 1023u)) & 1023u);  // the ring, the table, the sums
-    float2* const s_pairs = reinterpret_cast<float2*>(s_base + FewGeo<NT>::ring);
-    float* const s_part = reinterpret_cast<float*>(s_base + FewGeo<NT>::ring + kPairBytes);  // [2][D][W][P]
+    // the sums, the table at kFewTable, the ring
+    unsigned char* const s_zero = s_dyn - smem_u32(s_dyn);
+    float2* const s_pairs = reinterpret_cast<float2*>(s_zero + kFewTable);
+    float* const s_part = reinterpret_cast<float*>(s_dyn);  // [2][D][W][P]
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ __align__(8) unsigned long long s_full[W][kFewSlots];
     __shared__ int s_last;
@@ -52,13 +63,17 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     const int first = peer * work.groups + group, step = work.peers * work.groups;  // row tiles of this group
     const int rounds = (work.tiles - peer * work.groups + step - 1) / step;         // of the CTA: its first group has the most
     const int tokens = (int)out.tokens;
+    if (smem_u32(s_dyn) < (uint32_t)kFewBegin || smem_u32(s_dyn) + FewGeo<NT>::sums > kFewTable) {  // not the layout that this was built for
+        if (tid == 0 && blockIdx.x == 0) *status = 1;
+        return;
+    }
     bool failed = false;  // a wait ran out
     if (tid == 0) {
         if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
         if (work.slices > 1) tc_ticket_open(tickets + peer, work.epoch);
     }
     // The group's row tiles in order: codes and constants are requested kFewAhead of them before they are used.
-    const uint32_t ring = smem_u32(s_base) + (uint32_t)(warp * kFewSlots * kFewUnit), lanes = (live0 ? 5u : 0u) | (live1 ? 10u : 0u);
+    const uint32_t ring = kFewRing + (uint32_t)(warp * kFewSlots * kFewUnit), lanes = (live0 ? 5u : 0u) | (live1 ? 10u : 0u);
     const int mine = busy && first < work.tiles ? (work.tiles - 1 - first) / step + 1 : 0;  // row tiles of this group
     const int64_t per_row = cols >> block_shift, jump = (int64_t)step * 16 * per_row;
     int64_t at = ((int64_t)first * 16 + g) * per_row + (c0 >> block_shift);
@@ -84,7 +99,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     if (tid < 8) s_levels[tid] = make_float2(__ldg(levels + 2 * tid), __ldg(levels + 2 * tid + 1));
     fill_pairs(s_pairs, levels, tid, FewGeo<NT>::threads);
     __syncthreads();
-    const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
+    const uint32_t column = (uint32_t)lane * 8u + kFewTable;
     int k = 0, buf = 0, slot = 0;
     uint32_t parity = 0;
     for (int i = 0; i < rounds; ++i) {
@@ -95,14 +110,16 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
             if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
             FewCodes code;
             few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
-            few_multiply<ST, HALF, NT>(code, m[0], xr, acc, pairs, lane8, s_levels);
+            few_multiply<ST, HALF, NT>(code, m[0], xr, acc, column, s_levels);
         }
         if (++slot == kFewSlots) slot = 0, parity ^= 1u;
         float* const to0 = s_part + ((buf * D + k) * W + warp) * P + 2 * q * kFewPitch + g;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float* const to = to0 + 8 * n * kFewPitch;
-            to[0] = acc[n][0], to[kFewPitch] = acc[n][1], to[8] = acc[n][2], to[kFewPitch + 8] = acc[n][3];
+            const int t = 8 * n + 2 * q;
+            if (t < tokens) to[0] = acc[n][0], to[8] = acc[n][2];
+            if (t + 1 < tokens) to[kFewPitch] = acc[n][1], to[kFewPitch + 8] = acc[n][3];
         }
         if (k == D - 1 || i + 1 == rounds) {
             __syncthreads();
@@ -116,7 +133,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
 #pragma unroll 8
                 for (int s = 0; s < work.stripes; ++s) sum += p[s * P];
                 if (work.slices > 1)
-                    sums[((int64_t)slice * tokens + t) * rows + r] = sum;
+                    sums[((int64_t)slice * tokens + t) * (work.tiles * 16) + r] = sum;
                 else
                     out.store(sum + (correction ? correction[(int64_t)t * rows + r] : 0.0f), out.bias_at(r), out.residual_at(t, r), t, r);
             }
@@ -139,14 +156,27 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    for (uint32_t w = (uint32_t)tid >> 4; w < (uint32_t)(rounds * work.groups * tokens); w += FewGeo<NT>::threads / 16) {
+    // four rows a thread, several slices on their way at a time
+    const int64_t pitch = (int64_t)work.tiles * 16;
+    for (uint32_t w = (uint32_t)tid >> 2; w < (uint32_t)(rounds * work.groups * tokens); w += FewGeo<NT>::threads / 4) {
         const uint32_t rest = w / (uint32_t)tokens, t = w - rest * (uint32_t)tokens, i = rest / (uint32_t)work.groups, gr = rest - i * (uint32_t)work.groups;
-        const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)i * step) * 16 + (lane & 15);
-        if (r >= rows) continue;
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int s = 0; s < work.slices; ++s) sum += __ldcg(sums + ((int64_t)s * tokens + t) * rows + r);
-        out.store(sum + (correction ? correction[(int64_t)t * rows + r] : 0.0f), out.bias_at(r), out.residual_at(t, r), t, r);
+        const int64_t tile = (int64_t)peer * work.groups + gr + (int64_t)i * step, r = tile * 16 + 4 * (lane & 3);
+        if (tile >= work.tiles) continue;
+        const float4* p = reinterpret_cast<const float4*>(sums + (int64_t)t * pitch + r);
+        const int64_t next = tokens * pitch / 4;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < work.slices; s += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = s + u < work.slices ? __ldcg(p + (s + u) * next) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
+        }
+        const float z[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (r + u < rows)
+                out.store(z[u] + (correction ? correction[(int64_t)t * rows + r + u] : 0.0f), out.bias_at(r + u), out.residual_at(t, r + u), t, r + u);
     }
 }
 
@@ -221,18 +251,24 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
     FewPlan p;
     const int warps = tokens > 8 ? FewGeo<2>::warps : FewGeo<1>::warps;
     const int64_t stripes = (cols + kFewStripe - 1) / kFewStripe, tiles = (rows + 15) / 16;
-    const int64_t slices = (stripes + warps - 1) / warps;
+    // as few slices as give nearly all warps a stripe
+    int64_t slices = (stripes + warps - 1) / warps, best = 0;
+    for (int64_t n = slices; n <= 4 * slices && n <= kSMs && n <= stripes; ++n) {
+        const int64_t wide = (stripes + n - 1) / n, used = wide * (warps / wide) * 64 * stripes / (wide * n);  // warps that have a stripe, in 64ths
+        if (used > best + warps * 4) best = used, slices = n;
+    }
     FewWork& w = p.work;
     w.slices = (int)slices;
     w.stripes = (int)((stripes + slices - 1) / slices);
     w.groups = warps / w.stripes;
     if (w.groups > tiles) w.groups = (int)tiles;
     w.tiles = (int)tiles;
+    w.defer = tokens > 8 ? FewGeo<2>::defer((int)tokens) : FewGeo<1>::defer((int)tokens);
     const int64_t want = (tiles + w.groups - 1) / w.groups, have = kSMs / slices;
     w.peers = (int)(want < have ? want : have);
     p.grid = w.peers * w.slices;
     p.sums = up256((size_t)w.peers * 8);
-    p.correction = p.sums + (slices > 1 ? up256((size_t)slices * tokens * rows * 4) : 0);
+    p.correction = p.sums + (slices > 1 ? up256((size_t)slices * tokens * tiles * 64) : 0);
     p.total = p.correction + (list ? up256((size_t)tokens * rows * 4) : 0);
     return p;
 }
@@ -273,8 +309,9 @@ int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, co
 #define BOF4_FEW_GO(NT_, ST_, HALF_)                                                                                                              \
     {                                                                                                                                             \
         constexpr auto kern = linear_few_kernel<NT_, ST_, HALF_>;                                                                                 \
-        if ((rc = ensure_dynamic_smem<kern>(FewGeo<NT_>::smem))) return rc;                                                                       \
-        launch_after(kern, p.grid, FewGeo<NT_>::threads, FewGeo<NT_>::smem, st, code_map, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
+        constexpr int smem = (int)kFewRing + FewGeo<NT_>::ring - kFewBegin;  \
+        if ((rc = ensure_dynamic_smem<kern>(smem))) return rc;                                                                       \
+        launch_after(kern, p.grid, FewGeo<NT_>::threads, smem, st, code_map, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
                      ldx, out, correction, status, p.work, reinterpret_cast<unsigned long long*>(base), reinterpret_cast<float*>(base + p.sums)); \
     }
 #define BOF4_FEW_S(NT_, ST_) { if (w.block_size == 32) BOF4_FEW_GO(NT_, ST_, true) else BOF4_FEW_GO(NT_, ST_, false) }

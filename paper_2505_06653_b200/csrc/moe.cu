@@ -36,7 +36,10 @@ constexpr int kMoePitch = 20;      // sums of a column, 16 rows, and room that k
 constexpr int kMoePart = 8 * kMoePitch;  // sums of a warp and unit, [column][row]
 constexpr int kMoeDefer = 2;       // units between two additions over the stripes
 constexpr int kMoeRing = kMoeWarps * kFewSlots * kFewUnit;
-constexpr int kMoeSmem = kMoeRing + kPairBytes + 2 * kMoeDefer * kMoeWarps * kMoePart * 4 + 1024;  // (the ring is aligned to 1024)
+constexpr int kMoeSums = 2 * kMoeDefer * kMoeWarps * kMoePart * 4;
+static_assert(kMoeSums + 16384 <= (int)kFewTable, "the sums lie before the table, behind 16 KiB of other variables");
+constexpr int kMoeBegin = 12288;   // dynamic memory begins there or later (behind 11.6 KiB of other variables)
+constexpr int kMoeSmem = (int)kFewRing + kMoeRing - kMoeBegin;
 constexpr int kMoeChoices = kMoeTokens * kMoeTop;
 constexpr uint32_t kMoeSpin = 1u << 22;
 
@@ -73,9 +76,9 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
 moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUtensorMap map2, const __grid_constant__ MoeArgs p)
 {
     extern __shared__ unsigned char s_dyn[];
-    unsigned char* const s_base = s_dyn + ((1024u - (smem_u32(s_dyn) & 1023u)) & 1023u);  // the ring, the table, the sums
-    float2* const s_pairs = reinterpret_cast<float2*>(s_base + kMoeRing);
-    float* const s_part = reinterpret_cast<float*>(s_base + kMoeRing + kPairBytes);  // [2][kMoeDefer][kMoeWarps][kMoePart]
+    // the sums, the table at kFewTable, the ring
+    float2* const s_pairs = reinterpret_cast<float2*>(s_dyn - smem_u32(s_dyn) + kFewTable);
+    float* const s_part = reinterpret_cast<float*>(s_dyn);  // [2][kMoeDefer][kMoeWarps][kMoePart]
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ __align__(8) unsigned long long s_full[kMoeWarps][kFewSlots];
     __shared__ int4 s_what[2][kMoeDefer][kMoeWarps];  // of the units whose parts wait: first row, first place in the list, columns
@@ -87,9 +90,13 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     __shared__ int s_chosen, s_fail;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int grid = (int)gridDim.x;
-    const uint32_t pairs = (uint32_t)__cvta_generic_to_shared(s_pairs), lane8 = (uint32_t)lane * 8u;
+    const uint32_t column = (uint32_t)lane * 8u + kFewTable;
     if (lane < kFewSlots) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_full[warp][lane])) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (smem_u32(s_dyn) < (uint32_t)kMoeBegin || smem_u32(s_dyn) + kMoeSums > kFewTable) {  // not the layout that this was built for: the same for all CTAs
+        if (tid == 0 && blockIdx.x == 0) *p.status = 1;
+        return;
+    }
     if (tid == 0) {
         s_fail = 0;
         if (blockIdx.x == 0) *p.status = 0;
@@ -262,7 +269,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     int slot = 0;            // of the ring, over both walks: nothing is on its way between them
     uint32_t parity = 0;
     bool failed = false;     // a wait for codes ran out
-    const uint32_t ring = smem_u32(s_base) + (uint32_t)(warp * kFewSlots * kFewUnit);
+    const uint32_t ring = kFewRing + (uint32_t)(warp * kFewSlots * kFewUnit);
     auto walk = [&](auto second_c) {
         constexpr bool SECOND = decltype(second_c)::value;
         constexpr int PASS = SECOND ? 4 : 8;
@@ -346,7 +353,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                     if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
                     FewCodes code;
                     few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
-                    few_multiply<ST, HALF, 1>(code, m[0], xr, acc, pairs, lane8, s_levels);
+                    few_multiply<ST, HALF, 1>(code, m[0], xr, acc, column, s_levels);
                     if (++slot == kFewSlots) slot = 0, parity ^= 1u;
 #pragma unroll
                     for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
