@@ -151,38 +151,50 @@ __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1,
 // The table of level pairs lies at this address of shared memory, so that one permute makes a whole address of a code byte and the
 // lane: byte * 256 + lane * 8 + 0x10000.  What comes before it is the kernel's to use, the ring lies behind it.
 constexpr uint32_t kFewTable = 0x10000u, kFewRing = kFewTable + kPairBytes;
-// Eight codes to bf16 through the table; column = lane * 8 + kFewTable.
-__device__ __forceinline__ void few_lookup8(uint32_t w, float2 mm, uint32_t column, uint32_t* o)
+// Eight codes through the table, in two halves: the look-ups, and products and rounding.  column = lane * 8 + kFewTable.
+__device__ __forceinline__ void few_fetch8(uint32_t w, uint32_t column, float2 (&l)[4])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l[k].x), "=f"(l[k].y) : "r"(__byte_perm(w, column, 0x7604u | ((uint32_t)k << 4))));
+}
+__device__ __forceinline__ void few_round8(float m, const float2 (&l)[4], uint32_t (&o)[4])
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float2 l;
-        asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l.x), "=f"(l.y) : "r"(__byte_perm(w, column, 0x7604u | ((uint32_t)k << 4))));
-        const float2 v = __fmul2_rn(mm, l);
+        const float2 v = __fmul2_rn(make_float2(m, m), l[k]);
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[k]) : "f"(v.y), "f"(v.x));
     }
 }
-// acc[n]: rows g (0, 1) and 8 + g (2, 3), tokens 8 n + 2 q and 8 n + 2 q + 1.
+__device__ __forceinline__ uint32_t few_word(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+
+// acc[n]: rows g (0, 1) and 8 + g (2, 3), tokens 8 n + 2 q and 8 n + 2 q + 1.  A step is a word of each row; the look-ups of the
+// next step are issued before the products of this one.
 template <class ST, bool HALF, int NT>
 __device__ __forceinline__ void few_multiply(const FewCodes& c, const FewConst<ST, HALF>& raw, const uint32_t (&x)[NT][32], float (&acc)[NT][4],
                                              uint32_t column, const float2* levels)
 {
-    const float m[4] = {raw.value(0), HALF ? raw.value(1) : 0.0f, raw.value(2), HALF ? raw.value(3) : 0.0f};
+    const float m[4] = {raw.value(0), HALF ? raw.value(1) : raw.value(0), raw.value(2), HALF ? raw.value(3) : raw.value(2)};
     uint32_t lo[4], hi[4];
-    lt_table(HALF ? m[3] : m[2], levels, lo, hi);
+    lt_table(m[3], levels, lo, hi);
     float more[NT][4] = {};  // a second chain of sums
+    float2 la[2][4], lb[2][4];
+    // step i takes words of the first and of the last 32 columns in turn: table and permutes next to one another
+    auto word = [](int i) { return (i & 1) * 4 + (i >> 1); };
+    auto fetch = [&](int i) {
+        const int j = word(i);
+        few_fetch8(few_word(c.v[j >> 2], j & 3), column, la[i & 1]);
+        if (j < 4) few_fetch8(few_word(c.v[2 + (j >> 2)], j & 3), column, lb[i & 1]);
+    };
+    fetch(0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        // words of the first and of the last 32 columns in turn: table and permutes next to one another
-        const int j = (i & 1) * 4 + (i >> 1);
-        const uint4 va = c.v[j >> 2], vb = c.v[2 + (j >> 2)];
-        const uint32_t wa = (j & 3) == 0 ? va.x : (j & 3) == 1 ? va.y : (j & 3) == 2 ? va.z : va.w;
-        const uint32_t wb = (j & 3) == 0 ? vb.x : (j & 3) == 1 ? vb.y : (j & 3) == 2 ? vb.z : vb.w;
-        const float ma = HALF && j >= 4 ? m[1] : m[0];
+        const int j = word(i);
+        if (i < 7) fetch(i + 1);
         uint32_t a[4], b[4];
-        few_lookup8(wa, make_float2(ma, ma), column, a);
-        if (j < 4) few_lookup8(wb, make_float2(m[2], m[2]), column, b);
-        else lt_lookup8(wb, lo, hi, b);
+        few_round8(m[j >> 2], la[i & 1], a);
+        if (j < 4) few_round8(m[2], lb[i & 1], b);
+        else lt_lookup8(few_word(c.v[2 + (j >> 2)], j & 3), lo, hi, b);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll

@@ -220,72 +220,86 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             if (++in == per_tile) in = 0, ++tile;
         }
     } else if (warp == kLtIssue) {
-        // ---- the issuing warp
-        const uint32_t lead = lane == 0 ? 1u : 0u;
-        const uint64_t da0 = tc_smem_desc(a_ring, BWD ? 8192u : 16u), db0 = tc_smem_desc(b_ring);
-        // fp32 accumulator, bf16 x bf16, A M-major (backward) or K-major, B K-major, M = 128, N
-        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (BWD ? 1u << 15 : 0u) | ((uint32_t)(box_n >> 3) << 17) | ((uint32_t)(kLtM >> 4) << 24);
-        constexpr uint64_t a_step = BWD ? 2048 >> 4 : 32 >> 4;  // 16 of K
-        int in = in0, seg = 0, sa = 0, sb = 0;
-        uint32_t acc = 0u, pa = 0, pb = 0;
-        bool ok = true;
-        for (int n = 0; ok && n < lines; ++n) {
-            const int buf = seg & 1;
-            if (acc == 0u && !(ok = warp_wait(&s_acc_empty[buf], (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
-            for (int j = 0; j < kLtGroups; ++j) {
-                if (!(ok = warp_wait(&s_b_full[sb], pb) && warp_wait(&s_a_full[sa], pa))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t da = da0 + (uint64_t)(sa * (kLtABytes >> 4)), db = db0 + (uint64_t)(sb * (b_stage >> 4));
+        // ---- the issuing warp: one lane does it all (with the other lanes in step, their instructions predicated off, a
+        // k-block took 500 cycles to issue)
+        if (tc_elect()) {
+            auto wait = [&](unsigned long long* bar, uint32_t parity) -> bool {
+                if (tc_wait_soon(smem_u32(bar), parity)) return true;
+                s_fail = 1;
+                return false;
+            };
+            const uint64_t da0 = tc_smem_desc(a_ring, BWD ? 8192u : 16u), db0 = tc_smem_desc(b_ring);
+            // fp32 accumulator, bf16 x bf16, A M-major (backward) or K-major, B K-major, M = 128, N
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (BWD ? 1u << 15 : 0u) | ((uint32_t)(box_n >> 3) << 17) | ((uint32_t)(kLtM >> 4) << 24);
+            constexpr uint64_t a_step = BWD ? 2048 >> 4 : 32 >> 4;  // 16 of K
+            int in = in0, seg = 0, sa = 0, sb = 0;
+            uint32_t acc = 0u, pa = 0, pb = 0;
+            bool ok = true;
+            for (int n = 0; ok && n < lines; ++n) {
+                const int buf = seg & 1;
+                if (acc == 0u && !(ok = wait(&s_acc_empty[buf], (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
+                for (int j = 0; j < kLtGroups; ++j) {
+                    if (!(ok = wait(&s_b_full[sb], pb) && wait(&s_a_full[sa], pa))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = da0 + (uint64_t)(sa * (kLtABytes >> 4)), db = db0 + (uint64_t)(sb * (b_stage >> 4));
 #pragma unroll
-                for (int kk = 0; kk < kLtK / 16; ++kk) {
-                    asm volatile(
-                        "{\n\t.reg .pred p, q;\n\t"
-                        "setp.ne.b32 p, %4, 0;\n\t"
-                        "setp.ne.b32 q, %5, 0;\n\t"
-                        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                        :
-                        : "r"(tmem + (uint32_t)(buf * kLtMaxN)), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc), "r"(lead)
-                        : "memory");
-                    acc = 1u;
+                    for (int kk = 0; kk < kLtK / 16; ++kk) {
+                        asm volatile(
+                            "{\n\t.reg .pred p;\n\t"
+                            "setp.ne.b32 p, %4, 0;\n\t"
+                            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                            :
+                            : "r"(tmem + (uint32_t)(buf * kLtMaxN)), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc)
+                            : "memory");
+                        acc = 1u;
+                    }
+                    tc_commit(&s_a_empty[sa], 1u);
+                    tc_commit(&s_b_empty[sb], 1u);
+                    if (++sa == work.sa) sa = 0, pa ^= 1u;
+                    if (++sb == work.sb) sb = 0, pb ^= 1u;
                 }
-                tc_commit(&s_a_empty[sa], lead);
-                tc_commit(&s_b_empty[sb], lead);
-                if (++sa == work.sa) sa = 0, pa ^= 1u;
-                if (++sb == work.sb) sb = 0, pb ^= 1u;
-            }
-            if (ok && (++in == per_tile || n + 1 == lines)) {  // the end of a part of a tile
-                tc_commit(&s_acc_full[buf], lead);
-                in = 0, ++seg, acc = 0u;
+                if (ok && (++in == per_tile || n + 1 == lines)) {  // the end of a part of a tile
+                    tc_commit(&s_acc_full[buf], 1u);
+                    in = 0, ++seg, acc = 0u;
+                }
             }
         }
+        __syncwarp();
     } else if (warp == kLtTokens) {
         // ---- the B operand: 64 of K of the tile's tokens
-        int tile = tile0, in = in0, sb = 0;
-        uint32_t pb = 0;
-        bool ok = true;
-        for (int n = 0; ok && n < lines; ++n) {
-            const int t0 = (int)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
-            for (int j = 0; ok && j < kLtGroups; ++j) {
-                if (!(ok = warp_wait(&s_b_empty[sb], pb ^ 1u))) break;
-                if (lane == 0) tc_load_box(b_ring + (uint32_t)sb * b_stage, &token_map, &s_b_full[sb], b_stage, (in * kLtGroups + j) * kLtK, t0);
-                __syncwarp();
-                if (++sb == work.sb) sb = 0, pb ^= 1u;
+        if (tc_elect()) {
+            int tile = tile0, in = in0, sb = 0;
+            uint32_t pb = 0;
+            bool ok = true;
+            for (int n = 0; ok && n < lines; ++n) {
+                const int t0 = (int)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
+                for (int j = 0; j < kLtGroups; ++j) {
+                    if (!(ok = tc_wait(smem_u32(&s_b_empty[sb]), pb ^ 1u))) break;
+                    tc_load_box(b_ring + (uint32_t)sb * b_stage, &token_map, &s_b_full[sb], b_stage, (in * kLtGroups + j) * kLtK, t0);
+                    if (++sb == work.sb) sb = 0, pb ^= 1u;
+                }
+                if (++in == per_tile) in = 0, ++tile;
             }
-            if (++in == per_tile) in = 0, ++tile;
+            if (!ok) s_fail = 1;
         }
+        __syncwarp();
     } else if (warp == kLtCodes) {
         // ---- code lines
-        int tile = tile0, in = in0, line = 0;
-        uint32_t par = 0;
-        for (int n = 0; n < lines; ++n) {
-            if (!warp_wait(&s_line_empty[line], par ^ 1u)) break;
-            const int tm = (int)((uint32_t)tile / (uint32_t)work.tiles_n);
-            if (lane == 0)
+        if (tc_elect()) {
+            int tile = tile0, in = in0, line = 0;
+            uint32_t par = 0;
+            for (int n = 0; n < lines; ++n) {
+                if (!tc_wait(smem_u32(&s_line_empty[line]), par ^ 1u)) {
+                    s_fail = 1;
+                    break;
+                }
+                const int tm = (int)((uint32_t)tile / (uint32_t)work.tiles_n);
                 tc_load_box(code_ring + (uint32_t)line * kLtLineBytes, &code_map, &s_line_full[line], kLtLineBytes, BWD ? tm * 64 : in * 128, BWD ? in * 256 : tm * kLtM);
-            __syncwarp();
-            if (++line == work.sl) line = 0, par ^= 1u;
-            if (++in == per_tile) in = 0, ++tile;
+                if (++line == work.sl) line = 0, par ^= 1u;
+                if (++in == per_tile) in = 0, ++tile;
+            }
         }
+        __syncwarp();
     } else if (warp >= kLtResults) {
         // ---- results of the parts of tiles
         const int f = tid - kLtResults * 32, m = (warp & 3) * 32 + lane;

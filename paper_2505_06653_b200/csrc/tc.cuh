@@ -46,6 +46,27 @@ __device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity)
     return false;
 }
 
+// The same for a wait that has mostly come true already: a look without the offer to sleep first.
+__device__ __forceinline__ bool tc_wait_soon(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok || tc_wait(bar, parity);
+}
+// One lane of a converged warp, always the same one.
+__device__ __forceinline__ bool tc_elect()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0u;
+}
+
 // A block constant as it is in memory; widened where it is used, so that nothing waits for the load before.
 template <class ST>
 struct TcConst;
