@@ -23,11 +23,11 @@
 // parts to one CTA per SM; a tile that several CTAs share is summed in their order by the one that completes it last (a
 // ticket: nobody waits).  Warps with one job each, coupled by mbarriers:
 //
-//   16 producers  four groups of four warps, a k-block of the line each.  (Every line has four, so that a group is never
-//                 more than four k-blocks behind its next one: with four stages or more a barrier's parity is then
-//                 unambiguous.)
-//   1 issuer      four tcgen05.mma (M = 128, N = tokens, K = 16) per k-block, tcgen05.commit hands the stages back
-//   1 tokens, 1 codes   TMA loads of the B operand and of the code lines
+//   16 producers  four groups of four warps, a k-block of the line each, which always go to the same stages.  (Every line has
+//                 four k-blocks: groups that skipped some could get two turns of a stage apart, and a barrier's parity
+//                 would no longer say which.)
+//   1 issuer      four tcgen05.mma (M = 128, N = tokens, K = 16) per k-block, tcgen05.commit hands the stage back
+//   1 tokens, 1 codes   TMA loads of the B operand, and of half lines of codes (128 rows of 64 bytes in both directions)
 //   4 results     read a finished accumulator (there are two) while the next tile runs
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
@@ -41,16 +41,17 @@ constexpr int kLtGroups = 4;                 // producer groups, a k-block of a 
 constexpr int kLtM = 128, kLtK = 64;
 constexpr int kLtMaxN = 256;                 // tokens of a tile; columns of an accumulator
 constexpr int kLtABytes = kLtM * kLtK * 2;   // 16 KiB
-constexpr int kLtLineBytes = 16384;          // forward 128 rows x 128 bytes, backward 256 rows x 64 bytes
-constexpr int kLtMaxA = 6, kLtMaxB = 8, kLtMaxLines = 4;
-constexpr int kLtSmem = 214 * 1024;          // rings, with slack to align them to 1024 bytes
+constexpr int kLtHalfBytes = 8192;           // half a line of codes: two k-blocks; 128 rows x 64 bytes
+constexpr int kLtMaxStages = 8, kLtMaxHalves = 8;
+constexpr int kLtAhead = 6;                  // lines that L2 is asked for before the ring is
+constexpr int kLtSmem = 214 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
 constexpr int kLtIssue = 16, kLtTokens = 17, kLtCodes = 18, kLtResults = 20;  // warp 19 has no job: the results start at a multiple of 4
 constexpr int kLtThreads = 32 * (kLtResults + 4);
 
 struct LtWork {
     int tiles, tiles_n, per_tile;  // tiles, those along the tokens, lines of a tile
     int box_n;                     // tokens of a tile, a multiple of 16
-    int sa, sb, sl;                // stages of A, of B, code lines
+    int stages, halves;            // stages of A and B (4 or 8), half lines of codes (even)
     int each, extra;               // lines per CTA, and the remainder
     unsigned long long epoch;
     __host__ __device__ int start(int i) const { return i * each + (i < extra ? i : extra); }
@@ -99,8 +100,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                  unsigned char* __restrict__ ws, float* __restrict__ parts)
 {
     extern __shared__ unsigned char s_dyn[];
-    __shared__ __align__(8) unsigned long long s_a_full[kLtMaxA], s_a_empty[kLtMaxA], s_b_full[kLtMaxB], s_b_empty[kLtMaxB],
-        s_line_full[kLtMaxLines], s_line_empty[kLtMaxLines], s_acc_full[2], s_acc_empty[2];
+    __shared__ __align__(8) unsigned long long s_full[kLtMaxStages], s_empty[kLtMaxStages], s_half_full[kLtMaxHalves],
+        s_half_empty[kLtMaxHalves], s_acc_full[2], s_acc_empty[2];
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_sums, s_sum[2];
@@ -108,8 +109,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per_tile = work.per_tile, box_n = work.box_n;
     const uint32_t b_stage = (uint32_t)box_n * 128u;  // a multiple of 2048
-    const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)work.sa * kLtABytes;
-    const uint32_t b_ring = code_ring + (uint32_t)work.sl * kLtLineBytes;
+    const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)work.stages * kLtABytes;
+    const uint32_t b_ring = code_ring + (uint32_t)work.halves * kLtHalfBytes;
+    // line n of this CTA has stages turn(n) * 4 ... + 3, for the time(n)-th time
+    const int two = work.stages == 8 ? 1 : 0;
+    auto turn = [&](int n) { return n & two; };
+    auto time = [&](int n) { return (uint32_t)(n >> two) & 1u; };
     const int begin = work.start((int)blockIdx.x), finish = work.start((int)blockIdx.x + 1), lines = finish - begin;
     const int tile0 = (int)((uint32_t)begin / (uint32_t)per_tile), in0 = begin - tile0 * per_tile;
     const int segs = lines ? (in0 + lines - 1) / per_tile + 1 : 0;
@@ -124,9 +129,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     if (tid == 0) {
         if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
         s_fail = s_sums = 0;
-        for (int s = 0; s < work.sa; ++s) init(&s_a_full[s], 4), init(&s_a_empty[s], 1);
-        for (int s = 0; s < work.sb; ++s) init(&s_b_full[s], 1), init(&s_b_empty[s], 1);
-        for (int s = 0; s < work.sl; ++s) init(&s_line_full[s], 1), init(&s_line_empty[s], 4 * kLtGroups);
+        for (int s = 0; s < work.stages; ++s) init(&s_full[s], 4 + 1), init(&s_empty[s], 1);  // four warps of producers, and the tokens
+        for (int s = 0; s < work.halves; ++s) init(&s_half_full[s], 1), init(&s_half_empty[s], 8);
         for (int b = 0; b < 2; ++b) init(&s_acc_full[b], 1), init(&s_acc_empty[b], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -156,21 +160,20 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             if (ct * per_tile + ci + 1 < finish && ++ci == per_tile) ci = 0, ++ct;
         };
         if (lines) constants(c0, d0), constants(c1, d1), constants(c2, d2);
-        int line = 0, s = 0;
-        uint32_t line_par = 0, par = 0;
+        int slot = group >> 1;  // of the half line
+        uint32_t par = 0;
         for (int n = 0; n < lines; ++n) {
-            if (!warp_wait(&s_line_full[line], line_par)) break;
+            if (!warp_wait(&s_half_full[slot], par)) break;
             uint32_t w[8];
             {
-                const int r = BWD ? group * 64 + row : row;  // row of the line
-                const uint32_t at = code_ring + (uint32_t)line * kLtLineBytes + (uint32_t)r * (BWD ? 64u : 128u);
+                const int r = BWD ? (group & 1) * 64 + row : row, first = 2 * (BWD ? half : group & 1);  // row of the half line, its chunks
+                const uint32_t at = code_ring + (uint32_t)slot * kLtHalfBytes + (uint32_t)r * 64u;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int chunk = BWD ? (2 * half + h) ^ ((r >> 1) & 3) : (2 * group + h) ^ (r & 7);
+                for (int h = 0; h < 2; ++h)
                     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
-                                 : "r"(at + (uint32_t)chunk * 16u));
-                }
+                                 : "r"(at + (uint32_t)((first + h) ^ ((r >> 1) & 3)) * 16u)
+                                 : "memory");
             }
             const float m = c0.value(), m2 = HALF ? d0.value() : m;
             c0 = c1, c1 = c2;
@@ -182,10 +185,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             lt_table(m, s_levels, lo, hi);
 #pragma unroll
             for (int j = 0; j < 4; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
-            int st = s + group;
-            uint32_t p = par;
-            if (st >= work.sa) st -= work.sa, p ^= 1u;
-            if (!warp_wait(&s_a_empty[st], p ^ 1u)) break;
+            const int st = turn(n) * kLtGroups + group;
+            if (!warp_wait(&s_empty[st], time(n) ^ 1u)) break;
             const uint32_t at = a_ring + (uint32_t)st * kLtABytes + (uint32_t)thread * 128u, x = (uint32_t)(thread & 7);
             auto store = [&](int j, const uint32_t* q) {
                 asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((uint32_t)j ^ x) << 4)), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
@@ -211,37 +212,43 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) {
-                tc_arrive(&s_line_empty[line]);
-                tc_arrive(&s_a_full[st]);
-            }
-            if ((s += kLtGroups) >= work.sa) s -= work.sa, par ^= 1u;
-            if (++line == work.sl) line = 0, line_par ^= 1u;
+            // (the codes are given back once all of them have been used: given back when only their loads had been issued, slow
+            // memory let the next half line overtake them)
+            if (lane == 0) tc_arrive(&s_half_empty[slot]), tc_arrive(&s_full[st]);
+            if ((slot += 2) >= work.halves) slot = group >> 1, par ^= 1u;
             if (++in == per_tile) in = 0, ++tile;
         }
     } else if (warp == kLtIssue) {
         // ---- the issuing warp: one lane does it all (with the other lanes in step, their instructions predicated off, a
         // k-block took 500 cycles to issue)
         if (tc_elect()) {
-            auto wait = [&](unsigned long long* bar, uint32_t parity) -> bool {
-                if (tc_wait_soon(smem_u32(bar), parity)) return true;
+            auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+                if (tc_wait(bar, parity)) return true;
                 s_fail = 1;
                 return false;
             };
             const uint64_t da0 = tc_smem_desc(a_ring, BWD ? 8192u : 16u), db0 = tc_smem_desc(b_ring);
+            const uint32_t full0 = smem_u32(s_full);
             // fp32 accumulator, bf16 x bf16, A M-major (backward) or K-major, B K-major, M = 128, N
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (BWD ? 1u << 15 : 0u) | ((uint32_t)(box_n >> 3) << 17) | ((uint32_t)(kLtM >> 4) << 24);
             constexpr uint64_t a_step = BWD ? 2048 >> 4 : 32 >> 4;  // 16 of K
-            int in = in0, seg = 0, sa = 0, sb = 0;
-            uint32_t acc = 0u, pa = 0, pb = 0;
+            int in = in0, seg = 0;
+            uint32_t acc = 0u;
             bool ok = true;
-            for (int n = 0; ok && n < lines; ++n) {
-                const int buf = seg & 1;
-                if (acc == 0u && !(ok = wait(&s_acc_empty[buf], (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
+            for (int n = 0; n < lines; ++n) {
+                const uint32_t d = tmem + (uint32_t)((seg & 1) * kLtMaxN), par = time(n);
+                const int s0 = turn(n) * kLtGroups;
+                if (acc == 0u && !(ok = wait(smem_u32(&s_acc_empty[seg & 1]), (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
+                // a look at all four stages first: mostly they are full, and the looks overlap
+                bool ready[kLtGroups];
+#pragma unroll
+                for (int j = 0; j < kLtGroups; ++j) ready[j] = tc_look(full0 + 8u * (uint32_t)(s0 + j), par);
+#pragma unroll
                 for (int j = 0; j < kLtGroups; ++j) {
-                    if (!(ok = wait(&s_b_full[sb], pb) && wait(&s_a_full[sa], pa))) break;
+                    const int st = s0 + j;
+                    if (!ready[j] && !(ok = wait(full0 + 8u * (uint32_t)st, par))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = da0 + (uint64_t)(sa * (kLtABytes >> 4)), db = db0 + (uint64_t)(sb * (b_stage >> 4));
+                    const uint64_t da = da0 + (uint64_t)(st * (kLtABytes >> 4)), db = db0 + (uint64_t)(st * (b_stage >> 4));
 #pragma unroll
                     for (int kk = 0; kk < kLtK / 16; ++kk) {
                         asm volatile(
@@ -249,17 +256,15 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                             "setp.ne.b32 p, %4, 0;\n\t"
                             "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                             :
-                            : "r"(tmem + (uint32_t)(buf * kLtMaxN)), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc)
+                            : "r"(d), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc)
                             : "memory");
                         acc = 1u;
                     }
-                    tc_commit(&s_a_empty[sa], 1u);
-                    tc_commit(&s_b_empty[sb], 1u);
-                    if (++sa == work.sa) sa = 0, pa ^= 1u;
-                    if (++sb == work.sb) sb = 0, pb ^= 1u;
+                    tc_commit(&s_empty[st], 1u);
                 }
-                if (ok && (++in == per_tile || n + 1 == lines)) {  // the end of a part of a tile
-                    tc_commit(&s_acc_full[buf], 1u);
+                if (!ok) break;
+                if (++in == per_tile || n + 1 == lines) {  // the end of a part of a tile
+                    tc_commit(&s_acc_full[seg & 1], 1u);
                     in = 0, ++seg, acc = 0u;
                 }
             }
@@ -268,15 +273,14 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     } else if (warp == kLtTokens) {
         // ---- the B operand: 64 of K of the tile's tokens
         if (tc_elect()) {
-            int tile = tile0, in = in0, sb = 0;
-            uint32_t pb = 0;
+            int tile = tile0, in = in0;
             bool ok = true;
             for (int n = 0; ok && n < lines; ++n) {
                 const int t0 = (int)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
                 for (int j = 0; j < kLtGroups; ++j) {
-                    if (!(ok = tc_wait(smem_u32(&s_b_empty[sb]), pb ^ 1u))) break;
-                    tc_load_box(b_ring + (uint32_t)sb * b_stage, &token_map, &s_b_full[sb], b_stage, (in * kLtGroups + j) * kLtK, t0);
-                    if (++sb == work.sb) sb = 0, pb ^= 1u;
+                    const int st = turn(n) * kLtGroups + j;
+                    if (!(ok = tc_wait(smem_u32(&s_empty[st]), time(n) ^ 1u))) break;
+                    tc_load_box(b_ring + (uint32_t)st * b_stage, &token_map, &s_full[st], b_stage, (in * kLtGroups + j) * kLtK, t0);
                 }
                 if (++in == per_tile) in = 0, ++tile;
             }
@@ -284,20 +288,32 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         }
         __syncwarp();
     } else if (warp == kLtCodes) {
-        // ---- code lines
+        // ---- codes: half h of line `in` of a tile, brought into L2 kLtAhead lines before
         if (tc_elect()) {
-            int tile = tile0, in = in0, line = 0;
+            int tile = tile0, in = in0, slot = 0, pt = tile0, pi = in0;
             uint32_t par = 0;
-            for (int n = 0; n < lines; ++n) {
-                if (!tc_wait(smem_u32(&s_line_empty[line]), par ^ 1u)) {
-                    s_fail = 1;
-                    break;
+            bool ok = true;
+            auto x_of = [&](int t, int i, int h) { return BWD ? (int)((uint32_t)t / (uint32_t)work.tiles_n) * 64 : i * 128 + h * 64; };
+            auto y_of = [&](int t, int i, int h) { return BWD ? i * 256 + h * 128 : (int)((uint32_t)t / (uint32_t)work.tiles_n) * kLtM; };
+            for (int n = 0; n < kLtAhead; ++n)
+                if (++pi == per_tile) pi = 0, ++pt;
+            for (int n = 0; ok && n < lines; ++n) {
+                if (n + kLtAhead < lines) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&code_map)),
+                                     "r"(x_of(pt, pi, h)), "r"(y_of(pt, pi, h))
+                                     : "memory");
+                    if (++pi == per_tile) pi = 0, ++pt;
                 }
-                const int tm = (int)((uint32_t)tile / (uint32_t)work.tiles_n);
-                tc_load_box(code_ring + (uint32_t)line * kLtLineBytes, &code_map, &s_line_full[line], kLtLineBytes, BWD ? tm * 64 : in * 128, BWD ? in * 256 : tm * kLtM);
-                if (++line == work.sl) line = 0, par ^= 1u;
+                for (int h = 0; h < 2; ++h) {
+                    if (!(ok = tc_wait(smem_u32(&s_half_empty[slot]), par ^ 1u))) break;
+                    tc_load_box(code_ring + (uint32_t)slot * kLtHalfBytes, &code_map, &s_half_full[slot], kLtHalfBytes, x_of(tile, in, h), y_of(tile, in, h));
+                    if (++slot == work.halves) slot = 0, par ^= 1u;
+                }
                 if (++in == per_tile) in = 0, ++tile;
             }
+            if (!ok) s_fail = 1;
         }
         __syncwarp();
     } else if (warp >= kLtResults) {
@@ -425,10 +441,11 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t 
     w.tiles_n = (int)tiles_n;
     w.per_tile = (int)per_tile;
     w.box_n = (int)box;
-    w.sl = box > 128 ? 3 : 4;
-    w.sa = box > 128 ? 4 : 6;
-    w.sb = (int)((kLtSmem - 1024 - w.sl * kLtLineBytes - w.sa * kLtABytes) / (box * 128));
-    if (w.sb > kLtMaxB) w.sb = kLtMaxB;
+    // Eight stages where they leave room for a line of codes, two lines or more beside four otherwise; 256 tokens leave one.
+    const int room = kLtSmem - 1024, stage = kLtABytes + (int)box * 128;
+    w.stages = room - 8 * stage >= 2 * kLtHalfBytes ? 8 : 4;
+    w.halves = (room - w.stages * stage) / kLtHalfBytes & ~1;
+    if (w.halves > kLtMaxHalves) w.halves = kLtMaxHalves;
     // One CTA per SM, each with an equal part of the lines.  A tile is cut into at most so many parts that summing them
     // stays short beside the product: 16384 / tokens.
     const int64_t lines = tiles * per_tile, most = tiles * (16384 / box < 64 ? 16384 / box : 64);
@@ -471,7 +488,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
     p.work.epoch = tc_next_epoch();
     CUtensorMap code_map, token_map;
     int rc;
-    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, backward ? 64 : 128, backward ? 256 : kLtM, &code_map)) ||
+    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 64, kLtM, &code_map)) ||
         (rc = tc_make_map(who, operand, 2, backward ? w.rows : w.cols, out.tokens, ld * 2, 128, p.work.box_n, &token_map)))
         return rc;
     int* heads = nullptr;

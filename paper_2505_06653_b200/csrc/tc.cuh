@@ -46,8 +46,8 @@ __device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity)
     return false;
 }
 
-// The same for a wait that has mostly come true already: a look without the offer to sleep first.
-__device__ __forceinline__ bool tc_wait_soon(uint32_t bar, uint32_t parity)
+// A look at a barrier, without a wait.
+__device__ __forceinline__ bool tc_look(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
     asm volatile(
@@ -57,7 +57,7 @@ __device__ __forceinline__ bool tc_wait_soon(uint32_t bar, uint32_t parity)
         : "=r"(ok)
         : "r"(bar), "r"(parity)
         : "memory");
-    return ok || tc_wait(bar, parity);
+    return ok != 0u;
 }
 // One lane of a converged warp, always the same one.
 __device__ __forceinline__ bool tc_elect()

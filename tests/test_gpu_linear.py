@@ -355,6 +355,26 @@ def test_same_bits_again_on_other_streams_and_in_graphs(bof4):
             assert torch.equal(oy, y) and torch.equal(odx, dx)
 
 
+@pytest.mark.parametrize("tokens,rows,cols", [(3, 5000, 8192), (14, 2560, 4096), (40, 5000, 8192), (100, 5120, 8192), (250, 2560, 4096)])
+def test_cold_memory(bof4, tokens, rows, cols):
+    """Inputs that have left L2 arrive late and in another order: the same results, with any contents of the workspace."""
+    lv, codes, scales = integer_case(rows, cols, 64, rows + cols)
+    g = torch.Generator().manual_seed(tokens)
+    dy, x = ints(g, tokens, rows), ints(g, tokens, cols)
+    w = decode(codes, scales, 64, lv, rows, cols)
+    rb, rf = (dy.double() @ w).bfloat16(), (x.double() @ w.T).float()
+    big = torch.empty(300 << 20, dtype=torch.uint8, device="cuda")
+    n = max(bof4.bof4_linear_workspace_bytes(rows, cols, tokens, k) for k in (False, True))
+    for trial in range(12):
+        ws = torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda")
+        big.fill_(trial)
+        dx, _, s = bof4.bof4_linear_backward(codes, scales, rows, cols, 64, lv, dy, workspace=ws)
+        assert int(s.item()) == 0 and torch.equal(dx, rb)
+        big.fill_(trial)
+        y, s = bof4.bof4_linear(codes, scales, rows, cols, 64, lv, x, out_dtype=bof4.F32, workspace=ws)
+        assert int(s.item()) == 0 and torch.equal(y, rf)
+
+
 def test_random_shapes_are_exact(bof4):
     rng = np.random.default_rng(11)
     for trial in range(60):
