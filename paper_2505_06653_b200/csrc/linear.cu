@@ -241,6 +241,7 @@ extern "C" int bof4_linear(const uint8_t* d_codes, const void* d_scales, int sca
     out.act = activation;
     out.n = rows;
     out.tokens = n_tokens;
+    out.set_alignment();
     if (cols == 0) {
         const int64_t want = (rows * n_tokens + 255) / 256;
         launch_after(linear_empty_kernel, (int)(want < 8 * kSMs ? want : 8 * kSMs), 256, 0, st, out, d_status);
@@ -337,5 +338,6 @@ extern "C" int bof4_linear_backward(const uint8_t* d_codes, const void* d_scales
     out.act = BOF4_ACT_NONE;
     out.n = cols;
     out.tokens = n_tokens;
+    out.set_alignment();
     return linear_tc(fn, w, true, direct ? d_dy : dz, direct ? ld_dy : plan.ld, out, d_status, d_ws, need_product, st);
 }

@@ -26,6 +26,37 @@ __device__ __forceinline__ float activate(float z, int act)
         default: return z;
     }
 }
+// The same for several values: one branch for all of them.
+template <int N>
+__device__ __forceinline__ void activate_all(float (&z)[N], int act)
+{
+    switch (act) {
+        case BOF4_ACT_RELU:
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = activate(z[k], BOF4_ACT_RELU);
+            break;
+        case BOF4_ACT_GELU:
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = activate(z[k], BOF4_ACT_GELU);
+            break;
+        case BOF4_ACT_GELU_TANH:
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = activate(z[k], BOF4_ACT_GELU_TANH);
+            break;
+        case BOF4_ACT_SILU:
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = activate(z[k], BOF4_ACT_SILU);
+            break;
+        default: break;
+    }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 // act'(z) in fp32; far out, where the products below would be 0 * inf, the limits 0 and 1.
 __device__ __forceinline__ float activate_slope(float z, int act)
 {
@@ -59,6 +90,15 @@ struct LinearOut {
     int64_t ld_residual, ld_pre, ldy, n, tokens;
     int act;
     bool bias_bf16, y_bf16;
+    // rows of y, residual and pre begin at addresses that hold pairs of bf16 values / 16 bytes of their type
+    bool pairs, wide;
+    void set_alignment()
+    {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(residual) | reinterpret_cast<uintptr_t>(pre);
+        const int64_t l = tokens > 1 ? ldy | (residual ? ld_residual : 0) | (pre ? ld_pre : 0) : 0;
+        pairs = (a & 3u) == 0 && (l & 1) == 0;
+        wide = (a & 15u) == 0 && (l & 7) == 0;
+    }
     __device__ __forceinline__ float bias_at(int64_t o) const
     {
         if (!bias) return 0.0f;
@@ -78,6 +118,51 @@ struct LinearOut {
         const float v = activate(z, act) + r;
         if (y_bf16) static_cast<uint16_t*>(y)[t * ldy + o] = bf16_round(v);
         else static_cast<float*>(y)[t * ldy + o] = v;
+    }
+};
+
+// Sums of four neighbouring rows o ... o + 3 (o a multiple of four) of a token: residual (loaded before), bias, store.
+struct LinearFour {
+    float r[4];
+    __device__ __forceinline__ void residual(const LinearOut& out, int64_t t, int64_t o)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = 0.0f;
+        if (!out.residual) return;
+        const int64_t i = t * out.ld_residual + o;
+        if (out.wide && o + 3 < out.n) {
+            if (out.y_bf16) {
+                const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(out.residual) + i);
+                r[0] = __uint_as_float(u.x << 16), r[1] = __uint_as_float(u.x & 0xffff0000u), r[2] = __uint_as_float(u.y << 16), r[3] = __uint_as_float(u.y & 0xffff0000u);
+            } else {
+                const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(out.residual) + i);
+                r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (o + k < out.n) r[k] = out.residual_at(t, o + k);
+        }
+    }
+    __device__ __forceinline__ void store(const LinearOut& out, const float4& sum, int64_t t, int64_t o) const
+    {
+        float z[4] = {sum.x, sum.y, sum.z, sum.w};
+        if (out.bias) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] += o + k < out.n ? out.bias_at(o + k) : 0.0f;
+        }
+        if (!(out.wide && o + 3 < out.n)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (o + k < out.n) out.store(z[k], 0.0f, r[k], t, o + k);
+            return;
+        }
+        if (out.pre) *reinterpret_cast<uint2*>(out.pre + t * out.ld_pre + o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
+        activate_all(z, out.act);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] += r[k];
+        if (out.y_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out.y) + t * out.ldy + o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
+        else *reinterpret_cast<float4*>(static_cast<float*>(out.y) + t * out.ldy + o) = make_float4(z[0], z[1], z[2], z[3]);
     }
 };
 

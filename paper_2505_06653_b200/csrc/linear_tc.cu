@@ -92,6 +92,79 @@ linear_outlier_lists(const int32_t* __restrict__ idx, const uint16_t* __restrict
     }
 }
 
+// Sixteen tokens (the first `count` of them) of a finished accumulator: row o of the output in each lane.  Of bf16 values, the
+// lanes of a pair exchange one for every two tokens, so that each stores two rows of a token; their residual is read the same way.
+__device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, float b, int64_t t0, int count, int64_t o, bool live, int lane)
+{
+    uint32_t a[16];
+    __syncwarp();
+    lt_load16(src, a);
+    const bool odd = lane & 1, both = (o | 1) < out.n, one = (o & ~(int64_t)1) < out.n;  // the pair's two rows exist, its first
+    const bool paired = out.y_bf16 && out.pairs && count >= 16;
+    float r[16];
+    if (paired) {
+        const int64_t first = (t0 + odd) * out.ld_residual + (o & ~(int64_t)1);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            uint32_t u = 0u;
+            if (out.residual && one) {
+                const uint16_t* p = static_cast<const uint16_t*>(out.residual) + first + 2 * k * out.ld_residual;
+                u = both ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)*p;
+            }
+            r[2 * k] = __uint_as_float(u << 16), r[2 * k + 1] = __uint_as_float(u & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) r[k] = live && k < count ? out.residual_at(t0 + k, o) : 0.0f;
+    }
+    __syncwarp();
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    float z[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z[k] = __uint_as_float(a[k]) + b;
+    // rows (o & ~1, + 1) of tokens 2 k + odd
+    auto exchange = [&](float (&v)[16], auto&& use) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float other = __shfl_xor_sync(kFull, odd ? v[2 * k] : v[2 * k + 1], 1);
+            use(k, odd ? other : v[2 * k], odd ? v[2 * k + 1] : other);
+        }
+    };
+    auto put = [&](uint16_t* p, uint32_t u) {
+        if (both) *reinterpret_cast<uint32_t*>(p) = u;
+        else *p = (uint16_t)u;
+    };
+    if (paired) {
+        const int64_t even = o & ~(int64_t)1;
+        if (out.pre) {
+            uint16_t* p = out.pre + (t0 + odd) * out.ld_pre + even;
+            exchange(z, [&](int k, float x, float y) {
+                if (one) put(p + 2 * k * out.ld_pre, bf16_pair(x, y));
+            });
+        }
+        activate_all(z, out.act);
+        uint16_t* p = static_cast<uint16_t*>(out.y) + (t0 + odd) * out.ldy + even;
+        exchange(z, [&](int k, float x, float y) {
+            if (one) put(p + 2 * k * out.ldy, bf16_pair(x + r[2 * k], y + r[2 * k + 1]));
+        });
+        return;
+    }
+    if (out.pre) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (live && k < count) out.pre[(t0 + k) * out.ld_pre + o] = bf16_round(z[k]);
+    }
+    activate_all(z, out.act);
+    const int64_t at = t0 * out.ldy + o;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        if (!live || k >= count) continue;
+        const float v = z[k] + r[k];
+        if (out.y_bf16) static_cast<uint16_t*>(out.y)[at + k * out.ldy] = bf16_round(v);
+        else static_cast<float*>(out.y)[at + k * out.ldy] = v;
+    }
+}
+
 template <bool BWD, class ST, bool HALF, bool OPQ>  // HALF: blocks of 32 weights, two constants per thread and k-block
 __global__ void __launch_bounds__(kLtThreads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap token_map, const void* __restrict__ scales,
@@ -340,27 +413,18 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             const bool all = begin <= t0 && finish >= t0 + per_tile, live = o < out.n;
             const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * kLtMaxN);
             float* const part = parts + (2 * (int64_t)blockIdx.x + (begin <= t0 ? 1 : 0)) * kLtM * box_n;
-            const float b = all && live ? out.bias_at(o) : 0.0f;
-            for (int q = 0; q < count; q += 16) {
-                uint32_t a[16];
-                __syncwarp();
-                lt_load16(src + (uint32_t)q, a);
-                float r[16];
-                if (all && live) {
+            if (!all) {
+                float* to = part + m;
+                for (int q = 0; q < count; q += 16, to += 16 * kLtM) {
+                    uint32_t a[16];
+                    lt_load16(src + (uint32_t)q, a);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) r[k] = q + k < count ? out.residual_at(token0 + q + k, o) : 0.0f;
+                    for (int k = 0; k < 16; ++k) to[k * kLtM] = __uint_as_float(a[k]);  // (count is padded to 16 in the workspace)
                 }
-                __syncwarp();
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if (!all) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (q + k < count) part[(q + k) * kLtM + m] = __uint_as_float(a[k]);
-                } else if (live) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (q + k < count) out.store(__uint_as_float(a[k]), b, r[k], token0 + q + k, o);
-                }
+            } else {
+                const float b = live ? out.bias_at(o) : 0.0f;
+                for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, b, token0 + q, count - q, o, live, lane);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -393,20 +457,37 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         __threadfence();
         const float4* head = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + (work.start(i0) <= t0 ? 1 : 0)) * slab;
         const float4* next = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + 2) * slab;
-        for (int e = tid; e < count * (kLtM / 4); e += kLtThreads) {
-            float4 sum = __ldcg(head + e);
-            for (int i = 0; i < more; i += 4) {
-                float4 v[4];
+        constexpr int B = 3;  // quads of rows of a thread at a time
+        for (int e0 = tid; e0 < count * (kLtM / 4); e0 += B * kLtThreads) {
+            float4 sum[B];
+            LinearFour four[B];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = i + u < more ? __ldcg(next + (int64_t)(2 * (i + u)) * slab + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
+            for (int u = 0; u < B; ++u) {
+                const int e = e0 + u * kLtThreads;
+                const bool on = e < count * (kLtM / 4);
+                sum[u] = on ? __ldcg(head + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (on && o0 + (e & 31) * 4 < out.n) four[u].residual(out, token0 + (e >> 5), o0 + (e & 31) * 4);
             }
-            const float z[4] = {sum.x, sum.y, sum.z, sum.w};
-            const int64_t o = o0 + (e & 31) * 4, t = token0 + (e >> 5);
+            for (int i = 0; i < more; i += 2) {
+                float4 v[2][B];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (o + u < out.n) out.store(z[u], out.bias_at(o + u), out.residual_at(t, o + u), t, o + u);
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int u = 0; u < B; ++u) {
+                        const int e = e0 + u * kLtThreads;
+                        v[w][u] = i + w < more && e < count * (kLtM / 4) ? __ldcg(next + (int64_t)(2 * (i + w)) * slab + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int u = 0; u < B; ++u) sum[u].x += v[w][u].x, sum[u].y += v[w][u].y, sum[u].z += v[w][u].z, sum[u].w += v[w][u].w;
+            }
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const int e = e0 + u * kLtThreads;
+                const int64_t o = o0 + (e & 31) * 4;
+                if (e < count * (kLtM / 4) && o < out.n) four[u].store(out, sum[u], token0 + (e >> 5), o);
+            }
         }
     }
     if (warp == kLtIssue)
