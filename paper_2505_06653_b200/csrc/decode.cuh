@@ -20,6 +20,13 @@ __device__ __forceinline__ void tc_lookup8(uint32_t w, float2 mm, uint32_t pairs
     }
 }
 
+// The instruction itself: the intrinsic masks a selector that is not a constant, at the price of another instruction each time.
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
+    return r;
+}
 // Eight products by byte permutes.  lo[0..1], hi[0..1]: bytes of entries 0 ... 7, lo[2..3], hi[2..3]: of 8 ... 15.
 __device__ __forceinline__ void lt_lookup8(uint32_t w, const uint32_t (&lo)[4], const uint32_t (&hi)[4], uint32_t* o)
 {
@@ -28,10 +35,10 @@ __device__ __forceinline__ void lt_lookup8(uint32_t w, const uint32_t (&lo)[4], 
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         // result bytes: elements 1, 0, 3, 2 (the even element of a byte is its high nibble)
-        const uint32_t l = __byte_perm(__byte_perm(lo[0], lo[1], s), __byte_perm(lo[2], lo[3], s), t);
-        const uint32_t u = __byte_perm(__byte_perm(hi[0], hi[1], s), __byte_perm(hi[2], hi[3], s), t);
-        o[2 * h] = __byte_perm(l, u, 0x4051);
-        o[2 * h + 1] = __byte_perm(l, u, 0x6273);
+        const uint32_t l = prmt(prmt(lo[0], lo[1], s), prmt(lo[2], lo[3], s), t);
+        const uint32_t u = prmt(prmt(hi[0], hi[1], s), prmt(hi[2], hi[3], s), t);
+        o[2 * h] = prmt(l, u, 0x4051);
+        o[2 * h + 1] = prmt(l, u, 0x6273);
         s >>= 16, t >>= 16;
     }
 }

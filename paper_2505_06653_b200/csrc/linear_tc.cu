@@ -43,8 +43,9 @@ constexpr int kLtMaxN = 256;                 // tokens of a tile; columns of an 
 constexpr int kLtABytes = kLtM * kLtK * 2;   // 16 KiB
 constexpr int kLtHalfBytes = 8192;           // half a line of codes: two k-blocks; 128 rows x 64 bytes
 constexpr int kLtMaxStages = 8, kLtMaxHalves = 8;
+constexpr int kLtTableN = 64;                // tokens of a tile up to which there is room, and use, for the table of pairs
 constexpr int kLtAhead = 6;                  // lines that L2 is asked for before the ring is
-constexpr int kLtSmem = 214 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
+constexpr int kLtSmem = 225 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
 constexpr int kLtIssue = 16, kLtTokens = 17, kLtCodes = 18, kLtResults = 20;  // warp 19 has no job: the results start at a multiple of 4
 constexpr int kLtThreads = 32 * (kLtResults + 4);
 
@@ -53,6 +54,7 @@ struct LtWork {
     int box_n;                     // tokens of a tile, a multiple of 16
     int stages, halves;            // stages of A and B (4 or 8), half lines of codes (even)
     int each, extra;               // lines per CTA, and the remainder
+    bool table;                    // half of the codes go through a table
     unsigned long long epoch;
     __host__ __device__ int start(int i) const { return i * each + (i < extra ? i : extra); }
     __device__ int owner(int l) const
@@ -165,7 +167,8 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, fl
     }
 }
 
-template <bool BWD, class ST, bool HALF, bool OPQ>  // HALF: blocks of 32 weights, two constants per thread and k-block
+// HALF: blocks of 32 weights, two constants per thread and k-block.  LUT: half of the codes are looked up in a table of pairs.
+template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT>
 __global__ void __launch_bounds__(kLtThreads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap token_map, const void* __restrict__ scales,
                  int64_t cols, int block_shift, int64_t last_scale, const float* __restrict__ levels, const LinearOut out,
@@ -184,6 +187,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     const uint32_t b_stage = (uint32_t)box_n * 128u;  // a multiple of 2048
     const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)work.stages * kLtABytes;
     const uint32_t b_ring = code_ring + (uint32_t)work.halves * kLtHalfBytes;
+    const uint32_t pairs = b_ring + (uint32_t)work.stages * b_stage;
     // line n of this CTA has stages turn(n) * 4 ... + 3, for the time(n)-th time
     const int two = work.stages == 8 ? 1 : 0;
     auto turn = [&](int n) { return n & two; };
@@ -212,6 +216,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(2 * kLtMaxN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (LUT && warp < kLtIssue) fill_pairs(reinterpret_cast<float2*>(s_dyn + (pairs - smem_u32(s_dyn))), levels, tid, kLtIssue * 32);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -221,64 +226,83 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         // ---- producers
         const int group = warp >> 2, thread = (warp & 3) * 32 + lane;
         const int row = BWD ? thread & 63 : thread, half = BWD ? thread >> 6 : 0;  // of W within the k-block (backward), the tile (forward)
-        int tile = tile0, in = in0, ct = tile0, ci = in0;
-        // block constants three lines ahead (past the end: the last ones again; outside the matrix: its last one)
+        // Block constants, three lines ahead (past the end: the last ones again; outside the matrix: its last one): the index of the
+        // thread's first weight of a line, and what a line further adds to it.
         TcConst<ST> c0, c1, c2, d0, d1, d2;
+        int ct = tile0, ci = in0, unasked = lines;
+        auto first_of = [&](int t, int i) -> int64_t {
+            const int64_t tm = (uint32_t)t / (uint32_t)work.tiles_n, k = (int64_t)i * kLtGroups + group;
+            return BWD ? (k * kLtK + row) * cols + tm * kLtM + half * 64 : (tm * kLtM + row) * cols + k * kLtK;
+        };
+        int64_t weight = first_of(ct, ci);
+        const int64_t line_step = BWD ? (int64_t)kLtGroups * kLtK * cols : kLtGroups * kLtK;
         auto constants = [&](TcConst<ST>& c, TcConst<ST>& d) {
-            const int64_t tm = (uint32_t)ct / (uint32_t)work.tiles_n, k = (int64_t)ci * kLtGroups + group;
-            const int64_t i = BWD ? (k * kLtK + row) * cols + tm * kLtM + half * 64 : (tm * kLtM + row) * cols + k * kLtK;
-            const int64_t b = i >> block_shift;
+            const int64_t b = weight >> block_shift;
             c.load(scales, b < last_scale ? b : last_scale);
             if (HALF) d.load(scales, b + 1 < last_scale ? b + 1 : last_scale);
-            if (ct * per_tile + ci + 1 < finish && ++ci == per_tile) ci = 0, ++ct;
+            if (--unasked <= 0) return;
+            weight += line_step;
+            if (++ci == per_tile) ci = 0, ++ct, weight = first_of(ct, 0);
         };
         if (lines) constants(c0, d0), constants(c1, d1), constants(c2, d2);
+        const int* head_at = nullptr;  // OPQ: the list of the warp's part of a line's k-block, 4 * kLtGroups places further for the next line
+        int in = in0, tile = tile0;
+        auto head_of = [&] { return heads + (((int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * per_tile + in) * kLtGroups + group) * 4 + (warp & 3); };
+        if (OPQ && lines) head_at = head_of();
+        // the thread's 32 bytes of a half line: two chunks of its row (64-byte swizzle); its row of the A tile (128-byte swizzle)
+        const int r = BWD ? (group & 1) * 64 + row : row, chunk = (2 * (BWD ? half : group & 1)) ^ ((r >> 1) & 3);
+        const uint32_t code0 = code_ring + (uint32_t)(r * 64 + chunk * 16), code1 = code_ring + (uint32_t)(r * 64 + (chunk ^ 1) * 16);
+        const uint32_t tile_at = a_ring + (uint32_t)group * kLtABytes + (uint32_t)(thread * 128 + (thread & 7) * 16);
+        const uint32_t full0 = smem_u32(&s_full[group]), empty0 = smem_u32(&s_empty[group]);
         int slot = group >> 1;  // of the half line
         uint32_t par = 0;
         for (int n = 0; n < lines; ++n) {
             if (!warp_wait(&s_half_full[slot], par)) break;
             uint32_t w[8];
-            {
-                const int r = BWD ? (group & 1) * 64 + row : row, first = 2 * (BWD ? half : group & 1);  // row of the half line, its chunks
-                const uint32_t at = code_ring + (uint32_t)slot * kLtHalfBytes + (uint32_t)r * 64u;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
-                                 : "r"(at + (uint32_t)((first + h) ^ ((r >> 1) & 3)) * 16u)
-                                 : "memory");
-            }
+            const uint32_t codes = (uint32_t)slot * kLtHalfBytes;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(code0 + codes) : "memory");
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(code1 + codes) : "memory");
             const float m = c0.value(), m2 = HALF ? d0.value() : m;
             c0 = c1, c1 = c2;
             if (HALF) d0 = d1, d1 = d2;
             constants(c2, d2);
             int head = -1;
-            if (OPQ) head = __ldg(heads + (((int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * per_tile + in) * kLtGroups + group) * 4 + (warp & 3));
-            uint32_t lo[4], hi[4], v[16];
-            lt_table(m, s_levels, lo, hi);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
-            const int st = turn(n) * kLtGroups + group;
-            if (!warp_wait(&s_empty[st], time(n) ^ 1u)) break;
-            const uint32_t at = a_ring + (uint32_t)st * kLtABytes + (uint32_t)thread * 128u, x = (uint32_t)(thread & 7);
-            auto store = [&](int j, const uint32_t* q) {
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((uint32_t)j ^ x) << 4)), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
-            };
-#pragma unroll
-            for (int j = 0; j < 4; ++j) store(j, v + 4 * j);
-            if (HALF) lt_table(m2, s_levels, lo, hi);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                lt_lookup8(w[4 + j], lo, hi, v + 4 * j);
-                store(4 + j, v + 4 * j);
+            if (OPQ) {
+                head = __ldg(head_at);
+                head_at += 4 * kLtGroups;
+                if (++in == per_tile) {
+                    in = 0, ++tile;
+                    if (n + 1 < lines) head_at = head_of();
+                }
             }
+            // everything is decoded before the wait: what lies between a stage's release and its next use is the pipeline's slack
+            uint32_t lo[4], hi[4], v[32];
+            lt_table(LUT ? m2 : m, s_levels, lo, hi);
+            if (LUT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) tc_lookup8(w[j], make_float2(m, m), pairs, (uint32_t)lane * 8u, v + 4 * j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
+                if (HALF) lt_table(m2, s_levels, lo, hi);
+            }
+#pragma unroll
+            for (int j = 4; j < 8; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
+            const uint32_t st = (uint32_t)(turn(n) * kLtGroups), at = tile_at + st * kLtABytes;
+            if (!__all_sync(kFull, tc_wait(empty0 + 8u * st, time(n) ^ 1u))) {
+                if (lane == 0) s_fail = 1;
+                break;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at ^ (uint32_t)(j << 4)), "r"(v[4 * j]), "r"(v[4 * j + 1]), "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
             if (OPQ) {
                 while (head >= 0) {  // the same list for all lanes; a lane patches its own row
                     const int2 e = __ldg(nodes + head);
                     const uint32_t place = (uint32_t)e.y >> 16;
                     if ((int)(place >> 6) == lane) {
                         const uint32_t c = place & 63u;
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + (((c >> 3) ^ x) << 4) + (c & 7u) * 2u), "h"((uint16_t)e.y) : "memory");
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"((at ^ ((c >> 3) << 4)) + (c & 7u) * 2u), "h"((uint16_t)e.y) : "memory");
                     }
                     head = e.x;
                 }
@@ -287,9 +311,11 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             __syncwarp();
             // (the codes are given back once all of them have been used: given back when only their loads had been issued, slow
             // memory let the next half line overtake them)
-            if (lane == 0) tc_arrive(&s_half_empty[slot]), tc_arrive(&s_full[st]);
+            if (lane == 0) {
+                tc_arrive(&s_half_empty[slot]);
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full0 + 8u * st) : "memory");
+            }
             if ((slot += 2) >= work.halves) slot = group >> 1, par ^= 1u;
-            if (++in == per_tile) in = 0, ++tile;
         }
     } else if (warp == kLtIssue) {
         // ---- the issuing warp: one lane does it all (with the other lanes in step, their instructions predicated off, a
@@ -522,9 +548,10 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t 
     w.tiles_n = (int)tiles_n;
     w.per_tile = (int)per_tile;
     w.box_n = (int)box;
-    // Eight stages where they leave room for a line of codes, two lines or more beside four otherwise; 256 tokens leave one.
-    const int room = kLtSmem - 1024, stage = kLtABytes + (int)box * 128;
-    w.stages = room - 8 * stage >= 2 * kLtHalfBytes ? 8 : 4;
+    // Eight stages where they leave room for two lines of codes, four otherwise (256 tokens leave two lines beside them).
+    w.table = box <= kLtTableN;
+    const int room = kLtSmem - 1024 - (w.table ? kPairBytes : 0), stage = kLtABytes + (int)box * 128;
+    w.stages = room - 8 * stage >= 4 * kLtHalfBytes ? 8 : 4;
     w.halves = (room - w.stages * stage) / kLtHalfBytes & ~1;
     if (w.halves > kLtMaxHalves) w.halves = kLtMaxHalves;
     // One CTA per SM, each with an equal part of the lines.  A tile is cut into at most so many parts that summing them
@@ -585,20 +612,22 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
     }
     const int64_t last_scale = w.rows * w.cols / w.block_size - 1;
     float* const parts = reinterpret_cast<float*>(base + p.parts);
-#define BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_)                                                                                                        \
+#define BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, LUT_)                                                                                                  \
     {                                                                                                                                             \
-        constexpr auto kern = linear_tc_kernel<BWD_, ST_, HALF_, OPQ_>;                                                                           \
+        constexpr auto kern = linear_tc_kernel<BWD_, ST_, HALF_, OPQ_, LUT_>;                                                                     \
         if ((rc = ensure_dynamic_smem<kern>(kLtSmem))) return rc;                                                                                 \
         launch_after(kern, p.ctas, kLtThreads, kLtSmem, st, code_map, token_map, w.scales, w.cols, w.block_shift, last_scale, w.levels, out,      \
                      status, heads, nodes, p.work, base, parts);                                                                                  \
     }
-#define BOF4_LT_O(BWD_, ST_, HALF_) { if (opq) BOF4_LT_GO(BWD_, ST_, HALF_, true) else BOF4_LT_GO(BWD_, ST_, HALF_, false) }
+#define BOF4_LT_T(BWD_, ST_, HALF_, OPQ_) { if (p.work.table) BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, true) else BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, false) }
+#define BOF4_LT_O(BWD_, ST_, HALF_) { if (opq) BOF4_LT_T(BWD_, ST_, HALF_, true) else BOF4_LT_T(BWD_, ST_, HALF_, false) }
 #define BOF4_LT_H(BWD_, ST_) { if (w.block_size == 32) BOF4_LT_O(BWD_, ST_, true) else BOF4_LT_O(BWD_, ST_, false) }
 #define BOF4_LT_S(BWD_) { if (w.scale_dtype == BOF4_F32) BOF4_LT_H(BWD_, F32) else BOF4_LT_H(BWD_, BF16) }
     if (backward) BOF4_LT_S(true) else BOF4_LT_S(false)
 #undef BOF4_LT_S
 #undef BOF4_LT_H
 #undef BOF4_LT_O
+#undef BOF4_LT_T
 #undef BOF4_LT_GO
     BOF4_CUDA_TRY(cudaGetLastError());
     return BOF4_OK;
