@@ -33,12 +33,12 @@ namespace bof4 {
 constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMoeTokens = 64, kMoeExperts = 512, kMoeTop = 16;
 constexpr int kMoePitch = 20;      // sums of a column, 16 rows, and room that keeps the columns of a quad in different banks
-constexpr int kMoePart = 8 * kMoePitch;  // sums of a warp and unit, [column][row]
-constexpr int kMoeDefer = 2;       // units between two additions over the stripes
+constexpr int kMoeDefer = 16;      // at most so many units between two additions over the stripes
 constexpr int kMoeRing = kMoeWarps * kFewSlots * kFewUnit;
-constexpr int kMoeSums = 2 * kMoeDefer * kMoeWarps * kMoePart * 4;
-static_assert(kMoeSums + 16384 <= (int)kFewTable, "the sums lie before the table, behind 16 KiB of other variables");
-constexpr int kMoeBegin = 12288;   // dynamic memory begins there or later (behind 11.6 KiB of other variables)
+constexpr int kMoeSums = 40960;    // two buffers of sums, [unit][warp][column][row], or the router's partial sums
+static_assert(kMoeSums + 24576 <= (int)kFewTable, "the sums lie before the table, behind 24 KiB of other variables");
+static_assert((kMoeExperts * (kMoeTokens / 4) / kSMs + 1) * kMoeWarps * 16 <= kMoeSums, "router");
+constexpr int kMoeBegin = 21504;   // dynamic memory begins there or later (behind 20.6 KiB of other variables)
 constexpr int kMoeSmem = (int)kFewRing + kMoeRing - kMoeBegin;
 constexpr int kMoeChoices = kMoeTokens * kMoeTop;
 constexpr uint32_t kMoeSpin = 1u << 22;
@@ -64,6 +64,12 @@ struct MoeArgs {
     float* out;                 // [tokens * top][hidden]
 };
 
+__device__ __forceinline__ float moe_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    return v;
+}
 // Order-preserving map of a finite or infinite fp32 value to an unsigned integer (a NaN goes to one end).
 __device__ __forceinline__ uint32_t moe_key(float v)
 {
@@ -78,12 +84,13 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     extern __shared__ unsigned char s_dyn[];
     // the sums, the table at kFewTable, the ring
     float2* const s_pairs = reinterpret_cast<float2*>(s_dyn - smem_u32(s_dyn) + kFewTable);
-    float* const s_part = reinterpret_cast<float*>(s_dyn);  // [2][kMoeDefer][kMoeWarps][kMoePart]
+    float* const s_part = reinterpret_cast<float*>(s_dyn);
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ __align__(8) unsigned long long s_full[kMoeWarps][kFewSlots];
     __shared__ int4 s_what[2][kMoeDefer][kMoeWarps];  // of the units whose parts wait: first row, first place in the list, columns
-    __shared__ uint16_t s_id[kMoeChoices];       // expert of choice t * top + j
+    __shared__ __align__(16) uint16_t s_id[kMoeChoices];  // expert of choice t * top + j
     __shared__ uint16_t s_list[kMoeChoices];     // choices, by expert
+    __shared__ int s_count[kMoeExperts];         // choices of an expert, then its first place in the list
     __shared__ uint16_t s_first[kMoeExperts + 1], s_expert[kMoeExperts];  // of the chosen experts: first place in the list, which
     __shared__ int s_units[2][kMoeExperts + 1];  // units before a chosen expert, gate/up and down
     __shared__ int s_warp[2][kMoeWarps + 1];
@@ -121,43 +128,54 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         return s_fail == 0;
     };
 
-    // ---- router
+    // ---- router: an expert and four tokens a job, its columns over `wide` warps
+    for (int e = tid; e < p.experts; e += kMoeThreads) s_count[e] = 0;
     {
-        const int quads = (p.tokens + 3) / 4;
-        for (int job = (int)blockIdx.x + grid * warp; job < p.experts * quads; job += grid * kMoeWarps) {
-            const int e = job / quads, t0 = (job - e * quads) * 4, n = min(4, p.tokens - t0);
+        const int quads = (p.tokens + 3) / 4, jobs = p.experts * quads, mine = jobs > (int)blockIdx.x ? (jobs - 1 - (int)blockIdx.x) / grid + 1 : 0;
+        int wide = 1;
+        while (wide < kMoeWarps && wide * 256 < p.hidden) wide *= 2;
+        const int at_once = kMoeWarps / wide, part = warp & (wide - 1);
+        for (int k = warp / wide; k < mine; k += at_once) {
+            const int job = (int)blockIdx.x + k * grid, e = job / quads, t0 = (job - e * quads) * 4, n = min(4, p.tokens - t0);
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int64_t c = lane * 8; c < p.hidden; c += 256) {
+            for (int64_t c = part * 256 + lane * 8; c < p.hidden; c += wide * 256) {
                 float r[8];
                 if (p.router_bf16) {
                     const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.router) + e * p.hidden + c));
                     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) r[2 * k] = __uint_as_float(w[k] << 16), r[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                    for (int v = 0; v < 4; ++v) r[2 * v] = __uint_as_float(w[v] << 16), r[2 * v + 1] = __uint_as_float(w[v] & 0xffff0000u);
                 } else {
                     const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p.router) + e * p.hidden + c);
                     const float4 a = __ldg(f), b = __ldg(f + 1);
                     r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
                 }
+                uint4 u[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) u[t] = t < n ? __ldg(reinterpret_cast<const uint4*>(p.x + (t0 + t) * p.ldx + c)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
+                    const uint32_t w[4] = {u[t].x, u[t].y, u[t].z, u[t].w};
+                    // (a token that is not there is left out: its zeros would make a NaN of an infinite weight)
                     if (t < n) {
-                        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.x + (t0 + t) * p.ldx + c));
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            sum[t] = fmaf(r[2 * k], __uint_as_float(w[k] << 16), sum[t]);
-                            sum[t] = fmaf(r[2 * k + 1], __uint_as_float(w[k] & 0xffff0000u), sum[t]);
+                        for (int v = 0; v < 4; ++v) {
+                            sum[t] = fmaf(r[2 * v], __uint_as_float(w[v] << 16), sum[t]);
+                            sum[t] = fmaf(r[2 * v + 1], __uint_as_float(w[v] & 0xffff0000u), sum[t]);
                         }
                     }
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int o = 16; o >= 1; o >>= 1) sum[t] += __shfl_xor_sync(kFull, sum[t], o);
-                if (lane == 0 && t < n) p.logits[(t0 + t) * p.experts + e] = sum[t];
-            }
+            for (int t = 0; t < 4; ++t) sum[t] = moe_sum(sum[t]);
+            if (lane == 0) *reinterpret_cast<float4*>(s_part + (k * kMoeWarps + part) * 4) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        }
+        __syncthreads();
+        for (int i = tid; i < mine * 4; i += kMoeThreads) {
+            const int k = i >> 2, job = (int)blockIdx.x + k * grid, e = job / quads, t = (job - e * quads) * 4 + (i & 3);
+            float sum = 0.0f;
+            for (int w = 0; w < wide; ++w) sum += s_part[(k * kMoeWarps + w) * 4 + (i & 3)];
+            if (t < p.tokens) p.logits[t * p.experts + e] = sum;
         }
     }
     if (tid < 8) s_levels[tid] = make_float2(__ldg(p.levels + 2 * tid), __ldg(p.levels + 2 * tid + 1));
@@ -165,6 +183,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     if (!meet(0)) return;
 
     // ---- the choice, by every CTA for itself
+    const int ranks = (p.experts + 31) / 32;  // experts of a lane
     for (int t = warp; t < p.tokens; t += kMoeWarps) {
         constexpr int R = kMoeExperts / 32;
         float s[R];
@@ -172,57 +191,58 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         float most = -INFINITY;
 #pragma unroll
         for (int k = 0; k < R; ++k) {
+            if (k >= ranks) continue;
             const int e = k * 32 + lane;
             s[k] = e < p.experts ? __ldcg(p.logits + t * p.experts + e) : 0.0f;
-            if (e < p.experts) free |= 1u << k, most = fmaxf(most, s[k]);
+            if (e < p.experts) free |= 1u << k;
         }
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k < ranks && (free >> k & 1u)) most = fmaxf(most, s[k]);
         float total = 0.0f;
         if (p.score == BOF4_SCORE_SOFTMAX) {
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
 #pragma unroll
             for (int k = 0; k < R; ++k)
-                if (k * 32 + lane < p.experts) total += expf(s[k] - most);
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
+                if (k < ranks && (free >> k & 1u)) total += expf(s[k] - most);
+            total = moe_sum(total);
         }
-        float mine = 0.0f, chosen_sum = 0.0f;  // lane j: the score of choice j
+        float mine = 0.0f;  // lane j: the score of choice j
+        int chosen_e = 0;   // and which it is
         for (int j = 0; j < p.top; ++j) {
             // the largest remaining logit, then the lowest index
-            unsigned long long best = 0ull;
+            uint32_t best = 0u, which = 0xffffffffu;
             float value = 0.0f;
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                const unsigned long long key = (unsigned long long)moe_key(s[k]) << 32 | (0xffffffffu - (uint32_t)(k * 32 + lane));
-                if ((free >> k & 1u) && key > best) best = key, value = s[k];
+                if (k >= ranks) continue;
+                const uint32_t key = moe_key(s[k]);
+                if ((free >> k & 1u) && (which == 0xffffffffu || key > best)) best = key, which = (uint32_t)(k * 32 + lane), value = s[k];
             }
-            unsigned long long top = best;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) {
-                const unsigned long long other = __shfl_xor_sync(kFull, top, o);
-                if (other > top) top = other;
-            }
-            const int e = (int)(0xffffffffu - (uint32_t)top);
+            const bool any = which != 0xffffffffu;
+            const uint32_t top = __reduce_max_sync(kFull, any ? best : 0u);
+            const int e = (int)__reduce_min_sync(kFull, any && best == top ? which : 0xffffffffu);
             value = __shfl_sync(kFull, value, e & 31);
             if ((e & 31) == lane) free &= ~(1u << (e >> 5));
-            const float score = p.score == BOF4_SCORE_SOFTMAX ? expf(value - most) / total : 1.0f / (1.0f + expf(-value));
-            chosen_sum += score;
-            if (lane == j) mine = score, s_id[t * p.top + j] = (uint16_t)e;
+            if (lane == j) mine = value, chosen_e = e;
         }
-        if (p.renormalize) mine /= chosen_sum;
-        if (blockIdx.x == 0 && lane < p.top) {
-            p.ids[t * p.top + lane] = s_id[t * p.top + lane];
-            p.weights[t * p.top + lane] = mine * p.scale;
+        if (lane < p.top) mine = p.score == BOF4_SCORE_SOFTMAX ? expf(mine - most) / total : 1.0f / (1.0f + expf(-mine));
+        else mine = 0.0f;
+        if (p.renormalize) mine /= moe_sum(mine);
+        if (lane < p.top) {
+            const int a = t * p.top + lane;
+            s_id[a] = (uint16_t)chosen_e;
+            atomicAdd(&s_count[chosen_e], 1);
+            if (blockIdx.x == 0) p.ids[a] = chosen_e, p.weights[a] = mine * p.scale;
         }
     }
     __syncthreads();
     // ---- the chosen experts in ascending order, their choices, and the units before each
     const int choices = p.tokens * p.top;
-    const int tiles1 = (int)(p.ffn / 8), tiles2 = (int)((p.hidden + 15) / 16);
+    const int tiles1 = (int)(p.ffn / 8), tiles2 = (int)(p.hidden / 16);
     {
-        int count = 0;
-        if (tid < p.experts)
-            for (int a = 0; a < choices; ++a) count += s_id[a] == tid;
+        const int count = tid < p.experts ? s_count[tid] : 0;
         // running numbers over the threads: choices, and chosen experts
         int before = count, which = count > 0;
 #pragma unroll
@@ -232,14 +252,14 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         }
         if (lane == 31) s_warp[0][warp] = before, s_warp[1][warp] = which;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) before += s_warp[0][w], which += s_warp[1][w];
+#pragma unroll
+        for (int w = 0; w < kMoeWarps; ++w)
+            if (w < warp) before += s_warp[0][w], which += s_warp[1][w];
         if (count > 0) {
-            const int at = before - count, i = which - 1;
+            const int i = which - 1;
             s_expert[i] = (uint16_t)tid;
-            s_first[i] = (uint16_t)at;
-            int k = at;
-            for (int a = 0; a < choices; ++a)
-                if (s_id[a] == tid) s_list[k++] = (uint16_t)a;
+            s_first[i] = (uint16_t)(before - count);
+            s_count[tid] = before - count;
             // passes of eight tokens (gate/up) and of four (down)
             s_units[0][i] = (count + 7) / 8 * tiles1;
             s_units[1][i] = (count + 3) / 4 * tiles2;
@@ -247,6 +267,22 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         if (tid == kMoeThreads - 1) s_chosen = which, s_first[which] = (uint16_t)choices;
     }
     __syncthreads();
+    // a choice's place in its expert's list: the choices before it with the same expert.  (All CTAs need the same order: an expert's
+    // passes take their tokens from it.)
+    for (int a = tid; a < choices; a += kMoeThreads) {
+        const uint32_t id = s_id[a], twice = id << 16 | id;
+        int rank = 0;
+        for (int b = 0; b < a; b += 8) {
+            const uint4 v = *reinterpret_cast<const uint4*>(s_id + b);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t x = w[k] ^ twice;
+                rank += (b + 2 * k < a && (x & 0xffffu) == 0u) + (b + 2 * k + 1 < a && (x >> 16) == 0u);
+            }
+        }
+        s_list[s_count[id] + rank] = (uint16_t)a;
+    }
     const int chosen = s_chosen;
     if (warp < 2) {  // exclusive sums over the chosen experts, by a warp each
         int carry = 0;
@@ -270,7 +306,8 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     uint32_t parity = 0;
     bool failed = false;     // a wait for codes ran out
     const uint32_t ring = kFewRing + (uint32_t)(warp * kFewSlots * kFewUnit);
-    auto walk = [&](auto second_c) {
+    // `before`: what has to happen before the first tokens are read; codes are on their way by then.  False: it failed.
+    auto walk = [&](auto second_c, auto&& before) -> bool {
         constexpr bool SECOND = decltype(second_c)::value;
         constexpr int PASS = SECOND ? 4 : 8;
         const int* const units = s_units[SECOND ? 1 : 0];
@@ -322,8 +359,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                                  : "memory");
             }
             const int cc = c0 + 64 * q;
-            const uint32_t live = ((ok && cc < cols ? 5u : 0u) | (ok && cc + 32 < cols ? 10u : 0u)) &
-                                  (SECOND ? (ask.tile * 16 + g < hidden ? 3u : 0u) | (ask.tile * 16 + 8 + g < hidden ? 12u : 0u) : 15u);
+            const uint32_t live = (ok && cc < cols ? 5u : 0u) | (ok && cc + 32 < cols ? 10u : 0u);
             const int64_t col = cc >> p.block_shift;
             c.load(scales, (int64_t)(r0 + g) * per_row + col, (int64_t)(r1 + g) * per_row + col, live);
             ++asked;
@@ -333,6 +369,13 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         auto slot_after = [&](int k) { return slot + k >= kFewSlots ? slot + k - kFewSlots : slot + k; };
 #pragma unroll
         for (int k = 0; k < kFewAhead; ++k) request(slot_after(k), m[k]);
+        if (!before()) {  // nothing of this CTA may be on its way when it ends
+            for (int k = 0; k < min(asked, mine * rounds); ++k)
+                if (k < kFewAhead) (void)tc_wait(smem_u32(&s_full[warp][slot_after(k)]), slot + k >= kFewSlots ? parity ^ 1u : parity);
+            return false;
+        }
+        // columns that a part has, down after the two halves of h have been added up, and units between two additions over the stripes
+        const int columns = min(PASS, p.tokens), size = columns * kMoePitch, defer = min(kMoeDefer, kMoeSums / (2 * kMoeWarps * size * 4));
         int k = 0, buf = 0, have_i = -1, have_pass = -1;  // whose tokens xr holds
         uint32_t xr[1][32];
         for (int s = 0; s < steps; ++s) {
@@ -362,25 +405,32 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
             } else if (busy && stripe == 0 && lane == 0) {
                 s_what[buf][k][group] = make_int4(0, 0, 0, 0);
             }
-            float* const to = s_part + ((buf * kMoeDefer + k) * kMoeWarps + warp) * kMoePart + 2 * q * kMoePitch + g;
-            to[0] = acc[0][0], to[kMoePitch] = acc[0][1], to[8] = acc[0][2], to[kMoePitch + 8] = acc[0][3];
-            if (k == kMoeDefer - 1 || s + 1 == steps) {
+            if (SECOND) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[0][v] += __shfl_xor_sync(kFull, acc[0][v], 2);  // columns c and c + 4
+            }
+            float* const to = s_part + ((buf * defer + k) * kMoeWarps + warp) * size + 2 * q * kMoePitch + g;
+            if (2 * q < columns) to[0] = acc[0][0], to[8] = acc[0][2];
+            if (2 * q + 1 < columns) to[kMoePitch] = acc[0][1], to[kMoePitch + 8] = acc[0][3];
+            if (k == defer - 1 || s + 1 == steps) {
                 __syncthreads();
-                // results of k + 1 units of each group, rows along the lanes: gate/up 8 rows x 8 tokens, down 16 rows x 4 tokens
-                for (uint32_t e = (uint32_t)tid; e < (uint32_t)((k + 1) * groups * 64); e += kMoeThreads) {
-                    const uint32_t row = SECOND ? e & 15u : e & 7u, col = SECOND ? (e >> 4) & 3u : (e >> 3) & 7u, rest = e >> 6;
-                    const uint32_t j = rest / (uint32_t)groups, gr = rest - j * (uint32_t)groups;
+                // results of k + 1 units of each group, rows along the lanes
+                constexpr int ROWS = SECOND ? 16 : 8;
+                for (uint32_t e = (uint32_t)tid; e < (uint32_t)((k + 1) * groups * columns * ROWS); e += kMoeThreads) {
+                    const uint32_t row = e % ROWS, rest = e / ROWS, unit = rest / (uint32_t)columns, col = rest - unit * (uint32_t)columns;
+                    const uint32_t j = unit / (uint32_t)groups, gr = unit - j * (uint32_t)groups;
                     const int4 what = s_what[buf][j][gr];
                     if ((int)col >= what.z) continue;
                     const int a = s_list[what.y + (int)col];
-                    const float* part = s_part + ((buf * kMoeDefer + j) * kMoeWarps + gr * wide) * kMoePart + col * kMoePitch + row;
-                    constexpr int other = SECOND ? 4 * kMoePitch : 8;
+                    const float* part = s_part + ((buf * defer + j) * kMoeWarps + gr * wide) * size + col * kMoePitch + row;
                     float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll 4
-                    for (int w = 0; w < wide; ++w) v0 += part[w * kMoePart], v1 += part[w * kMoePart + other];
+                    for (int w = 0; w < wide; ++w) {
+                        v0 += part[w * size];
+                        if (!SECOND) v1 += part[w * size + 8];
+                    }
                     if (SECOND) {
-                        const int o = what.x * 16 + (int)row;
-                        if (o < hidden) p.out[(int64_t)a * hidden + o] = v0 + v1;
+                        p.out[(int64_t)a * hidden + what.x * 16 + (int)row] = v0;
                     } else {
                         const float h = activate(v0, p.act) * v1;
                         const uint16_t hi = bf16_round(h);
@@ -396,10 +446,10 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
             }
         }
         if (failed) atomicExch(p.status, 1);
+        return true;
     };
-    walk(std::false_type{});
-    if (!meet(1)) return;
-    walk(std::true_type{});
+    if (!walk(std::false_type{}, [] { return true; })) return;
+    if (!walk(std::true_type{}, [&] { return meet(1); })) return;
     if (!meet(2)) return;
 
     // ---- the weighted sums
