@@ -57,7 +57,7 @@ struct MoeArgs {
     int32_t* ids;
     float* weights;
     int* status;
-    unsigned long long* cells;  // barriers
+    unsigned long long* cell;   // arrivals at the barriers in the low 16 bits, the launch's epoch above
     unsigned long long epoch;
     float* logits;              // [tokens][experts]
     uint16_t *h_hi, *h_lo;      // [tokens * top][ffn]
@@ -107,17 +107,25 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     if (tid == 0) {
         s_fail = 0;
         if (blockIdx.x == 0) *p.status = 0;
-        tc_ticket_open(p.cells + 0, p.epoch), tc_ticket_open(p.cells + 1, p.epoch), tc_ticket_open(p.cells + 2, p.epoch), tc_ticket_open(p.cells + 3, p.epoch);
     }
-    // All CTAs of the grid meet; false: a time-out.  What they wrote before is visible after.
+    if (tid == kMoeThreads - 32) {  // (a warp that mostly has nothing to do at first)
+        // the cell needs no preparation: every CTA makes sure that it carries this launch's epoch before it arrives
+        unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(p.cell);
+        while ((old & ~0xffffull) != p.epoch) {
+            const unsigned long long seen = atomicCAS(p.cell, old, p.epoch);
+            if (seen == old) break;
+            old = seen;  // somebody else opened it or arrived: at most as many rounds as CTAs
+        }
+    }
+    // All CTAs of the grid meet for the which-th time; false: a time-out.  What they wrote before is visible after.
     auto meet = [&](int which) -> bool {
         __threadfence();
         __syncthreads();
         if (tid == 0) {
-            atomicAdd(p.cells + which, 1ull);
-            const unsigned long long all = p.epoch | (unsigned long long)grid;
+            atomicAdd(p.cell, 1ull);
+            const unsigned long long all = p.epoch + (unsigned long long)((which + 1) * grid);
             uint32_t spin = 0;
-            while (*reinterpret_cast<volatile unsigned long long*>(p.cells + which) != all && ++spin < kMoeSpin) __nanosleep(20);
+            while (*reinterpret_cast<volatile unsigned long long*>(p.cell) < all && ++spin < kMoeSpin) __nanosleep(20);
             if (spin >= kMoeSpin) {
                 s_fail = 1;
                 atomicExch(p.status, 1);
@@ -342,12 +350,20 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
             now.pass = in / tiles, now.tile = in - now.pass * tiles;
         }
         Place ask = now;
-        int asked = 0;
+        int asked = 0, row0 = 0, row1 = 0;   // rows of the unit that is asked for next, first of its eight and of the other eight
+        int64_t at0 = 0, at1 = 0;            // the lane's constants in rows g of each
+        auto aim = [&] {
+            const int e = s_expert[ask.i], cc = (ask.round * wide + stripe) * kFewStripe + 64 * q;
+            row0 = SECOND ? e * hidden + ask.tile * 16 : e * 2 * ffn + ask.tile * 8;
+            row1 = SECOND ? row0 + 8 : row0 + ffn;
+            at0 = (int64_t)(row0 + g) * per_row + (cc >> p.block_shift);
+            at1 = (int64_t)(row1 + g) * per_row + (cc >> p.block_shift);
+        };
+        if (mine) aim();
         FewConst<ST, HALF> m[kFewAhead + 1];
         auto request = [&](int k, FewConst<ST, HALF>& c) {
             const bool ok = asked < mine * rounds;
-            const int e = s_expert[ok ? ask.i : 0], c0 = (ask.round * wide + stripe) * kFewStripe;
-            const int r0 = SECOND ? e * hidden + ask.tile * 16 : e * 2 * ffn + ask.tile * 8, r1 = SECOND ? r0 + 8 : r0 + ffn;
+            const int c0 = (ask.round * wide + stripe) * kFewStripe, cc = c0 + 64 * q;
             if (ok && lane == 0) {
                 const uint32_t bar = smem_u32(&s_full[warp][k]), dst = ring + (uint32_t)(k * kFewUnit);
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)kFewUnit) : "memory");
@@ -355,15 +371,21 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                 for (int h = 0; h < 2; ++h)
                     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                                  :
-                                 : "r"(dst + h * 1024u), "l"(reinterpret_cast<uint64_t>(SECOND ? &map2 : &map1)), "r"(bar), "r"(c0 >> 1), "r"(h ? r1 : r0)
+                                 : "r"(dst + h * 1024u), "l"(reinterpret_cast<uint64_t>(SECOND ? &map2 : &map1)), "r"(bar), "r"(c0 >> 1), "r"(h ? row1 : row0)
                                  : "memory");
             }
-            const int cc = c0 + 64 * q;
-            const uint32_t live = (ok && cc < cols ? 5u : 0u) | (ok && cc + 32 < cols ? 10u : 0u);
-            const int64_t col = cc >> p.block_shift;
-            c.load(scales, (int64_t)(r0 + g) * per_row + col, (int64_t)(r1 + g) * per_row + col, live);
+            c.load(scales, at0, at1, (ok && cc < cols ? 5u : 0u) | (ok && cc + 32 < cols ? 10u : 0u));
             ++asked;
-            if (ok) step_on(ask);
+            if (!ok) return;
+            step_on(ask);
+            if (asked == mine * rounds) return;
+            if (rounds == 1 && ask.tile) {  // the next rows of the same expert
+                constexpr int next = SECOND ? 16 : 8;
+                row0 += next, row1 += next;
+                at0 += next * per_row, at1 += next * per_row;
+            } else {
+                aim();
+            }
         };
         // (ring slots go on from where the walk before ended)
         auto slot_after = [&](int k) { return slot + k >= kFewSlots ? slot + k - kFewSlots : slot + k; };
@@ -460,14 +482,14 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         if (p.y_bf16) static_cast<uint16_t*>(p.y)[t * p.ldy + o] = bf16_round(sum);
         else static_cast<float*>(p.y)[t * p.ldy + o] = sum;
     }
-    // the last to leave clears the barriers: a replayed launch has the same epoch
-    if (tid == 0 && (int)(atomicAdd(p.cells + 3, 1ull) & 255ull) == grid - 1) p.cells[0] = p.cells[1] = p.cells[2] = p.cells[3] = 0ull;
+    // the last to leave clears the cell: a replayed launch has the same epoch
+    if (tid == 0 && (int)(atomicAdd(p.cell, 1ull) & 0xffffull) == 4 * grid - 1) *p.cell = 0ull;
 }
 
 namespace {
 
 struct MoePlan {
-    size_t logits, hi, lo, out, total;  // byte offsets (the barriers are at 0), and the bytes of all
+    size_t logits, hi, lo, out, total;  // byte offsets (the barriers' cell is at 0), and the bytes of all
 };
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 MoePlan moe_plan(int64_t tokens, int64_t hidden, int64_t ffn, int64_t experts, int64_t top)
@@ -567,8 +589,9 @@ extern "C" int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t 
     a.ids = d_ids;
     a.weights = d_weights;
     a.status = d_status;
-    a.cells = reinterpret_cast<unsigned long long*>(base);
-    a.epoch = tc_next_epoch();
+    a.cell = reinterpret_cast<unsigned long long*>(base);
+    do a.epoch = tc_next_epoch() & ~0xffffull;
+    while (!a.epoch);
     a.logits = reinterpret_cast<float*>(base + plan.logits);
     a.h_hi = reinterpret_cast<uint16_t*>(base + plan.hi);
     a.h_lo = reinterpret_cast<uint16_t*>(base + plan.lo);
