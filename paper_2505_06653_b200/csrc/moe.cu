@@ -368,7 +368,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                 const uint32_t bar = smem_u32(&s_full[warp][k]), dst = ring + (uint32_t)(k * kFewUnit);
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)kFewUnit) : "memory");
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < (SECOND ? 1 : 2); ++h)
                     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                                  :
                                  : "r"(dst + h * 1024u), "l"(reinterpret_cast<uint64_t>(SECOND ? &map2 : &map1)), "r"(bar), "r"(c0 >> 1), "r"(h ? row1 : row0)
@@ -609,7 +609,7 @@ extern "C" int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t 
     int rc;
     CUtensorMap map1, map2;
     if ((rc = tc_make_map(fn, d_gate_up_codes, 1, hidden / 2, n_experts * 2 * ffn, hidden / 2, 128, 8, &map1)) ||
-        (rc = tc_make_map(fn, d_down_codes, 1, ffn / 2, n_experts * hidden, ffn / 2, 128, 8, &map2)))
+        (rc = tc_make_map(fn, d_down_codes, 1, ffn / 2, n_experts * hidden, ffn / 2, 128, 16, &map2)))
         return rc;
 #define BOF4_MOE_GO(ST_, HALF_)                                                  \
     {                                                                            \
