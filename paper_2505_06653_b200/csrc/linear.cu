@@ -191,7 +191,7 @@ extern "C" size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_
     if (rows < 0 || cols < 0 || n_tokens < 0 || capacity < 0 || rows > INT32_MAX || cols > INT32_MAX || n_tokens > INT32_MAX || capacity > INT32_MAX)
         return 0;
     if (rows == 0 || n_tokens == 0) return 256;
-    if (!backward && cols && linear_few_applies(rows, cols, n_tokens)) return linear_few_ws_bytes(rows, cols, n_tokens, capacity);
+    if (!backward && cols && linear_few_applies(rows, cols, n_tokens, capacity > 0)) return linear_few_ws_bytes(rows, cols, n_tokens, capacity);
     const size_t product = cols ? linear_tc_ws_bytes(rows, cols, n_tokens, backward != 0, capacity) : 256;
     if (!product || !backward) return product;
     return dz_plan(rows, n_tokens, product).total;
@@ -259,7 +259,7 @@ extern "C" int bof4_linear(const uint8_t* d_codes, const void* d_scales, int sca
     }
     w.codes = d_codes;
     w.levels = d_codebook;
-    if (linear_few_applies(rows, cols, n_tokens)) return linear_few(fn, w, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
+    if (linear_few_applies(rows, cols, n_tokens, w.capacity > 0)) return linear_few(fn, w, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
     return linear_tc(fn, w, false, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
 }
 

@@ -186,7 +186,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
               void* ws, size_t ws_bytes, cudaStream_t st);
 
 // The form for one to sixteen tokens.
-bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens);
+bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list);
 size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity);
 int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, const LinearOut& out, int* status, void* ws, size_t ws_bytes,
                cudaStream_t st);

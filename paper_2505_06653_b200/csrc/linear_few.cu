@@ -180,9 +180,9 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     }
 }
 
-// Outliers: correction[t, r] = sum over the entries of row r of (val - W^) x[t, c], zero elsewhere (set before).  A thread per entry
-// forms its terms, and the one with a row's first entry adds the row's up, in the order of the list; a row that runs past the
-// CTA's 256 entries is finished from global memory.
+// Outliers: correction[t, r] = sum over the entries of row r of (val - W^) x[t, c], zero elsewhere (set before).  A CTA takes 256
+// entries: their changes, a term per entry and token, and a row's terms added up in the order of the list; what is left of a row
+// more than 64 entries behind them comes from global memory.
 constexpr int kFewTokens = 16;
 template <class ST>
 __device__ __forceinline__ float scale_at(const void* scales, int64_t b)
@@ -196,8 +196,9 @@ few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict_
                       const uint16_t* __restrict__ val, const int64_t* __restrict__ n_out, int64_t capacity, float* __restrict__ correction)
 {
     if (!after_previous()) return;
-    __shared__ float s_term[256][kFewTokens + 1];
-    __shared__ int s_row[256];
+    constexpr int N = 256 + 64;  // the CTA's entries, and those behind them that may belong to its last row
+    __shared__ float s_term[N][kFewTokens + 1], s_change[N];
+    __shared__ int s_row[N], s_col[N];
     int64_t k_end = *n_out;
     if (k_end > capacity) k_end = capacity;
     const int64_t n = rows * cols;
@@ -212,25 +213,39 @@ few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict_
     };
     const int tid = threadIdx.x;
     for (int64_t base = (int64_t)blockIdx.x * 256; base < k_end; base += (int64_t)gridDim.x * 256) {
-        const int64_t k = base + tid;
-        const int r = k < k_end ? row_of(k) : -1;
-        s_row[tid] = r;
-        if (r >= 0) {
-            const float d = change_of(k);
-            const int64_t c = idx[k] - (int64_t)r * cols;
-            for (int t = 0; t < tokens; ++t) s_term[tid][t] = d * bf16_value(x[t * ldx + c]);
+        for (int e = tid; e < N; e += 256) {
+            const int64_t k = base + e;
+            const int r = k < k_end ? row_of(k) : -1;
+            s_row[e] = r;
+            s_col[e] = r >= 0 ? (int)(idx[k] - (int64_t)r * cols) : 0;
+            s_change[e] = r >= 0 ? change_of(k) : 0.0f;
         }
         __syncthreads();
-        if (r >= 0 && (tid > 0 ? s_row[tid - 1] : (k > 0 ? row_of(k - 1) : -1)) != r) {  // first outlier of its row
-            int end = tid;
-            while (end < 256 && s_row[end] == r) ++end;
-            for (int t = 0; t < tokens; ++t) {
-                float sum = 0.0f;
-                for (int j = tid; j < end; ++j) sum += s_term[j][t];
-                if (end == 256)
-                    for (int64_t kk = base + 256; kk < k_end && row_of(kk) == r; ++kk) sum += change_of(kk) * bf16_value(x[t * ldx + idx[kk] - (int64_t)r * cols]);
-                correction[(int64_t)t * rows + r] = sum;
+        // a term per entry and token, four on their way at a time
+        for (int e0 = tid; e0 < N * tokens; e0 += 4 * 256) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = e0 + u * 256, t = i / N, e = i - t * N;
+                v[u] = t < tokens && s_row[e] >= 0 ? s_change[e] * bf16_value(__ldg(x + t * ldx + s_col[e])) : 0.0f;
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = e0 + u * 256, t = i / N;
+                if (t < tokens) s_term[i - t * N][t] = v[u];
+            }
+        }
+        __syncthreads();
+        // the sums of a row's entries, a thread per token
+        for (int i = tid; i < 256 * tokens; i += 256) {
+            const int e = i & 255, t = i >> 8, row = s_row[e];
+            if (row < 0 || (e > 0 ? s_row[e - 1] : (base > 0 ? row_of(base - 1) : -1)) == row) continue;  // not the first outlier of its row
+            float sum = 0.0f;
+            int j = e;
+            while (j < N && s_row[j] == row) sum += s_term[j++][t];
+            if (j == N)
+                for (int64_t kk = base + N; kk < k_end && row_of(kk) == row; ++kk) sum += change_of(kk) * bf16_value(x[t * ldx + idx[kk] - (int64_t)row * cols]);
+            correction[(int64_t)t * rows + row] = sum;
         }
         __syncthreads();
     }
@@ -275,9 +290,12 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
 
 }  // namespace
 
-bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens)
+// Up to sixteen tokens, where the other form decodes as much for a tile of sixteen (8192 x 8192: 27 us against 32 for nine tokens, 33
+// against 32 for sixteen; 1024 x 4096: 9 against 13); up to six with a list of outliers, whose corrections cost 3 us a token there
+// and less here (8192 x 8192 with 65,536: 34 us against 42 for four tokens, 60 against 42 for twelve).
+bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list)
 {
-    return tokens <= kFewTokens && cols <= 32768 && rows <= (1 << 26);
+    return tokens <= (list ? 6 : kFewTokens) && cols <= 32768 && rows <= (1 << 26);
 }
 
 size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity) { return few_plan(rows, cols, tokens, capacity > 0).total; }

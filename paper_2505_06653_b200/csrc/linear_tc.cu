@@ -483,16 +483,13 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         __threadfence();
         const float4* head = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + (work.start(i0) <= t0 ? 1 : 0)) * slab;
         const float4* next = reinterpret_cast<const float4*>(parts) + (int64_t)(2 * i0 + 2) * slab;
-        constexpr int B = 3;  // quads of rows of a thread at a time
+        constexpr int B = 4;  // quads of rows of a thread at a time
         for (int e0 = tid; e0 < count * (kLtM / 4); e0 += B * kLtThreads) {
             float4 sum[B];
-            LinearFour four[B];
 #pragma unroll
             for (int u = 0; u < B; ++u) {
                 const int e = e0 + u * kLtThreads;
-                const bool on = e < count * (kLtM / 4);
-                sum[u] = on ? __ldcg(head + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-                if (on && o0 + (e & 31) * 4 < out.n) four[u].residual(out, token0 + (e >> 5), o0 + (e & 31) * 4);
+                sum[u] = e < count * (kLtM / 4) ? __ldcg(head + e) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
             for (int i = 0; i < more; i += 2) {
                 float4 v[2][B];
@@ -507,6 +504,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 for (int w = 0; w < 2; ++w)
 #pragma unroll
                     for (int u = 0; u < B; ++u) sum[u].x += v[w][u].x, sum[u].y += v[w][u].y, sum[u].z += v[w][u].z, sum[u].w += v[w][u].w;
+            }
+            LinearFour four[B];
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const int e = e0 + u * kLtThreads;
+                if (e < count * (kLtM / 4) && o0 + (e & 31) * 4 < out.n) four[u].residual(out, token0 + (e >> 5), o0 + (e & 31) * 4);
             }
 #pragma unroll
             for (int u = 0; u < B; ++u) {
