@@ -44,6 +44,7 @@ constexpr int kLtABytes = kLtM * kLtK * 2;   // 16 KiB
 constexpr int kLtHalfBytes = 8192;           // half a line of codes: two k-blocks; 128 rows x 64 bytes
 constexpr int kLtMaxStages = 8, kLtMaxHalves = 8;
 constexpr int kLtTableN = 64;                // tokens of a tile up to which there is room, and use, for the table of pairs
+constexpr int kLtLongK = 4096;               // K up to which results in fp32 have tiles of any width
 constexpr int kLtAhead = 6;                  // lines that L2 is asked for before the ring is
 constexpr int kLtSmem = 225 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
 constexpr int kLtIssue = 16, kLtTokens = 17, kLtCodes = 18, kLtResults = 20;  // warp 19 has no job: the results start at a multiple of 4
@@ -53,6 +54,7 @@ struct LtWork {
     int tiles, tiles_n, per_tile;  // tiles, those along the tokens, lines of a tile
     int box_n;                     // tokens of a tile, a multiple of 16
     int stages, halves;            // stages of A and B (4 or 8), half lines of codes (even)
+    int accs;                      // accumulators of a part of a tile, which the instructions of a k-block use in turn: 4, 2 or 1
     int each, extra;               // lines per CTA, and the remainder
     bool table;                    // half of the codes go through a table
     unsigned long long epoch;
@@ -94,13 +96,29 @@ linear_outlier_lists(const int32_t* __restrict__ idx, const uint16_t* __restrict
     }
 }
 
-// Sixteen tokens (the first `count` of them) of a finished accumulator: row o of the output in each lane.  Of bf16 values, the
-// lanes of a pair exchange one for every two tokens, so that each stores two rows of a token; their residual is read the same way.
-__device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, float b, int64_t t0, int count, int64_t o, bool live, int lane)
+// Sixteen columns of the warp's 32 rows, added over the accumulators in order.
+__device__ __forceinline__ void lt_sums(uint32_t src, int accs, float (&z)[16])
 {
     uint32_t a[16];
-    __syncwarp();
     lt_load16(src, a);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z[k] = __uint_as_float(a[k]);
+    for (int i = 1; i < accs; ++i) {
+        lt_load16(src + (uint32_t)(i * (kLtMaxN / accs)), a);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < 16; ++k) z[k] += __uint_as_float(a[k]);
+    }
+}
+
+// Sixteen tokens (the first `count` of them) of a finished accumulator: row o of the output in each lane.  Of bf16 values, the
+// lanes of a pair exchange one for every two tokens, so that each stores two rows of a token; their residual is read the same way.
+__device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t o, bool live, int lane)
+{
+    float z[16];
+    __syncwarp();
+    lt_sums(src, accs, z);
     const bool odd = lane & 1, both = (o | 1) < out.n, one = (o & ~(int64_t)1) < out.n;  // the pair's two rows exist, its first
     const bool paired = out.y_bf16 && out.pairs && count >= 16;
     float r[16];
@@ -119,11 +137,8 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, fl
 #pragma unroll
         for (int k = 0; k < 16; ++k) r[k] = live && k < count ? out.residual_at(t0 + k, o) : 0.0f;
     }
-    __syncwarp();
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-    float z[16];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) z[k] = __uint_as_float(a[k]) + b;
+    for (int k = 0; k < 16; ++k) z[k] += b;
     // rows (o & ~1, + 1) of tokens 2 k + odd
     auto exchange = [&](float (&v)[16], auto&& use) {
 #pragma unroll
@@ -189,7 +204,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     const uint32_t b_ring = code_ring + (uint32_t)work.halves * kLtHalfBytes;
     const uint32_t pairs = b_ring + (uint32_t)work.stages * b_stage;
     // line n of this CTA has stages turn(n) * 4 ... + 3, for the time(n)-th time
-    const int two = work.stages == 8 ? 1 : 0;
+    const int two = work.stages == 8 ? 1 : 0, accs = work.accs;
     auto turn = [&](int n) { return n & two; };
     auto time = [&](int n) { return (uint32_t)(n >> two) & 1u; };
     const int begin = work.start((int)blockIdx.x), finish = work.start((int)blockIdx.x + 1), lines = finish - begin;
@@ -335,7 +350,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             uint32_t acc = 0u;
             bool ok = true;
             for (int n = 0; n < lines; ++n) {
-                const uint32_t d = tmem + (uint32_t)((seg & 1) * kLtMaxN), par = time(n);
+                const uint32_t par = time(n);
+                uint32_t d[kLtK / 16];  // of the instructions of a k-block
+#pragma unroll
+                for (int kk = 0; kk < kLtK / 16; ++kk) d[kk] = tmem + (uint32_t)((seg & 1) * kLtMaxN + (kk & (accs - 1)) * (kLtMaxN / accs));
                 const int s0 = turn(n) * kLtGroups;
                 if (acc == 0u && !(ok = wait(smem_u32(&s_acc_empty[seg & 1]), (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
                 // a look at all four stages first: mostly they are full, and the looks overlap
@@ -355,10 +373,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                             "setp.ne.b32 p, %4, 0;\n\t"
                             "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                             :
-                            : "r"(d), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(acc)
+                            : "r"(d[kk]), "l"(da + a_step * kk), "l"(db + (uint64_t)(2 * kk)), "r"(idesc), "r"(kk < accs ? acc : 1u)
                             : "memory");
-                        acc = 1u;
                     }
+                    acc = 1u;
                     tc_commit(&s_empty[st], 1u);
                 }
                 if (!ok) break;
@@ -442,15 +460,14 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             if (!all) {
                 float* to = part + m;
                 for (int q = 0; q < count; q += 16, to += 16 * kLtM) {
-                    uint32_t a[16];
-                    lt_load16(src + (uint32_t)q, a);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    float z[16];
+                    lt_sums(src + (uint32_t)q, accs, z);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) to[k * kLtM] = __uint_as_float(a[k]);  // (count is padded to 16 in the workspace)
+                    for (int k = 0; k < 16; ++k) to[k * kLtM] = z[k];  // (count is padded to 16 in the workspace)
                 }
             } else {
                 const float b = live ? out.bias_at(o) : 0.0f;
-                for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, b, token0 + q, count - q, o, live, lane);
+                for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -537,12 +554,16 @@ struct LtPlan {
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // False: too large for 32-bit line numbers.
-bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t capacity, LtPlan* p)
+bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp32, int64_t capacity, LtPlan* p)
 {
     const int64_t m = backward ? cols : rows, k = backward ? rows : cols;
     // (k-blocks past the end of K have zeros for the tokens)
     const int64_t tiles_m = (m + kLtM - 1) / kLtM, per_tile = (k + kLtK * kLtGroups - 1) / (kLtK * kLtGroups), blocks = per_tile * kLtGroups;
-    const int64_t most_n = (tokens + kLtMaxN - 1) / kLtMaxN;
+    // The tensor cores cut the sum off at every step of 16 of K, so the error grows with the steps in one accumulator: 3.6e-6 of the
+    // result (2-norms) after K = 4096, 7e-6 after 8192.  That is nothing beside a rounding to bf16 (1.7e-3).  Results in fp32 with
+    // a longer K have tiles of at most 128 tokens, which leave room for two accumulators that each take half of the steps (tiles
+    // of 64 have four): 3.7e-6 at K = 8192, at 1.5 times the time (2048 tokens, 14336 rows: 660 us, 438 with tiles of 256).
+    const int64_t widest = fp32 && k > kLtLongK ? 128 : kLtMaxN, most_n = (tokens + widest - 1) / widest;
     // the tokens are dealt evenly over the tiles, in multiples of 16
     const int64_t box = ((tokens + most_n - 1) / most_n + 15) & ~(int64_t)15, tiles_n = (tokens + box - 1) / box, tiles = tiles_m * tiles_n;
     if (tiles_m > (1 << 24) || tokens > 0x7fffff00 || k > 0x7fffff00 || tiles > 0x3fffffff || tiles * per_tile > 0x3fffffff) return false;
@@ -557,6 +578,7 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t 
     w.stages = room - 8 * stage >= 4 * kLtHalfBytes ? 8 : 4;
     w.halves = (room - w.stages * stage) / kLtHalfBytes & ~1;
     if (w.halves > kLtMaxHalves) w.halves = kLtMaxHalves;
+    w.accs = box <= 64 ? 4 : box <= 128 ? 2 : 1;
     // One CTA per SM, each with an equal part of the lines.  A tile is cut into at most so many parts that summing them
     // stays short beside the product: 16384 / tokens.
     const int64_t lines = tiles * per_tile, most = tiles * (16384 / box < 64 ? 16384 / box : 64);
@@ -578,8 +600,9 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t 
 
 size_t linear_tc_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, bool backward, int64_t capacity)
 {
-    LtPlan p;
-    return lt_plan(rows, cols, tokens, backward, capacity, &p) ? p.total : 0;
+    LtPlan p, q;  // for results in bf16 and in fp32
+    if (!lt_plan(rows, cols, tokens, backward, false, capacity, &p) || !lt_plan(rows, cols, tokens, backward, true, capacity, &q)) return 0;
+    return p.total > q.total ? p.total : q.total;
 }
 
 int linear_tc(const char* who, const LinearW& w, bool backward, const void* operand, int64_t ld, const LinearOut& out, int* status,
@@ -587,7 +610,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
 {
     LtPlan p;
     const bool opq = w.out_idx && w.capacity > 0;
-    if (!lt_plan(w.rows, w.cols, out.tokens, backward, opq ? w.capacity : 0, &p)) {
+    if (!lt_plan(w.rows, w.cols, out.tokens, backward, !out.y_bf16, opq ? w.capacity : 0, &p)) {
         set_error("%s: matrix or batch too large", who);
         return BOF4_ERR_SHAPE;
     }
