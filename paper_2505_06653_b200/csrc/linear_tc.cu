@@ -53,6 +53,7 @@ constexpr int kLtThreads = 32 * (kLtResults + 4);
 struct LtWork {
     int tiles, tiles_n, per_tile;  // tiles, those along the tokens, lines of a tile
     int box_n;                     // tokens of a tile, a multiple of 16
+    int k;                         // K
     int stages, halves;            // stages of A and B (4 or 8), half lines of codes (even)
     int accs;                      // accumulators of a part of a tile, which the instructions of a k-block use in turn: 4, 2 or 1
     int each, extra;               // lines per CTA, and the remainder
@@ -241,7 +242,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         // ---- producers
         const int group = warp >> 2, thread = (warp & 3) * 32 + lane;
         const int row = BWD ? thread & 63 : thread, half = BWD ? thread >> 6 : 0;  // of W within the k-block (backward), the tile (forward)
-        // Block constants, three lines ahead (past the end: the last ones again; outside the matrix: its last one): the index of the
+        // Block constants, three lines ahead (past the last line: its own again; rows of M outside the matrix: its last one): the index of the
         // thread's first weight of a line, and what a line further adds to it.
         TcConst<ST> c0, c1, c2, d0, d1, d2;
         int ct = tile0, ci = in0, unasked = lines;
@@ -253,8 +254,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         const int64_t line_step = BWD ? (int64_t)kLtGroups * kLtK * cols : kLtGroups * kLtK;
         auto constants = [&](TcConst<ST>& c, TcConst<ST>& d) {
             const int64_t b = weight >> block_shift;
-            c.load(scales, b < last_scale ? b : last_scale);
-            if (HALF) d.load(scales, b + 1 < last_scale ? b + 1 : last_scale);
+            // (past the end of K the constants are zero, as the operand is: a product of its zeros with another row's infinity or NaN
+            // would reach the sums)
+            const int k = (ci * kLtGroups + group) * kLtK + (BWD ? row : 0);
+            c.v = d.v = 0;
+            if (k < work.k) c.load(scales, b < last_scale ? b : last_scale);
+            if (HALF && k + (BWD ? 0 : 32) < work.k) d.load(scales, b + 1 < last_scale ? b + 1 : last_scale);
             if (--unasked <= 0) return;
             weight += line_step;
             if (++ci == per_tile) ci = 0, ++ct, weight = first_of(ct, 0);
@@ -572,6 +577,7 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp3
     w.tiles_n = (int)tiles_n;
     w.per_tile = (int)per_tile;
     w.box_n = (int)box;
+    w.k = (int)k;
     // Eight stages where they leave room for two lines of codes, four otherwise (256 tokens leave two lines beside them).
     w.table = box <= kLtTableN;
     const int room = kLtSmem - 1024 - (w.table ? kPairBytes : 0), stage = kLtABytes + (int)box * 128;

@@ -295,6 +295,29 @@ def test_non_finite_tokens_stay_by_themselves(bof4):
         assert not bool(torch.isfinite(y[1]).any()) and bool(torch.isnan(y[tokens - 1]).all())
 
 
+@pytest.mark.parametrize("tokens", [1, 12, 20, 300])
+@pytest.mark.parametrize("rows,cols,block", [(200, 96, 32), (131, 320, 64), (64, 64, 64), (300, 4096, 4096), (77, 8256, 64)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_non_finite_weights_stay_in_their_rows_and_columns(bof4, tokens, rows, cols, block, bad):
+    """Blocks whose constant is not finite reach the results of their own row (forward) and columns (backward), and no others:
+    what pads a matrix to whole tiles is zero."""
+    lv, codes, scales = integer_case(rows, cols, block, 6)
+    per_row, row = cols // block, rows // 2
+    scales[row * per_row] = scales[-1] = bad        # the first block of a row, and the last one of the matrix
+    w = decode(codes, scales, block, lv, rows, cols)
+    g = torch.Generator().manual_seed(tokens)
+    x, dy = ints(g, tokens, cols, lo=1, hi=2), ints(g, tokens, rows, lo=1, hi=2)
+    y, status = bof4.bof4_linear(codes, scales, rows, cols, block, lv, x, out_dtype=bof4.F32)
+    keep = [r for r in range(rows) if r not in (row, rows - 1)]
+    assert int(status.item()) == 0 and torch.equal(y[:, keep].double(), x.double() @ w[keep].T)
+    assert not bool(torch.isfinite(y[:, [row, rows - 1]]).any())
+    dx, _, status = bof4.bof4_linear_backward(codes, scales, rows, cols, block, lv, dy)
+    hit = torch.zeros(cols, dtype=torch.bool, device="cuda")
+    hit[:block] = hit[-block:] = True
+    assert int(status.item()) == 0 and torch.equal(dx[:, ~hit], (dy.double() @ w[:, ~hit]).bfloat16())
+    assert not bool(torch.isfinite(dx[:, hit]).any())
+
+
 def test_the_operand_is_what_dequantise_writes(bof4):
     """A run of the calls as they are used: quantise with outliers, one token and many through the layer, its gradient."""
     rows, cols, block = 256, 1024, 64

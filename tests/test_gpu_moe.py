@@ -197,6 +197,24 @@ def test_random_layers(bof4):  # noqa: F811
     assert done >= 10, done
 
 
+def test_other_experts_do_not_matter(bof4):  # noqa: F811
+    """Experts that nobody chose may hold anything, next to the chosen ones as they lie."""
+    experts, hidden, ffn, block = 8, 96, 160, 32
+    gate_up, down = layer(3, experts, hidden, ffn, block)
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(7, hidden, generator=g).bfloat16().cuda()
+    router = (torch.randn(experts, hidden, generator=g) * 0.1).bfloat16().cuda()
+    router[[1, 2, 4, 6, 7]] = 0
+    x[:, 0], router[:, 0] = 100.0, torch.tensor([1.0, -1, -1, 1, -1, 1, -1, -1], device="cuda").bfloat16()
+    y, ids, w, s = bof4.bof4_moe(x, router, gate_up, down, ffn, block, LV, 3)
+    assert sorted(set(ids.flatten().tolist())) == [0, 3, 5]
+    for bad in (float("inf"), float("nan")):
+        for scales, per in ((gate_up[1], 2 * ffn * hidden // block), (down[1], hidden * ffn // block)):
+            scales.view(experts, per)[[1, 2, 4, 6, 7]] = bad
+        y2, ids2, w2, s = bof4.bof4_moe(x, router, gate_up, down, ffn, block, LV, 3)
+        assert int(s.item()) == 0 and torch.equal(y, y2) and torch.equal(ids, ids2) and torch.equal(w, w2) and bool(torch.isfinite(y2.float()).all())
+
+
 def test_no_tokens(bof4):  # noqa: F811
     gate_up, down = layer(1, 4, 64, 64, 64)
     y, ids, w, s = bof4.bof4_moe(torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 64, device="cuda"), gate_up, down, 64, 64, LV, 2)
