@@ -390,8 +390,8 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
  *   z[t, r] = sum_c W^[r, c] x[t, c] + bias[r],   y[t, r] = act(z[t, r]) + residual[t, r]
  * with W rows x cols as for bof4_gemv (a block never straddles two rows).  Reading: W^ is the dequantised weight rounded to
  * bf16, bit for bit what bof4_dequantize writes, and the stored value where the outlier list has an entry; products are exact
- * and added up in fp32 (in an order that depends on shapes and types alone, so two calls on the same inputs give the same
- * bits); bias, activation and residual are applied in fp32; y is rounded once.  (bof4_gemv keeps the unrounded product
+ * and added up in fp32 (in an order that depends on shapes, types and whether there is a list alone, so two calls on the same
+ * inputs give the same bits); bias, activation and residual are applied in fp32; y is rounded once.  (bof4_gemv keeps the unrounded product
  * scale * level instead.)
  *   d_codes     device, rows * cols / 2 bytes, 32-byte aligned;  d_scales, d_codebook as for bof4_gemv
  *   d_x         device, bf16, token t at d_x + t * ldx, 16-byte aligned; ldx a multiple of 8
@@ -399,7 +399,8 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
  *   d_residual  device, values of y_dtype, token t at t * ld_residual, or NULL; may be d_y itself (with ld_residual = ldy)
  *   activation  BOF4_ACT_*
  *   d_out_idx / d_out_val / d_n_out / capacity   outlier list as for bof4_dequantize (ascending, distinct indices), or all
- *               NULL; with a list, rows * cols must fit 32-bit indices
+ *               NULL; with a list, rows * cols must fit 32-bit indices.  For few tokens an entry is a correction, (value - W^) x,
+ *               so a value of x that is not finite may give NaN there where value * x is infinite
  *   d_y         device, out, y_dtype (BOF4_BF16 or BOF4_F32), token t at t * ldy
  *   d_pre       device, out, bf16, token t at t * ld_pre: z, as bof4_linear_backward wants it where there is an
  *               activation; or NULL
@@ -456,7 +457,8 @@ BOF4_API size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_t 
  *   d_status    device int, written: 0, or 1 when a bounded wait inside the kernel ran out (y is then undefined)
  *   d_ws        device workspace of bof4_moe_workspace_bytes bytes, 256-byte aligned, any contents; two calls that may run
  *               at the same time must not share one
- * One cooperative launch (a CTA on every SM) on `stream`; no host synchronisation.
+ * One cooperative launch (a CTA on every SM) on `stream`; no host synchronisation.  It can be captured; after a status of 1 the
+ * workspace is filled with zeros before the same captured launch runs again.
  */
 BOF4_API int bof4_moe(const void* d_x, int64_t ldx, int64_t n_tokens, int64_t hidden, const void* d_router, int router_dtype, int n_experts,
                       int top_k, int score, int renormalize, float scale, const uint8_t* d_gate_up_codes, const void* d_gate_up_scales,

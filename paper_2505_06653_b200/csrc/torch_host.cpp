@@ -439,7 +439,7 @@ void check_matrix(const at::Tensor& codes, const at::Tensor& scales, int64_t row
     int64_t n = 0;
     if (rows < 0 || cols < 0 || __builtin_mul_overflow(rows, cols, &n) || codes.scalar_type() != at::kByte || codes.numel() * 2 != n)
         fail(PyExc_ValueError, "codes must be uint8 and hold rows * cols weights");
-    if (block < 1 || scales.numel() != n / block || scales.device() != codes.device())
+    if (block < 1 || block > INT32_MAX || scales.numel() != n / block || scales.device() != codes.device())
         fail(PyExc_ValueError, "scales must hold one constant per block, on the device of the codes");
 }
 void check_outliers(const Outliers& o, at::Device d)
