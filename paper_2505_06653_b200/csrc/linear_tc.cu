@@ -16,8 +16,10 @@
 // conversions for 64 weights) and keeps them in eight registers, the low bytes of the 16 bf16 values in four and the high
 // bytes in four.  A code is then looked up by byte permutes: four codes take two permutes of the lower and the upper eight
 // entries and one that picks between them by bit 3, for the low and for the high bytes, and two that put the bytes together.
-// That is 2.6 instructions per weight of the integer pipe and no shared memory; a table of level pairs in shared memory
-// (gemm_tc.cu) takes 4 bytes of its data path per weight, which the tensor cores need here for their own operands.
+// That is 2.6 instructions per weight of the integer pipe (3.0 with the making of the table: 390 to 420 cycles per k-block of
+// 128 x 64 weights) and no shared memory; a table of level pairs in shared memory (gemm_tc.cu) takes 4 bytes of its data path
+// per weight, which the tensor cores need here for their own operands.  Tiles of up to 64 tokens leave both the room and the
+// cycles for the table, and half of the codes go through it.
 //
 // The work is dealt as in gemm_tc.cu: lines (four k-blocks of 64 of K) of all tiles, tile after tile, in equal contiguous
 // parts to one CTA per SM; a tile that several CTAs share is summed in their order by the one that completes it last (a
@@ -29,6 +31,15 @@
 //   1 issuer      four tcgen05.mma (M = 128, N = tokens, K = 16) per k-block, tcgen05.commit hands the stage back
 //   1 tokens, 1 codes   TMA loads of the B operand, and of half lines of codes (128 rows of 64 bytes in both directions)
 //   4 results     read a finished accumulator (there are two) while the next tile runs
+//
+// A stage has one barrier that both operands complete, and is handed back by one commit; codes are handed back by half lines,
+// so that the ring needs 16 KiB less than whole lines would.
+//
+// What bounds it (profiles: 28672 x 8192 by 32 tokens, 14336 x 4096 by 2048): up to 64 tokens decoding, about 760 cycles per
+// k-block with shared memory and the integer pipe at 68 % each; at 256 tokens the data path of shared memory, through which both
+// operands go in and out: 832 cycles per k-block, of which the tensor cores need 512.  28672 x 8192: 24 tokens 86 us, 64 90, 128
+// 103, 256 122, 2048 870 (1107 TFLOP/s; the power limit holds the clock down).  Two SMs on one tile (cta_group::2, each decoding
+// half of it) took 1.7 times as long: the producers of both wait for one another at every stage.
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
 #include "decode.cuh"

@@ -415,6 +415,40 @@ def test_random_shapes_are_exact(bof4):
         assert int(s.item()) == 0 and torch.equal(dx, (dy.double() @ w).bfloat16()), (tokens, rows, cols, block)
 
 
+def test_offsets_beyond_32_bits(bof4):
+    """A matrix of more than 2^32 weights, results of more than 2^31 values: rows, tokens and columns at the far ends."""
+    rows, cols, block = 132000, 32768, 4096
+    g = torch.Generator(device="cuda").manual_seed(1)
+    lv = integer_case(1, 64, 64, 1)[0]
+    codes = torch.randint(0, 256, (rows * cols // 2,), generator=g, dtype=torch.uint8, device="cuda")
+    scales = 2.0 ** torch.randint(-4, 2, (rows * cols // block,), generator=g, device="cuda").bfloat16()
+    some = [0, 65535, 65536, 131071, 131072, rows - 1]
+    w = torch.cat([decode(codes[r * cols // 2:(r + 1) * cols // 2], scales[r * cols // block:(r + 1) * cols // block], block, lv, 1, cols) for r in some])
+    for tokens in (1, 9, 20):
+        x = torch.randint(-1, 2, (tokens, cols), generator=g, device="cuda").bfloat16()
+        x[:, :28672] = 0  # (the sums stay exact)
+        y, status = bof4.bof4_linear(codes, scales, rows, cols, block, lv, x, out_dtype=bof4.F32)
+        assert int(status.item()) == 0 and torch.equal(y[:, some].double(), x.double() @ w.T)
+    dy = torch.zeros(20, rows, dtype=torch.bfloat16, device="cuda")
+    dy[:, some] = torch.randint(-2, 3, (20, len(some)), generator=g, device="cuda").bfloat16()
+    dx, db, status = bof4.bof4_linear_backward(codes, scales, rows, cols, block, lv, dy, want_dbias=True)
+    assert int(status.item()) == 0 and torch.equal(dx, (dy[:, some].double() @ w).bfloat16()) and torch.equal(db, dy.float().sum(0))
+    del codes, scales, w, dy
+    tokens, rows, cols = 67000, 32768, 64
+    lv, codes, scales = integer_case(rows, cols, 64, 2)
+    w = decode(codes, scales, 64, lv, rows, cols)
+    x = torch.randint(-2, 3, (tokens, cols), generator=g, device="cuda").bfloat16()
+    y, status = bof4.bof4_linear(codes, scales, rows, cols, 64, lv, x)
+    some = [0, 65535, 65536, tokens - 1]
+    assert int(status.item()) == 0 and torch.equal(y[some], (x[some].double() @ w.T).bfloat16())
+    y.zero_()
+    y[some] = torch.randint(-1, 2, (len(some), rows), generator=g, device="cuda").bfloat16()
+    y[:, 4096:] = 0
+    dx, db, status = bof4.bof4_linear_backward(codes, scales, rows, cols, 64, lv, y.relu(), pre=y, activation=bof4.ACT_RELU, want_dbias=True)
+    assert int(status.item()) == 0 and torch.equal(dx[some], (y[some].relu().double() @ w).bfloat16()) and torch.equal(db, y[some].relu().float().sum(0))
+    assert int(torch.count_nonzero(dx)) == int(torch.count_nonzero(dx[some]))
+
+
 def test_refusals(bof4):
     rows, cols = 8, 128
     lv, codes, scales = integer_case(rows, cols, 64, 1)

@@ -215,6 +215,22 @@ def test_other_experts_do_not_matter(bof4):  # noqa: F811
         assert int(s.item()) == 0 and torch.equal(y, y2) and torch.equal(ids, ids2) and torch.equal(w, w2) and bool(torch.isfinite(y2.float()).all())
 
 
+def test_offsets_beyond_32_bits(bof4):  # noqa: F811
+    """Experts of more than 2^32 weights together; the last ones are chosen."""
+    experts, hidden, ffn, block = 512, 2112, 2112, 64
+    g = torch.Generator(device="cuda").manual_seed(9)
+
+    def matrix(n):
+        codes = torch.randint(0, 256, (n // 2,), generator=g, dtype=torch.uint8, device="cuda")
+        return codes, (0.04 + 0.02 * torch.rand(n // block, generator=g, device="cuda")).bfloat16()
+    gate_up, down = matrix(experts * 2 * ffn * hidden), matrix(experts * hidden * ffn)
+    x = torch.randn(5, hidden, generator=g, device="cuda").bfloat16()
+    router = (torch.randn(experts, hidden, generator=g, device="cuda") * 1.5 / math.sqrt(hidden)).bfloat16()
+    x[:, 0], router[:, 0], router[[0, 300, 509, 511], 0] = 32.0, 0.0, 1.0
+    y, ids, w = check(bof4, x, router, gate_up, down, ffn, block, 4)
+    assert sorted(set(ids.flatten().tolist())) == [0, 300, 509, 511]
+
+
 def test_no_tokens(bof4):  # noqa: F811
     gate_up, down = layer(1, 4, 64, 64, 64)
     y, ids, w, s = bof4.bof4_moe(torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 64, device="cuda"), gate_up, down, 64, 64, LV, 2)
