@@ -36,12 +36,13 @@ namespace bof4 {
 constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMoeTokens = 64, kMoeExperts = 512, kMoeTop = 16;
 constexpr int kMoePitch = 20;      // sums of a column, 16 rows, and room that keeps the columns of a quad in different banks
-constexpr int kMoeDefer = 16;      // at most so many units between two additions over the stripes
+constexpr int kMoeWait = 16;       // columns of a row group that wait for the addition over the stripes
 constexpr int kMoeRing = kMoeWarps * kFewSlots * kFewUnit;
-constexpr int kMoeSums = 40960;    // two buffers of sums, [unit][warp][column][row], or the router's partial sums
-static_assert(kMoeSums + 24576 <= (int)kFewTable, "the sums lie before the table, behind 24 KiB of other variables");
+constexpr int kMoeRoom = kMoeWait * kMoePitch;               // sums of a warp: of as many columns
+constexpr int kMoeSums = 2 * kMoeWarps * kMoeRoom * 4;       // two buffers of them, [warp][column][row]; or the router's partial sums
+static_assert(kMoeSums + 20480 <= (int)kFewTable, "the sums lie before the table, behind 20 KiB of other variables");
 static_assert((kMoeExperts * (kMoeTokens / 4) / kSMs + 1) * kMoeWarps * 16 <= kMoeSums, "router");
-constexpr int kMoeBegin = 21504;   // dynamic memory begins there or later (behind 20.6 KiB of other variables)
+constexpr int kMoeBegin = 17408;   // dynamic memory begins there or later (behind 16.6 KiB of other variables)
 constexpr int kMoeSmem = (int)kFewRing + kMoeRing - kMoeBegin;
 constexpr int kMoeChoices = kMoeTokens * kMoeTop;
 constexpr uint32_t kMoeSpin = 1u << 22;
@@ -90,7 +91,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     float* const s_part = reinterpret_cast<float*>(s_dyn);
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ __align__(8) unsigned long long s_full[kMoeWarps][kFewSlots];
-    __shared__ int4 s_what[2][kMoeDefer][kMoeWarps];  // of the units whose parts wait: first row, first place in the list, columns
+    __shared__ int2 s_what[2][kMoeWarps][kMoeWait];  // of the columns whose parts wait, by row group: tile of rows, choice
     __shared__ __align__(16) uint16_t s_id[kMoeChoices];  // expert of choice t * top + j
     __shared__ uint16_t s_list[kMoeChoices];     // choices, by expert
     __shared__ int s_count[kMoeExperts];         // choices of an expert, then its first place in the list
@@ -331,7 +332,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         const bool busy = group < groups;
         const int total = units[chosen], all = grid * groups, each = total / all, extra = total % all;
         auto start_of = [&](int k) { return k * each + min(k, extra); };  // first unit of row group k of the grid
-        const int group0 = (int)blockIdx.x * groups, steps = each + (group0 < extra);  // the CTA's first group has the most
+        const int group0 = (int)blockIdx.x * groups;
         const int begin = busy ? start_of(group0 + group) : 0, mine = busy ? start_of(group0 + group + 1) - begin : 0;
         // a place in the order of units: expert (of the chosen ones), pass over its tokens, tile of its rows, round over the stripes
         struct Place {
@@ -399,76 +400,70 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                 if (k < kFewAhead) (void)tc_wait(smem_u32(&s_full[warp][slot_after(k)]), slot + k >= kFewSlots ? parity ^ 1u : parity);
             return false;
         }
-        // columns that a part has, down after the two halves of h have been added up, and units between two additions over the stripes
-        const int columns = min(PASS, p.tokens), size = columns * kMoePitch, defer = min(kMoeDefer, kMoeSums / (2 * kMoeWarps * size * 4));
-        int k = 0, buf = 0, have_i = -1, have_pass = -1;  // whose tokens xr holds
+        // Sums of a unit's columns wait until no room is left for those of the next one; then the stripes of the row group meet and add them
+        // up.  (Row groups have their own barriers and cadence.  With one of the whole CTA, at places that suited the unit with the most
+        // columns it took longer.)
+        int cols_waiting = 0, buf = 0, have_i = -1, have_pass = -1;  // whose tokens xr holds
         uint32_t xr[1][32];
-        for (int s = 0; s < steps; ++s) {
+        for (int s = 0; s < mine; ++s) {
             float acc[1][4] = {};
-            if (s < mine) {
-                if (stripe == 0 && lane == 0) s_what[buf][k][group] = make_int4(now.tile, s_first[now.i] + now.pass * PASS, columns_of(now), 0);
-                for (int round = 0; round < rounds; ++round) {
-                    __syncwarp();  // all lanes have read the slot that is asked for now
-                    request(slot_after(kFewAhead), m[kFewAhead]);
-                    if (rounds > 1 || now.i != have_i || now.pass != have_pass) {
-                        have_i = now.i, have_pass = now.pass;
-                        const int c0 = (round * wide + stripe) * kFewStripe + 64 * q, col = SECOND ? g & 3 : g;
-                        const bool live = col < columns_of(now);
-                        const int a = live ? s_list[s_first[now.i] + now.pass * PASS + col] : 0;
-                        const uint16_t* src = SECOND ? (g < 4 ? p.h_hi : p.h_lo) + (int64_t)a * ffn : p.x + (int64_t)(a / p.top) * p.ldx;
-                        few_tokens(xr[0], src + c0, live && c0 < cols, live && c0 + 32 < cols);
-                    }
-                    if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
-                    FewCodes code;
-                    few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
-                    few_multiply<ST, HALF, 1>(code, m[0], xr, acc, column, s_levels);
-                    if (++slot == kFewSlots) slot = 0, parity ^= 1u;
-#pragma unroll
-                    for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
-                    step_on(now);
+            const int columns = min(columns_of(now), PASS), place = s_first[now.i] + now.pass * PASS;
+            if (stripe == 0 && lane < columns) s_what[buf][group][cols_waiting + lane] = make_int2(now.tile, s_list[place + lane]);
+            for (int round = 0; round < rounds; ++round) {
+                __syncwarp();  // all lanes have read the slot that is asked for now
+                request(slot_after(kFewAhead), m[kFewAhead]);
+                if (rounds > 1 || now.i != have_i || now.pass != have_pass) {
+                    have_i = now.i, have_pass = now.pass;
+                    const int c0 = (round * wide + stripe) * kFewStripe + 64 * q, col = SECOND ? g & 3 : g;
+                    const bool live = col < columns;
+                    const int a = live ? s_list[place + col] : 0;
+                    const uint16_t* src = SECOND ? (g < 4 ? p.h_hi : p.h_lo) + (int64_t)a * ffn : p.x + (int64_t)(a / p.top) * p.ldx;
+                    few_tokens(xr[0], src + c0, live && c0 < cols, live && c0 + 32 < cols);
                 }
-            } else if (busy && stripe == 0 && lane == 0) {
-                s_what[buf][k][group] = make_int4(0, 0, 0, 0);
+                if (!failed && !tc_wait(smem_u32(&s_full[warp][slot]), parity)) failed = true;
+                FewCodes code;
+                few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
+                few_multiply<ST, HALF, 1>(code, m[0], xr, acc, column, s_levels);
+                if (++slot == kFewSlots) slot = 0, parity ^= 1u;
+#pragma unroll
+                for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
+                step_on(now);
             }
             if (SECOND) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[0][v] += __shfl_xor_sync(kFull, acc[0][v], 2);  // columns c and c + 4
+                for (int v = 0; v < 4; ++v) acc[0][v] += __shfl_xor_sync(kFull, acc[0][v], 2);  // columns c and c + 4: the two halves of h
             }
-            float* const to = s_part + ((buf * defer + k) * kMoeWarps + warp) * size + 2 * q * kMoePitch + g;
+            float* const to = s_part + (buf * kMoeWarps + warp) * kMoeRoom + (cols_waiting + 2 * q) * kMoePitch + g;
             if (2 * q < columns) to[0] = acc[0][0], to[8] = acc[0][2];
             if (2 * q + 1 < columns) to[kMoePitch] = acc[0][1], to[kMoePitch + 8] = acc[0][3];
-            if (k == defer - 1 || s + 1 == steps) {
-                __syncthreads();
-                // results of k + 1 units of each group, rows along the lanes
-                constexpr int ROWS = SECOND ? 16 : 8;
-                for (uint32_t e = (uint32_t)tid; e < (uint32_t)((k + 1) * groups * columns * ROWS); e += kMoeThreads) {
-                    const uint32_t row = e % ROWS, rest = e / ROWS, unit = rest / (uint32_t)columns, col = rest - unit * (uint32_t)columns;
-                    const uint32_t j = unit / (uint32_t)groups, gr = unit - j * (uint32_t)groups;
-                    const int4 what = s_what[buf][j][gr];
-                    if ((int)col >= what.z) continue;
-                    const int a = s_list[what.y + (int)col];
-                    const float* part = s_part + ((buf * defer + j) * kMoeWarps + gr * wide) * size + col * kMoePitch + row;
-                    float v0 = 0.0f, v1 = 0.0f;
+            cols_waiting += columns;
+            if (s + 1 < mine && cols_waiting + min(columns_of(now), PASS) <= kMoeWait) continue;
+            if (wide > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(wide * 32) : "memory");
+            else __syncwarp();
+            // rows along the lanes
+            constexpr int ROWS = SECOND ? 16 : 8;
+            for (int e = stripe * 32 + lane; e < cols_waiting * ROWS; e += wide * 32) {
+                const int row = e % ROWS, col = e / ROWS;
+                const int2 what = s_what[buf][group][col];
+                const float* part = s_part + (buf * kMoeWarps + group * wide) * kMoeRoom + col * kMoePitch + row;
+                float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll 4
-                    for (int w = 0; w < wide; ++w) {
-                        v0 += part[w * size];
-                        if (!SECOND) v1 += part[w * size + 8];
-                    }
-                    if (SECOND) {
-                        p.out[(int64_t)a * hidden + what.x * 16 + (int)row] = v0;
-                    } else {
-                        const float h = activate(v0, p.act) * v1;
-                        const uint16_t hi = bf16_round(h);
-                        const int64_t o = (int64_t)a * ffn + what.x * 8 + (int)row;
-                        p.h_hi[o] = hi;
-                        p.h_lo[o] = bf16_round(isfinite(h) ? h - bf16_value(hi) : 0.0f);
-                    }
+                for (int w = 0; w < wide; ++w) {
+                    v0 += part[w * kMoeRoom];
+                    if (!SECOND) v1 += part[w * kMoeRoom + 8];
                 }
-                buf ^= 1;
-                k = 0;
-            } else {
-                ++k;
+                if (SECOND) {
+                    p.out[(int64_t)what.y * hidden + what.x * 16 + row] = v0;
+                } else {
+                    const float h = activate(v0, p.act) * v1;
+                    const uint16_t hi = bf16_round(h);
+                    const int64_t o = (int64_t)what.y * ffn + what.x * 8 + row;
+                    p.h_hi[o] = hi;
+                    p.h_lo[o] = bf16_round(isfinite(h) ? h - bf16_value(hi) : 0.0f);
+                }
             }
+            buf ^= 1;
+            cols_waiting = 0;
         }
         if (failed) atomicExch(p.status, 1);
         return true;
