@@ -80,6 +80,7 @@ __device__ __forceinline__ uint32_t moe_key(float v)
     const uint32_t b = __float_as_uint(v + 0.0f);  // -0 counts as +0
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float moe_unkey(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 
 template <class ST, bool HALF>
 __global__ void __launch_bounds__(kMoeThreads, 1)
@@ -199,45 +200,54 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     for (int t = warp; t < p.tokens; t += kMoeWarps) {
         constexpr int R = kMoeExperts / 32;
         float s[R];
-        uint32_t free = 0u;  // experts of this lane that have not been taken
         float most = -INFINITY;
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            if (k >= ranks) continue;
+            if (k >= ranks) break;
             const int e = k * 32 + lane;
             s[k] = e < p.experts ? __ldcg(p.logits + t * p.experts + e) : 0.0f;
-            if (e < p.experts) free |= 1u << k;
         }
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-            if (k < ranks && (free >> k & 1u)) most = fmaxf(most, s[k]);
         float total = 0.0f;
         if (p.score == BOF4_SCORE_SOFTMAX) {
 #pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (k >= ranks) break;
+                if (k * 32 + lane < p.experts) most = fmaxf(most, s[k]);
+            }
+#pragma unroll
             for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
 #pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (k < ranks && (free >> k & 1u)) total += expf(s[k] - most);
+            for (int k = 0; k < R; ++k) {
+                if (k >= ranks) break;
+                if (k * 32 + lane < p.experts) total += expf(s[k] - most);
+            }
             total = moe_sum(total);
         }
-        float mine = 0.0f;  // lane j: the score of choice j
+        // the lane's experts as keys, 0 for one that is taken, and the first of its largest ones: only the lane whose expert is taken
+        // looks for its next one
+        uint32_t key[R], best = 0u, which = 0u;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k >= ranks) break;
+            const int e = k * 32 + lane;
+            key[k] = e < p.experts ? max(moe_key(s[k]), 1u) : 0u;
+            if (key[k] > best) best = key[k], which = (uint32_t)e;
+        }
+        float mine = 0.0f;  // lane j: the logit of choice j, then its score
         int chosen_e = 0;   // and which it is
         for (int j = 0; j < p.top; ++j) {
             // the largest remaining logit, then the lowest index
-            uint32_t best = 0u, which = 0xffffffffu;
-            float value = 0.0f;
+            const uint32_t top = __reduce_max_sync(kFull, best), e = __reduce_min_sync(kFull, best == top ? which : 0xffffffffu);
+            if (lane == j) mine = moe_unkey(top), chosen_e = (int)e;
+            if ((e & 31u) == (uint32_t)lane) {
+                best = 0u;
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                if (k >= ranks) continue;
-                const uint32_t key = moe_key(s[k]);
-                if ((free >> k & 1u) && (which == 0xffffffffu || key > best)) best = key, which = (uint32_t)(k * 32 + lane), value = s[k];
+                for (int k = 0; k < R; ++k) {
+                    if (k >= ranks) break;
+                    if ((uint32_t)k == e >> 5) key[k] = 0u;
+                    if (key[k] > best) best = key[k], which = (uint32_t)(k * 32 + lane);
+                }
             }
-            const bool any = which != 0xffffffffu;
-            const uint32_t top = __reduce_max_sync(kFull, any ? best : 0u);
-            const int e = (int)__reduce_min_sync(kFull, any && best == top ? which : 0xffffffffu);
-            value = __shfl_sync(kFull, value, e & 31);
-            if ((e & 31) == lane) free &= ~(1u << (e >> 5));
-            if (lane == j) mine = value, chosen_e = e;
         }
         if (lane < p.top) mine = p.score == BOF4_SCORE_SOFTMAX ? expf(mine - most) / total : 1.0f / (1.0f + expf(-mine));
         else mine = 0.0f;
