@@ -408,7 +408,8 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
  *   d_ws        device workspace of bof4_linear_workspace_bytes(rows, cols, n_tokens, 0, capacity) bytes, 256-byte aligned,
  *               any contents; two calls that may run at the same time must not share one
  * Row strides are in elements and do not matter where n_tokens is 1.  Outputs must not overlap inputs but as said.
- * No host synchronisation.
+ * No host synchronisation.  The call can be captured; after a status of 1 the workspace is filled with zeros before the same
+ * captured launches run again.
  */
 BOF4_API int bof4_linear(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size,
                          const float* d_codebook, const void* d_x, int64_t ldx, int64_t n_tokens, const void* d_bias, int bias_dtype,

@@ -12,7 +12,7 @@
 // is a part; a launch of their own would cost more, and would have to build the table of level pairs anew):
 //
 //   router   a job per expert and four tokens, its columns over several warps; 4 us for 64 experts of 2048 columns
-//   gate/up  every CTA works the choice out for itself (a warp per token), then lists the chosen experts with their tokens; 4 us.
+//   gate/up  every CTA works the choice out for itself (a warp per token), then lists the chosen experts with their tokens; 3 us.
 //            Units of eight rows of G with the same eight of U (one 16-row product of decode.cuh, so that a lane holds
 //            both halves of h) are dealt in equal contiguous runs over the row groups of the grid
 //   down     units of 16 rows of D, the two halves of h as separate columns of the product
@@ -21,8 +21,9 @@
 // A unit's columns are split over the stripes of a row group (a warp each, 256 columns; several stripes a warp where a row is
 // longer than a CTA has warps for) and its parts are added up in shared memory in a fixed order: no sum depends on scheduling.
 //
-// One token, 64 experts of 2048 x 1408 with eight chosen: 33 us, mostly latency; 19 tokens, 128 experts: 144 us, 1670 GB/s, bound by
-// decoding (decode.cuh) and by experts whose tokens need more than one pass.
+// One token, 64 experts of 2048 x 1408, six chosen: 32 us, mostly latency.  19 tokens, 128 experts of 2048 x 768, eight chosen: 137 us,
+// 1760 GB/s, of them router and its barrier 11, choice and list 6, gate/up 68, down 33, two barriers with the waiting for the slowest CTA
+// 12, sums 2.  The walks are bound by decoding (decode.cuh), 15 to 16 codes per clock and SM.
 //
 // The waits on the barrier are bounded: a time-out sets the status word and everybody leaves.
 #include <type_traits>
