@@ -96,7 +96,7 @@ __device__ __forceinline__ void fill_pairs(float2* pairs, const float* __restric
 // bytes of its data path per code (32 codes per clock at most) and one instruction of the integer pipe, byte permutes take 2.9 of
 // that pipe (22 per clock).  Three quarters of the codes go through the table, the last 32 columns of row 8 + g
 // through permutes: 42 per clock for the one, 40 for the other.  Together with the conversions (each code one half), addresses and
-// products an SM reaches 22 to 25 (28672 x 8192 by one token 42 us: shared memory 64 %, integer pipe 66 %, issue 60 %).
+// products an SM reaches 18 to 20 (28672 x 8192 by one token 42 us: shared memory 64 %, integer pipe 66 %, issue 60 %).
 
 constexpr int kFewStripe = 256;
 

@@ -231,6 +231,29 @@ def test_offsets_beyond_32_bits(bof4):  # noqa: F811
     assert sorted(set(ids.flatten().tolist())) == [0, 300, 509, 511]
 
 
+def test_two_layers_at_once(bof4):  # noqa: F811
+    """Calls on two streams, with workspaces of their own, and a dense layer on a third: none waits for another in vain."""
+    g = torch.Generator().manual_seed(12)
+    experts, hidden, ffn = 16, 2048, 1024
+    gate_up, down = layer(12, experts, hidden, ffn, 64)
+    router = (torch.randn(experts, hidden, generator=g) * 0.05).bfloat16().cuda()
+    xs = [torch.randn(n, hidden, generator=g).bfloat16().cuda() for n in (3, 40)]
+    x = torch.randn(300, hidden, generator=g).bfloat16().cuda()
+    want = [bof4.bof4_moe(t, router, gate_up, down, ffn, 64, LV, 4)[0] for t in xs]
+    dense = bof4.bof4_linear(*gate_up, experts * 2 * ffn, hidden, 64, LV, x)[0]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(3)], []
+    for _ in range(10):
+        for t, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                got.append(bof4.bof4_moe(t, router, gate_up, down, ffn, 64, LV, 4))
+        with torch.cuda.stream(streams[2]):
+            got.append(bof4.bof4_linear(*gate_up, experts * 2 * ffn, hidden, 64, LV, x))
+    torch.cuda.synchronize()
+    for i, r in enumerate(got):
+        assert int(r[-1].item()) == 0 and torch.equal(r[0], (want + [dense])[i % 3])
+
+
 def test_no_tokens(bof4):  # noqa: F811
     gate_up, down = layer(1, 4, 64, 64, 64)
     y, ids, w, s = bof4.bof4_moe(torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 64, device="cuda"), gate_up, down, 64, 64, LV, 2)
