@@ -186,7 +186,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
 // Outliers: correction[t, r] = sum over the entries of row r of (val - W^) x[t, c], zero elsewhere (set before).  A CTA takes 256
 // entries: their changes, a term per entry and token, and a row's terms added up in the order of the list; what is left of a row
 // more than 64 entries behind them comes from global memory.
-constexpr int kFewTokens = 16;
+constexpr int kFewTokens = 16, kFewListTokens = 6;  // tokens of a call, without and with a list
 template <class ST>
 __device__ __forceinline__ float scale_at(const void* scales, int64_t b)
 {
@@ -200,7 +200,7 @@ few_correction_kernel(const uint8_t* __restrict__ codes, const void* __restrict_
 {
     if (!after_previous()) return;
     constexpr int N = 256 + 64;  // the CTA's entries, and those behind them that may belong to its last row
-    __shared__ float s_term[N][kFewTokens + 1], s_change[N];
+    __shared__ float s_term[N][kFewListTokens + 1], s_change[N];
     __shared__ int s_row[N], s_col[N];
     int64_t k_end = *n_out;
     if (k_end > capacity) k_end = capacity;
@@ -298,7 +298,7 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
 // and less here (8192 x 8192 with 65,536: 34 us against 42 for four tokens, 60 against 42 for twelve).
 bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list)
 {
-    return tokens <= (list ? 6 : kFewTokens) && cols <= 32768 && rows <= (1 << 26);
+    return tokens <= (list ? kFewListTokens : kFewTokens) && cols <= 32768 && rows <= (1 << 26);
 }
 
 size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity) { return few_plan(rows, cols, tokens, capacity > 0).total; }
