@@ -289,3 +289,22 @@ def test_refusals(bof4):  # noqa: F811
     bad(TypeError, out=torch.zeros(2, hidden, device="cuda"))
     need = bof4.bof4_moe_workspace_bytes(2, hidden, ffn, experts, 2)
     bad(bof4.Bof4Error, workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens,hidden,ffn", [(3, 8192, 5120), (20, 4608, 8448)])
+def test_cold_memory(bof4, tokens, hidden, ffn):  # noqa: F811
+    """Rows of more columns than a CTA has warps for, so that a unit takes several turns of the ring of codes, from memory that has
+    left L2: the same bits as the first time, whatever the workspace holds."""
+    experts, top, block = 4, 2, 64
+    g = torch.Generator().manual_seed(tokens)
+    gate_up, down = layer(hidden, experts, hidden, ffn, block)
+    x = torch.randn(tokens, hidden, generator=g).bfloat16().cuda()
+    router = (torch.randn(experts, hidden, generator=g) * 1.5 / math.sqrt(hidden)).bfloat16().cuda()
+    y, ids, w = check(bof4, x, router, gate_up, down, ffn, block, top)
+    big = torch.empty(300 << 20, dtype=torch.uint8, device="cuda")
+    n = bof4.bof4_moe_workspace_bytes(tokens, hidden, ffn, experts, top)
+    for trial in range(12):
+        ws = torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda")
+        big.fill_(trial)
+        y2, ids2, w2, s = bof4.bof4_moe(x, router, gate_up, down, ffn, block, LV, top, out_dtype=bof4.F32, workspace=ws)
+        assert int(s.item()) == 0 and torch.equal(y2, y) and torch.equal(ids2, ids) and torch.equal(w2, w)
