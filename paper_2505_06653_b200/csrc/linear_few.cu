@@ -83,7 +83,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     int left = (int)(rows - (int64_t)first * 16) - g, row = first * 16, asked = 0;
     FewConst<ST, HALF> m[kFewAhead + 1];  // of the next units, the oldest first
     auto request = [&](int slot, FewConst<ST, HALF>& c) {
-        if (asked < mine && lane == 0)
+        if (asked < mine && lane == 0 && !failed)
             tc_load_box(ring + (uint32_t)(slot * kFewUnit), &code_map, &s_full[warp][slot], kFewUnit, (int)(c0 >> 1), row);
         c.load(scales, at, at + 8 * per_row, ((left > 0 ? 3u : 0u) | (left > 8 ? 12u : 0u)) & lanes);
         ++asked, row += step * 16, left -= step * 16, at += jump;
@@ -148,7 +148,10 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
 #pragma unroll
         for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
     }
-    if (failed) atomicExch(status, 1);
+    if (failed) {  // nothing was asked for since; what was before must not reach shared memory after the CTA has left
+        atomicExch(status, 1);
+        tc_settle();
+    }
     if (work.slices == 1) return;
     __threadfence();
     __syncthreads();

@@ -503,10 +503,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (s_fail) {
-        // copies and tensor-core instructions issued before the time-out may still be under way: they take
-        // microseconds; give them a bounded 100 before shared and tensor memory go away
         if (tid == 0) atomicExch(status, 1);
-        for (int i = 0; i < 100; ++i) __nanosleep(1000);
+        tc_settle();
     }
     for (int k = 0; k < s_sums; ++k) {  // the parts in the order of the CTAs; all but the first begin inside the tile
         const int tile = s_sum[k], t0 = tile * per_tile, i0 = work.owner(t0), more = work.owner(t0 + per_tile - 1) - i0;

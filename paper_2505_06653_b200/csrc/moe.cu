@@ -379,7 +379,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         auto request = [&](int k, FewConst<ST, HALF>& c) {
             const bool ok = asked < mine * rounds;
             const int c0 = (ask.round * wide + stripe) * kFewStripe, cc = c0 + 64 * q;
-            if (ok && lane == 0) {
+            if (ok && lane == 0 && !failed) {
                 const uint32_t bar = smem_u32(&s_full[warp][k]), dst = ring + (uint32_t)(k * kFewUnit);
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)kFewUnit) : "memory");
 #pragma unroll
@@ -408,7 +408,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         for (int k = 0; k < kFewAhead; ++k) request(slot_after(k), m[k]);
         if (!before()) {  // nothing of this CTA may be on its way when it ends
             for (int k = 0; k < min(asked, mine * rounds); ++k)
-                if (k < kFewAhead) (void)tc_wait(smem_u32(&s_full[warp][slot_after(k)]), slot + k >= kFewSlots ? parity ^ 1u : parity);
+                if (k < kFewAhead && !failed) (void)tc_wait(smem_u32(&s_full[warp][slot_after(k)]), slot + k >= kFewSlots ? parity ^ 1u : parity);
             return false;
         }
         // Sums of a unit's columns wait until no room is left for those of the next one; then the stripes of the row group meet and add them
@@ -480,7 +480,10 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
             buf ^= 1;
             cols_waiting = 0;
         }
-        if (failed) atomicExch(p.status, 1);
+        if (failed) {  // nothing was asked for since; what was before must not reach shared memory after the CTA has left
+            atomicExch(p.status, 1);
+            tc_settle();
+        }
         return true;
     };
     if (!walk(std::false_type{}, [] { return true; })) return;

@@ -46,6 +46,13 @@ __device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity)
     return false;
 }
 
+// After a wait has run out: copies and tensor-core instructions that were issued before may still be under way.  They take
+// microseconds; they get a bounded 100 before shared and tensor memory go away.
+__device__ __forceinline__ void tc_settle()
+{
+    for (int i = 0; i < 100; ++i) __nanosleep(1000);
+}
+
 // A look at a barrier, without a wait.
 __device__ __forceinline__ bool tc_look(uint32_t bar, uint32_t parity)
 {
