@@ -250,8 +250,13 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                 }
             }
         }
-        if (lane < p.top) mine = p.score == BOF4_SCORE_SOFTMAX ? expf(mine - most) / total : 1.0f / (1.0f + expf(-mine));
-        else mine = 0.0f;
+        // Scores that are divided by their sum may have a common factor: where the token's largest logit `lead` is negative the logistic ones
+        // are exp(l) / (1 + exp(l)) with exp(lead) taken out, so that the largest is at least 1/2.  (1 / (1 + exp(-l)) is 0 for l < -88.7.)
+        const float lead = p.score == BOF4_SCORE_SIGMOID && p.renormalize ? fminf(__shfl_sync(kFull, mine, 0), 0.0f) : 0.0f;
+        if (lane >= p.top) mine = 0.0f;
+        else if (p.score == BOF4_SCORE_SOFTMAX) mine = expf(mine - most) / total;
+        else if (lead < 0.0f) mine = expf(mine - lead) / (1.0f + expf(mine));
+        else mine = 1.0f / (1.0f + expf(-mine));
         if (p.renormalize) mine /= moe_sum(mine);
         if (lane < p.top) {
             const int a = t * p.top + lane;

@@ -308,3 +308,34 @@ def test_cold_memory(bof4, tokens, hidden, ffn):  # noqa: F811
         big.fill_(trial)
         y2, ids2, w2, s = bof4.bof4_moe(x, router, gate_up, down, ffn, block, LV, top, out_dtype=bof4.F32, workspace=ws)
         assert int(s.item()) == 0 and torch.equal(y2, y) and torch.equal(ids2, ids) and torch.equal(w2, w)
+
+
+@pytest.mark.parametrize("router_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("first,step", [(-90, 1), (-88, 1), (-100, 7), (-200, 30), (-1, 30), (-600, 1), (0, 60), (3, 40), (100, 64)])
+def test_logistic_scores_far_out(bof4, router_dtype, first, step):  # noqa: F811
+    """Weights that are divided by their sum depend on the differences of logits where all lie far below zero.  The logits are integers
+    that x picks out of the router, so a weight is off by a few units of exp, sum and quotient only: 2^-20 relative, or what fp32
+    cannot hold."""
+    experts, hidden, ffn, top = 9, 64, 64, 4
+    gate_up, down = layer(21, experts, hidden, ffn, 64)
+    g = torch.Generator().manual_seed(22)
+    x = torch.randn(3, hidden, generator=g).bfloat16().cuda()
+    x[:, :3] = torch.eye(3)
+    order = torch.randperm(experts, generator=g).cuda()
+    router = torch.zeros(experts, hidden, device="cuda")
+    router[order, 0] = first - step * torch.arange(experts, device="cuda").float()
+    router[:, 1], router[order, 2] = first, first - 2.0 * step * torch.arange(experts, device="cuda").float()
+    router = router.to(router_dtype)
+    assert torch.equal(x.double() @ router.double().T, router[:, :3].double().T.round())
+    y, ids, w, s = bof4.bof4_moe(x, router, gate_up, down, ffn, 64, LV, top, score=bof4.SCORE_SIGMOID, out_dtype=bof4.F32)
+    ry, tol, rids, rw, _ = reference(x, router, gate_up, down, ffn, 64, top, "silu", "sigmoid", True, 1.0, check_gap=False)
+    assert int(s.item()) == 0 and torch.equal(ids, rids)
+    assert bool(((w.double() - rw).abs() <= 2.0 ** -20 * rw + 1e-37).all()), (w, rw)
+    assert bool(((y.double() - ry).abs() <= tol + 1e-12).all())
+    _, _, one, _ = bof4.bof4_moe(x, router, gate_up, down, ffn, 64, LV, 1, score=bof4.SCORE_SIGMOID, scale=0.5)
+    assert bool((one == 0.5).all())
+    # an expert that is masked out has no weight beside one that is not
+    masked = router.clone()
+    masked[order[1:], 0] = -float("inf")
+    y, ids, w, s = bof4.bof4_moe(x[:1], masked, gate_up, down, ffn, 64, LV, top, score=bof4.SCORE_SIGMOID)
+    assert int(ids[0, 0]) == int(order[0]) and w[0].tolist() == [1.0, 0.0, 0.0, 0.0] and bool(torch.isfinite(y.float()).all())
