@@ -476,7 +476,8 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                     p.out[(int64_t)what.y * hidden + what.x * 16 + row] = v0;
                 } else {
                     const float h = activate(v0, p.act) * v1;
-                    const uint16_t hi = bf16_round(h);
+                    uint16_t hi = bf16_round(h);
+                    if (isfinite(h) && (hi & 0x7fffu) == 0x7f80u) --hi;  // above the largest bf16 value: that one, and the rest in the second half
                     const int64_t o = (int64_t)what.y * ffn + what.x * 8 + row;
                     p.h_hi[o] = hi;
                     p.h_lo[o] = bf16_round(isfinite(h) ? h - bf16_value(hi) : 0.0f);

@@ -339,3 +339,32 @@ def test_logistic_scores_far_out(bof4, router_dtype, first, step):  # noqa: F811
     masked[order[1:], 0] = -float("inf")
     y, ids, w, s = bof4.bof4_moe(x[:1], masked, gate_up, down, ffn, 64, LV, top, score=bof4.SCORE_SIGMOID)
     assert int(ids[0, 0]) == int(order[0]) and w[0].tolist() == [1.0, 0.0, 0.0, 0.0] and bool(torch.isfinite(y.float()).all())
+
+
+# Levels among which 0 and 1 are: matrices that pick single values out of their operand, and exact sums.
+PICK = np.array([-15, -13, -11, -9, -7, -5, -3, -1, 1, 3, 5, 7, 9, 11, 0, 16], np.float32) / 16
+ZERO, ONE = 14, 15
+
+
+def packed(codes, scale, block=64):
+    """(codes, scales) of a matrix of codes, all blocks with the same constant."""
+    c = codes.to(torch.uint8).reshape(-1, 2)
+    return ((c[:, 0] << 4) | c[:, 1]).cuda(), torch.full((codes.numel() // block,), scale).bfloat16().cuda()
+
+
+def test_h_beside_the_largest_values(bof4):  # noqa: F811
+    """h above the largest bf16 value but finite in fp32: both halves stay finite, and the product with a small weight is exact."""
+    hidden = ffn = 64
+    up = torch.full((2 * ffn, hidden), ZERO)
+    up[:ffn, :2], up[ffn:, 2] = ONE, ONE      # g = x0 + x1, u = x2
+    x = torch.zeros(4, hidden, dtype=torch.bfloat16, device="cuda")
+    x[:, 0], x[:, 1], x[:, 2] = 255 * 2.0 ** 57, 3 * 2.0 ** 55, 2.0 ** 63
+    x[1, 2], x[2, 1], x[3, 2] = -2.0 ** 63, 0.0, float("inf")
+    h = (x[:, 0].double() + x[:, 1].double()) * x[:, 2].double()
+    assert h[0] > 255.5 * 2.0 ** 120 and h[0] < 2.0 ** 128 and h[2] == 255 * 2.0 ** 120
+    down = torch.full((hidden, ffn), ZERO)
+    down[torch.arange(hidden), torch.arange(ffn)] = ONE
+    y, _, _, s = bof4.bof4_moe(x, torch.zeros(1, hidden, device="cuda"), packed(up, 1.0), packed(down, 2.0 ** -10), ffn, 64, PICK, 1, activation=bof4.ACT_NONE,
+                               out_dtype=bof4.F32)
+    assert int(s.item()) == 0 and torch.equal(y[:3].double(), (h[:3, None] * 2.0 ** -10).expand(3, hidden))
+    assert not bool(torch.isfinite(y[3]).any())
