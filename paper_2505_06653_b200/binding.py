@@ -488,7 +488,10 @@ def bof4_linear(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int,
                 workspace: Optional[torch.Tensor] = None):
     """y [n_tokens, rows] = act(x W^T + bias) + residual for x bf16 [n_tokens, cols] (rows of x, residual, pre and out may be
     apart from one another).  `pre` (bf16 [n_tokens, rows]) receives x W^T + bias, which bof4_linear_backward wants where there
-    is an activation.  -> (y, status int32[1]); status 0 unless a bounded wait inside the kernel ran out."""
+    is an activation.  -> (y, status int32[1]); status 0 unless a bounded wait inside the kernel ran out.
+
+    No autograd graph is recorded by this call and the two below: while gradients are on, a tensor that requires one is refused.
+    A layer that is trained through calls them from a torch.autograd.Function, in which gradients are off."""
     return _native().linear(codes, scales, rows, cols, block_size, levels, x, bias, residual, activation, out_dtype, pre, outliers, out,
                             workspace)
 

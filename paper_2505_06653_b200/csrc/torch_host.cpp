@@ -10,6 +10,7 @@
 // Other Python threads run while the library enqueues (a launch waits where the stream's queue is full) and while
 // memory is allocated (which may synchronise): what such a stretch uses is owned by this call, not borrowed
 // from a list that another thread may change.
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -19,7 +20,9 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <optional>
+#include <utility>
 #include <vector>
 
 #include "../../include/bof4.h"
@@ -450,9 +453,29 @@ void check_outliers(const Outliers& o, at::Device d)
         fail(PyExc_ValueError, "outliers must be (idx int32, val bfloat16, n_out int64[1]) on the device of the weights");
 }
 
+// The layers record no graph: with gradients on, a tensor that wants one would lose it without a word.  Names in the order of the arguments.
+void check_grad(const char* fn, PyObject* const* a, std::initializer_list<std::pair<int, const char*>> args)
+{
+    if (!at::GradMode::is_enabled()) return;
+    auto look = [&](PyObject* o, const char* name) {
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+            failf(PyExc_ValueError,
+                  "%s records no autograd graph and %s requires a gradient: call it under torch.no_grad(), or from a torch.autograd.Function", fn, name);
+    };
+    for (const auto& [k, name] : args) {
+        if (PyTuple_Check(a[k]) || PyList_Check(a[k])) {
+            Ref f(PySequence_Fast(a[k], name));
+            for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(f.p); ++i) look(PySequence_Fast_GET_ITEM(f.p, i), name);
+        } else {
+            look(a[k], name);
+        }
+    }
+}
+
 // (codes, scales, rows, cols, block_size, levels, x, bias, residual, activation, out_dtype, pre, outliers, out, workspace)
 PyObject* linear(PyObject* const* a)
 {
+    check_grad("bof4_linear", a, {{1, "scales"}, {5, "levels"}, {6, "x"}, {7, "bias"}, {8, "residual"}, {11, "pre"}, {12, "outliers"}, {13, "out"}});
     const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
     const int64_t rows = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
     check_matrix(codes, scales, rows, cols, block);
@@ -501,6 +524,7 @@ PyObject* linear(PyObject* const* a)
 // (codes, scales, rows, cols, block_size, levels, dy, pre, activation, want_dx, want_dbias, outliers, out, workspace)
 PyObject* linear_backward(PyObject* const* a)
 {
+    check_grad("bof4_linear_backward", a, {{1, "scales"}, {5, "levels"}, {6, "dy"}, {7, "pre"}, {11, "outliers"}, {12, "out"}});
     const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
     const int64_t rows = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
     check_matrix(codes, scales, rows, cols, block);
@@ -545,6 +569,7 @@ PyObject* linear_backward(PyObject* const* a)
 // (x, router, gate_up, down, ffn, block_size, levels, top_k, activation, score, renormalize, scale, out_dtype, out, workspace)
 PyObject* moe(PyObject* const* a)
 {
+    check_grad("bof4_moe", a, {{0, "x"}, {1, "router"}, {2, "gate_up"}, {3, "down"}, {6, "levels"}, {13, "out"}});
     const at::Tensor router = dev(a[1], "router");
     const at::Device d = router.device();
     if (router.dim() != 2 || tensor(a[0], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, hidden] and router [n_experts, hidden]");
