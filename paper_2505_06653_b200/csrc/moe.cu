@@ -41,7 +41,8 @@ constexpr int kMoeWait = 16;       // columns of a row group that wait for the a
 constexpr int kMoeRing = kMoeWarps * kFewSlots * kFewUnit;
 constexpr int kMoeRoom = kMoeWait * kMoePitch;               // sums of a warp: of as many columns
 constexpr int kMoeSums = 2 * kMoeWarps * kMoeRoom * 4;       // two buffers of them, [warp][column][row]; or the router's partial sums
-static_assert(kMoeSums + 20480 <= (int)kFewTable, "the sums lie before the table, behind 20 KiB of other variables");
+constexpr int kMoeUnread = 256;    // bytes before the table that are written and not read
+static_assert(kMoeSums + 20480 + kMoeUnread <= (int)kFewTable, "the sums lie before the table, behind 20 KiB of other variables");
 static_assert((kMoeExperts * (kMoeTokens / 4) / kSMs + 1) * kMoeWarps * 16 <= kMoeSums, "router");
 constexpr int kMoeBegin = 17408;   // dynamic memory begins there or later (behind 16.6 KiB of other variables)
 constexpr int kMoeSmem = (int)kFewRing + kMoeRing - kMoeBegin;
@@ -106,7 +107,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
     const uint32_t column = (uint32_t)lane * 8u + kFewTable;
     if (lane < kFewSlots) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_full[warp][lane])) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (smem_u32(s_dyn) < (uint32_t)kMoeBegin || smem_u32(s_dyn) + kMoeSums > kFewTable) {  // not the layout that this was built for: the same for all CTAs
+    if (smem_u32(s_dyn) < (uint32_t)kMoeBegin || smem_u32(s_dyn) + kMoeSums + kMoeUnread > kFewTable) {  // not the layout that this was built for: the same for all CTAs
         if (tid == 0 && blockIdx.x == 0) *p.status = 1;
         return;
     }
@@ -424,7 +425,6 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
         for (int s = 0; s < mine; ++s) {
             float acc[1][4] = {};
             const int columns = min(columns_of(now), PASS), place = s_first[now.i] + now.pass * PASS;
-            float* const to = s_part + (buf * kMoeWarps + warp) * kMoeRoom + (cols_waiting + 2 * q) * kMoePitch + g;
             if (stripe == 0 && lane < columns) s_what[buf][group][cols_waiting + lane] = make_int2(now.tile, s_list[place + lane]);
             for (int round = 0; round < rounds; ++round) {
                 __syncwarp();  // all lanes have read the slot that is asked for now
@@ -442,9 +442,8 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
                 few_read(code, ring + (uint32_t)(slot * kFewUnit), lane);
                 few_multiply<ST, HALF, 1>(code, m[0], xr, acc, column, s_levels);
                 // The slot is asked for again in the next round: by then its codes have to be in registers, not only their loads under way.
-                // A sum of this round depends on all of them, so it is stored where the unit's sums will be (the last round's are, below).
-                if (round + 1 < rounds && 2 * q < columns)
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem_u32(to)), "f"(acc[0][0]) : "memory");
+                // A sum of this round depends on all of them, so it is stored, where nobody reads it.  (The last round's sums are stored below.)
+                if (rounds > 1) asm volatile("st.shared.f32 [%0], %1;" ::"r"(column - kMoeUnread), "f"(acc[0][0]) : "memory");
                 if (++slot == kFewSlots) slot = 0, parity ^= 1u;
 #pragma unroll
                 for (int u = 0; u < kFewAhead; ++u) m[u] = m[u + 1];
@@ -454,6 +453,7 @@ moe_kernel(const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUt
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[0][v] += __shfl_xor_sync(kFull, acc[0][v], 2);  // columns c and c + 4: the two halves of h
             }
+            float* const to = s_part + (buf * kMoeWarps + warp) * kMoeRoom + (cols_waiting + 2 * q) * kMoePitch + g;
             if (2 * q < columns) to[0] = acc[0][0], to[8] = acc[0][2];
             if (2 * q + 1 < columns) to[kMoePitch] = acc[0][1], to[kMoePitch + 8] = acc[0][3];
             cols_waiting += columns;
