@@ -129,6 +129,19 @@ int64_t integer(PyObject* o)
     if (u == -1 && PyErr_Occurred()) throw PySet{};
     return u;
 }
+// An integer that the library takes as an int: none is cut off to another value.
+int small(PyObject* o, const char* name)
+{
+    const int64_t v = integer(o);
+    if (v < INT32_MIN || v > INT32_MAX) failf(PyExc_ValueError, "%s is out of range", name);
+    return (int)v;
+}
+bool truth(PyObject* o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw PySet{};
+    return v != 0;
+}
 double real(PyObject* o)
 {
     const double v = PyFloat_AsDouble(o);
@@ -483,7 +496,7 @@ PyObject* linear(PyObject* const* a)
     if (tensor(a[6], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, cols]");
     const int64_t n = tensor(a[6], "x").size(0);
     const Rows x(a[6], "x", n, cols, at::kBFloat16, d);
-    const int od = (int)integer(a[10]), act = (int)integer(a[9]), sd = dtype_code(scales);
+    const int od = small(a[10], "out_dtype"), act = small(a[9], "activation"), sd = dtype_code(scales);
     if (od != BOF4_F32 && od != BOF4_BF16) fail(PyExc_ValueError, "out_dtype must be F32 or BF16");
     const c10::cuda::CUDAGuard guard(d);
     const at::Tensor cb = codebook(a[5], d);
@@ -530,10 +543,10 @@ PyObject* linear_backward(PyObject* const* a)
     check_matrix(codes, scales, rows, cols, block);
     const at::Device d = codes.device();
     if (tensor(a[6], "dy").dim() != 2) fail(PyExc_ValueError, "dy must be [n_tokens, rows]");
-    const int dd = dtype_code(tensor(a[6], "dy")), act = (int)integer(a[8]), sd = dtype_code(scales);
+    const int dd = dtype_code(tensor(a[6], "dy")), act = small(a[8], "activation"), sd = dtype_code(scales);
     const int64_t n = tensor(a[6], "dy").size(0);
     const Rows dy(a[6], "dy", n, rows, torch_dtype(dd), d);
-    const bool want_dx = PyObject_IsTrue(a[9]) == 1, want_db = PyObject_IsTrue(a[10]) == 1;
+    const bool want_dx = truth(a[9]), want_db = truth(a[10]);
     const c10::cuda::CUDAGuard guard(d);
     const at::Tensor cb = codebook(a[5], d);
     const Outliers o(a[11]);
@@ -585,12 +598,12 @@ PyObject* moe(PyObject* const* a)
         check_matrix(m[2 * k], m[2 * k + 1], experts * (k ? hidden : 2 * ffn), k ? ffn : hidden, block);
         if (m[2 * k].device() != d) fail(PyExc_ValueError, "all tensors must be on one device");
     }
-    const int sd = dtype_code(m[1]), od = (int)integer(a[12]), rd = dtype_code(router);
+    const int sd = dtype_code(m[1]), od = small(a[12], "out_dtype"), rd = dtype_code(router);
     if (dtype_code(m[3]) != sd) fail(PyExc_TypeError, "the constants of gate_up and down must share a dtype");
     if (od != BOF4_F32 && od != BOF4_BF16) fail(PyExc_ValueError, "out_dtype must be F32 or BF16");
     const int64_t top = integer(a[7]);
     if (top < 1 || top > 16) fail(PyExc_ValueError, "top_k must be 1 ... 16");
-    const int act = (int)integer(a[8]), score = (int)integer(a[9]), renorm = PyObject_IsTrue(a[10]) == 1;
+    const int act = small(a[8], "activation"), score = small(a[9], "score"), renorm = truth(a[10]);
     const float scale = (float)real(a[11]);
     const c10::cuda::CUDAGuard guard(d);
     const at::Tensor cb = codebook(a[6], d);

@@ -1,5 +1,5 @@
-"""bof4_linear, bof4_linear_backward and bof4_moe record no autograd graph: a tensor that requires a gradient is refused while gradients
-are on, and taken where they are off (inference, or inside a torch.autograd.Function)."""
+"""bof4_linear, bof4_linear_backward and bof4_moe as torch sees them.  They record no autograd graph: a tensor that requires a gradient is
+refused while gradients are on, and taken where they are off (inference, or inside a torch.autograd.Function)."""
 import numpy as np
 import pytest
 import torch
@@ -106,3 +106,19 @@ def test_a_layer_that_is_trained_through(bof4, tokens):
     ((torch.relu(b[0] @ w.T + b[1]) + b[2]) * c.double()).sum().backward()
     assert torch.equal(a[0].grad, b[0].grad.bfloat16())
     assert torch.equal(a[1].grad.double(), b[1].grad) and torch.equal(a[2].grad.double(), b[2].grad)
+
+
+@pytest.mark.gpu
+def test_numbers_are_not_cut_off(bof4):
+    """A code beyond 32 bits is refused, not taken for its lower half; a flag that has no truth value raises its own error."""
+    (linear, kl), (backward, kb), (moe, km) = arguments(bof4, "cuda")
+    for fn, kw, names in ((linear, kl, ("activation", "out_dtype", "block_size")), (backward, kb, ("activation", "block_size")),
+                          (moe, km, ("activation", "score", "out_dtype", "block_size", "top_k"))):
+        for name in names:
+            for value in (1 << 32, (1 << 32) + 1, -(1 << 32), (1 << 32) + 32):
+                with pytest.raises(ValueError):
+                    fn(**{**kw, name: value})
+    neither = torch.ones(2)
+    for fn, kw, name in ((backward, kb, "want_dx"), (backward, kb, "want_dbias"), (moe, km, "renormalize")):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            fn(**{**kw, name: neither})
