@@ -48,14 +48,15 @@
 
 namespace bof4 {
 
-constexpr int kLtGroups = 4;                 // producer groups, a k-block of a line each
+constexpr int kLtGroups = 4;                 // producer groups, a k-block of a line and a stage each
 constexpr int kLtM = 128, kLtK = 64;
 constexpr int kLtMaxN = 256;                 // tokens of a tile; columns of an accumulator
 constexpr int kLtABytes = kLtM * kLtK * 2;   // 16 KiB
 constexpr int kLtHalfBytes = 8192;           // half a line of codes: two k-blocks; 128 rows x 64 bytes
-constexpr int kLtMaxStages = 8, kLtMaxHalves = 8;
+constexpr int kLtMaxHalves = 8;
 constexpr int kLtTableN = 64;                // tokens of a tile up to which there is room, and use, for the table of pairs
 constexpr int kLtLongK = 4096;               // K up to which results in fp32 have tiles of any width
+constexpr int kLtMaxParts = 64;              // of a tile
 constexpr int kLtAhead = 6;                  // lines that L2 is asked for before the ring is
 constexpr int kLtSmem = 225 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
 constexpr int kLtIssue = 16, kLtTokens = 17, kLtCodes = 18, kLtResults = 20;  // warp 19 has no job: the results start at a multiple of 4
@@ -65,7 +66,7 @@ struct LtWork {
     int tiles, tiles_n, per_tile;  // tiles, those along the tokens, lines of a tile
     int box_n;                     // tokens of a tile, a multiple of 16
     int k;                         // K
-    int stages, halves;            // stages of A and B (4 or 8), half lines of codes (even)
+    int halves;                    // half lines of codes in the ring (even, at least four)
     int accs;                      // accumulators of a part of a tile, which the instructions of a k-block use in turn: 4, 2 or 1
     int each, extra;               // lines per CTA, and the remainder
     bool table;                    // half of the codes go through a table
@@ -203,7 +204,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                  unsigned char* __restrict__ ws, float* __restrict__ parts)
 {
     extern __shared__ unsigned char s_dyn[];
-    __shared__ __align__(8) unsigned long long s_full[kLtMaxStages], s_empty[kLtMaxStages], s_half_full[kLtMaxHalves],
+    __shared__ __align__(8) unsigned long long s_full[kLtGroups], s_empty[kLtGroups], s_half_full[kLtMaxHalves],
         s_half_empty[kLtMaxHalves], s_acc_full[2], s_acc_empty[2];
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ uint32_t s_tmem;
@@ -212,13 +213,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per_tile = work.per_tile, box_n = work.box_n;
     const uint32_t b_stage = (uint32_t)box_n * 128u;  // a multiple of 2048
-    const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)work.stages * kLtABytes;
+    const uint32_t a_ring = (smem_u32(s_dyn) + 1023u) & ~1023u, code_ring = a_ring + (uint32_t)(kLtGroups * kLtABytes);
     const uint32_t b_ring = code_ring + (uint32_t)work.halves * kLtHalfBytes;
-    const uint32_t pairs = b_ring + (uint32_t)work.stages * b_stage;
-    // line n of this CTA has stages turn(n) * 4 ... + 3, for the time(n)-th time
-    const int two = work.stages == 8 ? 1 : 0, accs = work.accs;
-    auto turn = [&](int n) { return n & two; };
-    auto time = [&](int n) { return (uint32_t)(n >> two) & 1u; };
+    const uint32_t pairs = b_ring + (uint32_t)kLtGroups * b_stage;
+    const int accs = work.accs;
+    // a line takes a turn of every stage: line n of this CTA the n-th
+    auto time = [](int n) { return (uint32_t)n & 1u; };
     const int begin = work.start((int)blockIdx.x), finish = work.start((int)blockIdx.x + 1), lines = finish - begin;
     const int tile0 = (int)((uint32_t)begin / (uint32_t)per_tile), in0 = begin - tile0 * per_tile;
     const int segs = lines ? (in0 + lines - 1) / per_tile + 1 : 0;
@@ -233,7 +233,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     if (tid == 0) {
         if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
         s_fail = s_sums = 0;
-        for (int s = 0; s < work.stages; ++s) init(&s_full[s], 4 + 1), init(&s_empty[s], 1);  // four warps of producers, and the tokens
+        for (int s = 0; s < kLtGroups; ++s) init(&s_full[s], 4 + 1), init(&s_empty[s], 1);  // four warps of producers, and the tokens
         for (int s = 0; s < work.halves; ++s) init(&s_half_full[s], 1), init(&s_half_empty[s], 8);
         for (int b = 0; b < 2; ++b) init(&s_acc_full[b], 1), init(&s_acc_empty[b], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -319,21 +319,20 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             }
 #pragma unroll
             for (int j = 4; j < 8; ++j) lt_lookup8(w[j], lo, hi, v + 4 * j);
-            const uint32_t st = (uint32_t)(turn(n) * kLtGroups), at = tile_at + st * kLtABytes;
-            if (!__all_sync(kFull, tc_wait(empty0 + 8u * st, time(n) ^ 1u))) {
+            if (!__all_sync(kFull, tc_wait(empty0, time(n) ^ 1u))) {
                 if (lane == 0) s_fail = 1;
                 break;
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at ^ (uint32_t)(j << 4)), "r"(v[4 * j]), "r"(v[4 * j + 1]), "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(tile_at ^ (uint32_t)(j << 4)), "r"(v[4 * j]), "r"(v[4 * j + 1]), "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
             if (OPQ) {
                 while (head >= 0) {  // the same list for all lanes; a lane patches its own row
                     const int2 e = __ldg(nodes + head);
                     const uint32_t place = (uint32_t)e.y >> 16;
                     if ((int)(place >> 6) == lane) {
                         const uint32_t c = place & 63u;
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"((at ^ ((c >> 3) << 4)) + (c & 7u) * 2u), "h"((uint16_t)e.y) : "memory");
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"((tile_at ^ ((c >> 3) << 4)) + (c & 7u) * 2u), "h"((uint16_t)e.y) : "memory");
                     }
                     head = e.x;
                 }
@@ -344,7 +343,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             // memory let the next half line overtake them)
             if (lane == 0) {
                 tc_arrive(&s_half_empty[slot]);
-                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full0 + 8u * st) : "memory");
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full0) : "memory");
             }
             if ((slot += 2) >= work.halves) slot = group >> 1, par ^= 1u;
         }
@@ -370,18 +369,16 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 uint32_t d[kLtK / 16];  // of the instructions of a k-block
 #pragma unroll
                 for (int kk = 0; kk < kLtK / 16; ++kk) d[kk] = tmem + (uint32_t)((seg & 1) * kLtMaxN + (kk & (accs - 1)) * (kLtMaxN / accs));
-                const int s0 = turn(n) * kLtGroups;
                 if (acc == 0u && !(ok = wait(smem_u32(&s_acc_empty[seg & 1]), (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
                 // a look at all four stages first: mostly they are full, and the looks overlap
                 bool ready[kLtGroups];
 #pragma unroll
-                for (int j = 0; j < kLtGroups; ++j) ready[j] = tc_look(full0 + 8u * (uint32_t)(s0 + j), par);
+                for (int j = 0; j < kLtGroups; ++j) ready[j] = tc_look(full0 + 8u * (uint32_t)j, par);
 #pragma unroll
                 for (int j = 0; j < kLtGroups; ++j) {
-                    const int st = s0 + j;
-                    if (!ready[j] && !(ok = wait(full0 + 8u * (uint32_t)st, par))) break;
+                    if (!ready[j] && !(ok = wait(full0 + 8u * (uint32_t)j, par))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = da0 + (uint64_t)(st * (kLtABytes >> 4)), db = db0 + (uint64_t)(st * (b_stage >> 4));
+                    const uint64_t da = da0 + (uint64_t)(j * (kLtABytes >> 4)), db = db0 + (uint64_t)(j * (b_stage >> 4));
 #pragma unroll
                     for (int kk = 0; kk < kLtK / 16; ++kk) {
                         asm volatile(
@@ -393,7 +390,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                             : "memory");
                     }
                     acc = 1u;
-                    tc_commit(&s_empty[st], 1u);
+                    tc_commit(&s_empty[j], 1u);
                 }
                 if (!ok) break;
                 if (++in == per_tile || n + 1 == lines) {  // the end of a part of a tile
@@ -411,9 +408,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             for (int n = 0; ok && n < lines; ++n) {
                 const int t0 = (int)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
                 for (int j = 0; j < kLtGroups; ++j) {
-                    const int st = turn(n) * kLtGroups + j;
-                    if (!(ok = tc_wait(smem_u32(&s_empty[st]), time(n) ^ 1u))) break;
-                    tc_load_box(b_ring + (uint32_t)st * b_stage, &token_map, &s_full[st], b_stage, (in * kLtGroups + j) * kLtK, t0);
+                    if (!(ok = tc_wait(smem_u32(&s_empty[j]), time(n) ^ 1u))) break;
+                    tc_load_box(b_ring + (uint32_t)j * b_stage, &token_map, &s_full[j], b_stage, (in * kLtGroups + j) * kLtK, t0);
                 }
                 if (++in == per_tile) in = 0, ++tile;
             }
@@ -587,16 +583,16 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp3
     w.per_tile = (int)per_tile;
     w.box_n = (int)box;
     w.k = (int)k;
-    // Eight stages where they leave room for two lines of codes, four otherwise (256 tokens leave two lines beside them).
+    // Four stages, and as many half lines of codes as there is room for beside them: four (256 tokens) to eight.  (Eight stages would leave
+    // less than two lines of codes whatever the number of tokens: the table takes 64 KiB up to 64 of them, the stages themselves beyond.)
     w.table = box <= kLtTableN;
     const int room = kLtSmem - 1024 - (w.table ? kPairBytes : 0), stage = kLtABytes + (int)box * 128;
-    w.stages = room - 8 * stage >= 4 * kLtHalfBytes ? 8 : 4;
-    w.halves = (room - w.stages * stage) / kLtHalfBytes & ~1;
+    w.halves = (room - kLtGroups * stage) / kLtHalfBytes & ~1;
     if (w.halves > kLtMaxHalves) w.halves = kLtMaxHalves;
     w.accs = box <= 64 ? 4 : box <= 128 ? 2 : 1;
-    // One CTA per SM, each with an equal part of the lines.  A tile is cut into at most so many parts that summing them
-    // stays short beside the product: 16384 / tokens.
-    const int64_t lines = tiles * per_tile, most = tiles * (16384 / box < 64 ? 16384 / box : 64);
+    // One CTA per SM, each with an equal part of the lines, but for few tiles of a long K: a tile is not cut into more than kLtMaxParts, which
+    // one CTA adds up (128 x 256 sums in fp32 each).
+    const int64_t lines = tiles * per_tile, most = tiles * kLtMaxParts;
     int64_t ctas = lines < kSMs ? lines : kSMs;
     if (ctas > most) ctas = most;
     p->ctas = (int)ctas;
