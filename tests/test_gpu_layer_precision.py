@@ -2,7 +2,6 @@
 exact, the two halves of an expert layer's h, and how much of a long sum in fp32 is lost."""
 import math
 
-import numpy as np
 import pytest
 import torch
 
