@@ -296,9 +296,10 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
 
 }  // namespace
 
-// Up to sixteen tokens, where the other form decodes as much for a tile of sixteen (8192 x 8192: 27 us against 32 for nine tokens, 33
-// against 32 for sixteen; 1024 x 4096: 9 against 13); up to six with a list of outliers, whose corrections cost 3 us a token there
-// and less here (8192 x 8192 with 65,536: 34 us against 42 for four tokens, 60 against 42 for twelve).
+// Up to sixteen tokens, where the other form decodes as much for a tile of sixteen (8192 x 8192: 26.7 us against 31.7 for nine tokens, 29.2
+// against 31.9 for twelve, 33.1 against 31.9 for sixteen; 1024 x 4096 by sixteen: 9 against 13).  Up to six with a list of outliers: its corrections
+// cost about 2 us a token here, its entries in the tiles the same for any number of tokens there (8192 x 8192 with 65,536: 35.0 us against 42.2 for
+// four tokens, 40.0 against 42.2 for six, 42.6 against 42.2 for seven, 60 against 42 for twelve).
 bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list)
 {
     return tokens <= (list ? kFewListTokens : kFewTokens) && cols <= 32768 && rows <= (1 << 26);
