@@ -61,7 +61,7 @@ __device__ __forceinline__ void lt_table(float m, const float2* levels, uint32_t
     }
 }
 
-constexpr int kPairBytes = 256 * 32 * 8;
+constexpr int kPairBytes = 256 * 32 * 8;  // level pairs per code byte, a column per lane
 
 // Fills the table of level pairs; all warps of the CTA take part.  A row of the table is the same pair 32 times: a warp
 // writes rows in turn, the levels in its registers.

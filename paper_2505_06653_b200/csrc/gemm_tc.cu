@@ -69,9 +69,8 @@ struct TcGeo {
     static_assert(stages % kTcIssuers == 0, "a stage belongs to one issuing warp");
 };
 constexpr int kTcLineBytes = kTcM * 128;         // 16 KiB
-constexpr int kTcPairBytes = 256 * 32 * 8;       // level pairs per code byte, a column per lane
 constexpr int kTcXBytes = 64 * 1024;                  // all stages of X
-constexpr int kTcSmem = kTcXBytes + kTcLines * kTcLineBytes + kTcPairBytes + 1024;  // + slack to align to 1024 bytes
+constexpr int kTcSmem = kTcXBytes + kTcLines * kTcLineBytes + kPairBytes + 1024;  // + slack to align to 1024 bytes
 // warps: 0 ... 15 produce, then issuers, X, constants and codes, results
 constexpr int kTcIssue = kTcGroups * 4, kTcX = kTcIssue + kTcIssuers, kTcCodes = kTcX + 1, kTcEpilogue = kTcCodes + 1;
 constexpr int kTcThreads = 32 * (kTcEpilogue + 4);  // 24 warps: 80 registers each

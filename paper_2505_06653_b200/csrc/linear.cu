@@ -147,8 +147,6 @@ __global__ void __launch_bounds__(256) linear_empty_kernel(const LinearOut out, 
 
 namespace {
 
-size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The checks that the two entry points share.

@@ -195,6 +195,9 @@ struct LinearFour {
     }
 };
 
+// Parts of a workspace begin at multiples of 256 bytes.
+inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
 // The 4-bit matrix and its outlier list.
 struct LinearW {
     const uint8_t* codes;

@@ -265,8 +265,6 @@ struct FewPlan {
     size_t sums = 0, correction = 0, total = 0;  // byte offsets (the tickets are at 0), and the bytes of all
 };
 
-size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-
 FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
 {
     FewPlan p;

@@ -561,8 +561,6 @@ struct LtPlan {
     size_t parts = 0, heads = 0, nodes = 0, total = 0;  // byte offsets (the tickets are at 0), and the bytes of all
 };
 
-size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-
 // False: too large for 32-bit line numbers.
 bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp32, int64_t capacity, LtPlan* p)
 {

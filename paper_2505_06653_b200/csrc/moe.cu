@@ -513,7 +513,6 @@ namespace {
 struct MoePlan {
     size_t logits, hi, lo, out, total;  // byte offsets (the barriers' cell is at 0), and the bytes of all
 };
-size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 MoePlan moe_plan(int64_t tokens, int64_t hidden, int64_t ffn, int64_t experts, int64_t top)
 {
     MoePlan p;
