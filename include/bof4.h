@@ -392,7 +392,8 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
  * bf16, bit for bit what bof4_dequantize writes, and the stored value where the outlier list has an entry; products are exact
  * and added up in fp32 (in an order that depends on shapes, types and whether there is a list alone, so two calls on the same
  * inputs give the same bits); bias, activation and residual are applied in fp32; y is rounded once.  (bof4_gemv keeps the unrounded product
- * scale * level instead.)
+ * scale * level instead.  bof4_gemm_tc computes the same sums for exactly 16, 32, 48 or 64 contiguous tokens and rows a multiple of 128, into fp32
+ * [rows][n_rhs] and nothing else; where that is all that is wanted it is the faster call: 28672 x 8192 by 32 in 62 us against 85.)
  *   d_codes     device, rows * cols / 2 bytes, 32-byte aligned;  d_scales, d_codebook as for bof4_gemv
  *   d_x         device, bf16, token t at d_x + t * ldx, 16-byte aligned; ldx a multiple of 8
  *   d_bias      device, rows values of bias_dtype, or NULL
@@ -400,7 +401,7 @@ BOF4_API int bof4_gemm_tc(const uint8_t* d_codes, const void* d_scales, int scal
  *   activation  BOF4_ACT_*
  *   d_out_idx / d_out_val / d_n_out / capacity   outlier list as for bof4_dequantize (ascending, distinct indices), or all
  *               NULL; with a list, rows * cols must fit 32-bit indices.  For few tokens an entry is a correction, (value - W^) x,
- *               so a value of x that is not finite may give NaN there where value * x is infinite
+ *               so a value of x or a weight below an entry that is not finite may give NaN there where value * x is not
  *   d_y         device, out, y_dtype (BOF4_BF16 or BOF4_F32), token t at t * ldy
  *   d_pre       device, out, bf16, token t at t * ld_pre: z, as bof4_linear_backward wants it where there is an
  *               activation; or NULL
@@ -443,10 +444,11 @@ BOF4_API size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_t 
  * A whole mixture-of-experts layer for a few tokens, its experts' matrices in 4 bits:
  *   s[t, e] = sum_c x[t, c] R[e, c];   score = softmax_e(s) or 1 / (1 + exp(-s))
  *   the top_k experts of token t: the largest s, descending (equal ones: lowest index first);  w[t, j] = scale * score, divided
- *   by the sum of the token's top_k scores where renormalize != 0
+ *   by the sum of the token's top_k scores where renormalize != 0 (finite for finite s, however far below zero all of them lie)
  *   h = act(G_e x) * (U_e x);   y[t] = sum_j w[t, j] D_e h
  * with the dequantised weights in bf16 as for bof4_linear and fp32 everywhere else but in h, of which 16 bits enter the product
- * with D_e (2^-17 relative).  Every sum is taken in an order that depends on the shapes and the choice of experts alone.  Only
+ * with D_e (2^-17 relative; an infinite weight of D_e gives infinities or NaN).  The choice is made on s in fp32, so experts that are closer than the
+ * roundings of that sum may change places.  Every sum is taken in an order that depends on the shapes and the choice of experts alone.  Only
  * the experts that some token chose are read.
  *   d_x         device, bf16, n_tokens (0 ... 64) rows of `hidden`, token t at t * ldx; 16-byte aligned, ldx a multiple of 8
  *   d_router    device, [n_experts][hidden] of router_dtype, 16-byte aligned;  n_experts 1 ... 512, top_k 1 ... 16

@@ -8,7 +8,7 @@
 // (a ticket: nobody waits) adds the slices up in order.
 //
 // Bound by decoding (decode.cuh), and in small calls by set-up: the table of level pairs, the first codes and the drain take 4 us.
-// 4096 x 4096 by one token 7.0 us, 11008 x 4096 by five 14.0, 28672 x 8192 by one 42, by eight 50.
+// 4096 x 4096 by one token 7.0 us, 11008 x 4096 by five 14.0, 28672 x 8192 by one 42 to 45, by eight 50 to 55.
 #include "decode.cuh"
 #include "linear.cuh"
 #include "tc.cuh"
@@ -295,7 +295,7 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
 }  // namespace
 
 // Up to sixteen tokens, where the other form decodes as much for a tile of sixteen (8192 x 8192: 26.7 us against 31.7 for nine tokens, 29.2
-// against 31.9 for twelve, 33.1 against 31.9 for sixteen; 1024 x 4096 by sixteen: 9 against 13).  Up to six with a list of outliers: its corrections
+// against 31.9 for twelve, 33.1 against 31.9 for sixteen; 1024 x 4096 by sixteen: 9 against 13; the largest lose: 28672 x 8192 by sixteen 97 against 84).  Up to six with a list of outliers: its corrections
 // cost about 2 us a token here, its entries in the tiles the same for any number of tokens there (8192 x 8192 with 65,536: 35.0 us against 42.2 for
 // four tokens, 40.0 against 42.2 for six, 42.6 against 42.2 for seven, 60 against 42 for twelve).
 bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list)

@@ -21,9 +21,10 @@
 // A unit's columns are split over the stripes of a row group (a warp each, 256 columns; several stripes a warp where a row is
 // longer than a CTA has warps for) and its parts are added up in shared memory in a fixed order: no sum depends on scheduling.
 //
-// One token, 64 experts of 2048 x 1408, six chosen: 32 us, mostly latency.  19 tokens, 128 experts of 2048 x 768, eight chosen: 137 us,
-// 1760 GB/s, of them router and its barrier 11, choice and list 6, gate/up 68, down 33, two barriers with the waiting for the slowest CTA
-// 12, sums 2.  The walks are bound by decoding (decode.cuh), 15 to 16 codes per clock and SM.
+// One token, 64 experts of 2048 x 1408, six chosen: 33 us, mostly latency.  19 tokens, 128 experts of 2048 x 768, eight chosen: 140 us,
+// 1720 GB/s, of them router and its barrier 11, choice and list 6, gate/up 68, down 33, two barriers with the waiting for the slowest CTA
+// 12, sums 2.  The walks are bound by decoding (decode.cuh), 15 to 16 codes per clock and SM.  All 128 registers a thread are taken and two spill
+// (six to nine with blocks of 32).
 //
 // The waits on the barrier are bounded: a time-out sets the status word and everybody leaves.
 #include <type_traits>
