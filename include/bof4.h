@@ -441,6 +441,73 @@ BOF4_API int bof4_linear_backward(const uint8_t* d_codes, const void* d_scales, 
 BOF4_API size_t bof4_linear_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, int backward, int64_t capacity);
 
 /*
+ * Both projections of a gated feed-forward block, its activation and their product, for any number of tokens:
+ *   z[t, r] = sum_c W^[r, c] x[t, c] + bias[r],   h[t, f] = act(z[t, f]) * z[t, ffn + f]
+ * W has 2 * ffn rows, quantised as one flat tensor: the ffn rows of the gate, then those of the up projection (as an expert's rows for
+ * bof4_moe).  W^, products and sums as for bof4_linear; bias, activation and product are applied in fp32 and h is rounded once.  (The
+ * down projection of the block is a bof4_linear on h, with the residual.)
+ *   d_bias    device, 2 * ffn values of bias_dtype, or NULL
+ *   d_h       device, out, h_dtype (BOF4_BF16 or BOF4_F32), token t at t * ldh
+ *   d_pre     device, out, bf16 [n_tokens][2 * ffn], token t at t * ld_pre: z, as bof4_gated_backward wants it; or NULL
+ *   d_ws      device workspace of bof4_gated_workspace_bytes(ffn, cols, n_tokens, 0, capacity) bytes, 256-byte aligned, any contents;
+ *             two calls that may run at the same time must not share one.  From some hundred tokens on it holds the decoded matrix
+ * Other arguments, alignments, outlier lists, overlap and capture as for bof4_linear.
+ */
+BOF4_API int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t ffn, int64_t cols, int block_size,
+                        const float* d_codebook, const void* d_x, int64_t ldx, int64_t n_tokens, const void* d_bias, int bias_dtype, int activation,
+                        const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity, void* d_h, int h_dtype,
+                        int64_t ldh, void* d_pre, int64_t ld_pre, int* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward pass of bof4_gated with the quantised weights held fixed:
+ *   dz[t, f] = dh[t, f] * z[t, ffn + f] * act'(z[t, f]),   dz[t, ffn + f] = dh[t, f] * act(z[t, f])
+ *   dx[t, c] = sum_r dz[t, r] W^[r, c],   dbias[r] = sum_t dz[t, r]
+ * dz is formed in fp32; the product takes it rounded to bf16, the sums of dbias take it unrounded.
+ *   d_dh      device, dh_dtype (BOF4_BF16 or BOF4_F32), token t at t * ld_dh
+ *   d_pre     device, bf16, z as bof4_gated left it, token t at t * ld_pre
+ *   d_dx      device, out, bf16, token t at t * ld_dx, or NULL: not wanted
+ *   d_dbias   device, out, fp32 [2 * ffn], or NULL
+ *   d_ws      device workspace of bof4_gated_workspace_bytes(ffn, cols, n_tokens, 1, capacity) bytes, as for bof4_gated
+ */
+BOF4_API int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t ffn, int64_t cols, int block_size,
+                                 const float* d_codebook, const void* d_dh, int dh_dtype, int64_t ld_dh, int64_t n_tokens, const void* d_pre,
+                                 int64_t ld_pre, int activation, const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out,
+                                 int64_t capacity, void* d_dx, int64_t ld_dx, float* d_dbias, int* d_status, void* d_ws, size_t ws_bytes,
+                                 void* stream);
+
+/* Bytes of workspace for the two calls above (backward != 0: for the second).  Host function, no CUDA call.  0 for invalid or too
+ * large shapes. */
+BOF4_API size_t bof4_gated_workspace_bytes(int64_t ffn, int64_t cols, int64_t n_tokens, int backward, int64_t capacity);
+
+/*
+ * Softmax cross entropy of tokens over a vocabulary whose matrix (the language model's head) is in 4 bits, and the gradient of x with
+ * the weights held fixed.  The logits are never kept:
+ *   z[t, v] = sum_c W^[v, c] x[t, c],   lse[t] = log sum_v exp(z[t, v]),   loss[t] = lse[t] - z[t, targets[t]]
+ *   dx[t] = dloss[t] * (sum_v exp(z[t, v] - lse[t]) W^[v] - W^[targets[t]])
+ * W is rows x cols (rows: the vocabulary) as for bof4_linear; W^, products and sums of z as there.  exp and the sums over v are fp32;
+ * the second product takes the probabilities rounded to bf16 and adds them up in fp32, dx is rounded once.  The target's own
+ * probability enters neither sum, so a loss near zero and its gradient keep their relative precision.  What is not finite among a token's
+ * logits makes that token's results not finite, others' not.
+ *   d_targets   device, int64 [n_tokens].  A negative target is ignored: loss 0, dx 0 (lse is still written).  One of `rows` or more
+ *               is treated the same way and sets *d_status to 2
+ *   d_dloss     device, fp32 [n_tokens]: the gradient of the whole with respect to loss[t] (1 / count for a mean); NULL: ones
+ *   d_loss, d_lse   device, out, fp32 [n_tokens]; d_lse may be NULL
+ *   d_dx        device, out, bf16, token t at t * ld_dx, or NULL: no gradient (and half of the work)
+ *   d_status    device int, written: 0, 1 when a bounded wait inside a kernel ran out (results are then undefined), 2 as above
+ *   d_ws        device workspace of bof4_cross_entropy_workspace_bytes(rows, cols, n_tokens, d_dx != NULL, capacity) bytes, 256-byte
+ *               aligned, any contents; two calls that may run at the same time must not share one
+ * rows and cols at least 1 (where there are tokens).  Other arguments, alignments, outlier lists (ascending indices) and capture as for
+ * bof4_linear; outputs must not overlap inputs.  No host synchronisation.
+ */
+BOF4_API int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size,
+                                const float* d_codebook, const void* d_x, int64_t ldx, int64_t n_tokens, const int64_t* d_targets,
+                                const float* d_dloss, const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity,
+                                float* d_loss, float* d_lse, void* d_dx, int64_t ld_dx, int* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Bytes of its workspace.  Host function, no CUDA call.  0 for invalid or too large shapes. */
+BOF4_API size_t bof4_cross_entropy_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, int want_dx, int64_t capacity);
+
+/*
  * A whole mixture-of-experts layer for a few tokens, its experts' matrices in 4 bits:
  *   s[t, e] = sum_c x[t, c] R[e, c];   score = softmax_e(s) or 1 / (1 + exp(-s))
  *   the top_k experts of token t: the largest s, descending (equal ones: lowest index first);  w[t, j] = scale * score, divided

@@ -58,7 +58,8 @@ EXPORTS = ("bof4_workspace_bytes", "bof4_fit_workspace_bytes", "bof4_em_step", "
            "bof4_default_init", "bof4_last_error", "bof4_theoretical_codebook", "bof4_theoretical_codebook_batch",
            "bof4_gemv", "bof4_outlier_count", "bof4_scales_compress", "bof4_scales_expand",
            "bof4_theoretical_codebook_general", "bof4_quantize_batch", "bof4_dequantize_batch", "bof4_m_step", "bof4_gemm_tc",
-           "bof4_linear", "bof4_linear_backward", "bof4_linear_workspace_bytes", "bof4_moe", "bof4_moe_workspace_bytes")
+           "bof4_linear", "bof4_linear_backward", "bof4_linear_workspace_bytes", "bof4_moe", "bof4_moe_workspace_bytes",
+           "bof4_gated", "bof4_gated_backward", "bof4_gated_workspace_bytes", "bof4_cross_entropy", "bof4_cross_entropy_workspace_bytes")
 
 
 class Bof4Error(RuntimeError):
@@ -135,6 +136,16 @@ def lib() -> ctypes.CDLL:
         L.bof4_moe.restype = i32
         L.bof4_moe.argtypes = [vp, i64, i64, i64, vp, i32, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, i32, i64, i32, vp, i32,
                                vp, i32, i64, vp, vp, vp, vp, sz, vp]
+        L.bof4_gated_workspace_bytes.restype = sz
+        L.bof4_gated_workspace_bytes.argtypes = [i64, i64, i64, i32, i64]
+        L.bof4_gated.restype = i32
+        L.bof4_gated.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i64, i64, vp, i32, i32, vp, vp, vp, i64, vp, i32, i64, vp, i64, vp, vp, sz, vp]
+        L.bof4_gated_backward.restype = i32
+        L.bof4_gated_backward.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i32, i64, i64, vp, i64, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.bof4_cross_entropy_workspace_bytes.restype = sz
+        L.bof4_cross_entropy_workspace_bytes.argtypes = [i64, i64, i64, i32, i64]
+        L.bof4_cross_entropy.restype = i32
+        L.bof4_cross_entropy.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, sz, vp]
         L.bof4_m_step.restype = i32
         L.bof4_m_step.argtypes = [vp, i32, i32, vp, ctypes.c_uint32, vp, vp, vp]
         L.bof4_scales_compress.restype = i32
@@ -490,7 +501,7 @@ def bof4_linear(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int,
     apart from one another).  `pre` (bf16 [n_tokens, rows]) receives x W^T + bias, which bof4_linear_backward wants where there
     is an activation.  -> (y, status int32[1]); status 0 unless a bounded wait inside the kernel ran out.
 
-    No autograd graph is recorded by this call and the two below: while gradients are on, a tensor that requires one is refused.
+    No autograd graph is recorded by this call and the layers below: while gradients are on, a tensor that requires one is refused.
     A layer that is trained through calls them from a torch.autograd.Function, in which gradients are off."""
     return _native().linear(codes, scales, rows, cols, block_size, levels, x, bias, residual, activation, out_dtype, pre, outliers, out,
                             workspace)
@@ -504,6 +515,46 @@ def bof4_linear_backward(codes: torch.Tensor, scales: torch.Tensor, rows: int, c
     dbias fp32 [rows] or None, status int32[1])."""
     return _native().linear_backward(codes, scales, rows, cols, block_size, levels, dy, pre, activation, want_dx, want_dbias, outliers,
                                      out, workspace)
+
+
+def bof4_gated_workspace_bytes(ffn: int, cols: int, n_tokens: int, backward: bool = False, capacity: int = 0) -> int:
+    """Bytes of the workspace of bof4_gated (backward: of bof4_gated_backward), which the calls otherwise allocate themselves."""
+    return int(lib().bof4_gated_workspace_bytes(ffn, cols, n_tokens, int(backward), capacity))
+
+
+def bof4_gated(codes: torch.Tensor, scales: torch.Tensor, ffn: int, cols: int, block_size: int, levels, x: torch.Tensor,
+               bias: Optional[torch.Tensor] = None, activation: int = ACT_SILU, out_dtype: int = BF16, pre: Optional[torch.Tensor] = None,
+               outliers: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None):
+    """h [n_tokens, ffn] = act(x G^T + b_g) * (x U^T + b_u) for x bf16 [n_tokens, cols] and a 4-bit matrix of 2 ffn rows, the rows of the
+    gate G and then those of U (rows of x, pre and out may be apart from one another; bias holds 2 ffn values).  `pre` (bf16
+    [n_tokens, 2 ffn]) receives both projections, which bof4_gated_backward wants.  -> (h, status int32[1])"""
+    return _native().gated(codes, scales, ffn, cols, block_size, levels, x, bias, activation, out_dtype, pre, outliers, out, workspace)
+
+
+def bof4_gated_backward(codes: torch.Tensor, scales: torch.Tensor, ffn: int, cols: int, block_size: int, levels, dh: torch.Tensor, pre: torch.Tensor,
+                        activation: int = ACT_SILU, want_dx: bool = True, want_dbias: bool = False,
+                        outliers: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None):
+    """Gradients of bof4_gated for dh [n_tokens, ffn] with the weights held fixed -> (dx bf16 [n_tokens, cols] or None,
+    dbias fp32 [2 ffn] or None, status int32[1])."""
+    return _native().gated_backward(codes, scales, ffn, cols, block_size, levels, dh, pre, activation, want_dx, want_dbias, outliers, out, workspace)
+
+
+def bof4_cross_entropy_workspace_bytes(rows: int, cols: int, n_tokens: int, want_dx: bool = False, capacity: int = 0) -> int:
+    """Bytes of the workspace of bof4_cross_entropy, which the call otherwise allocates itself."""
+    return int(lib().bof4_cross_entropy_workspace_bytes(rows, cols, n_tokens, int(want_dx), capacity))
+
+
+def bof4_cross_entropy(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, block_size: int, levels, x: torch.Tensor,
+                       targets: torch.Tensor, dloss: Optional[torch.Tensor] = None, want_dx: bool = False,
+                       outliers: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Softmax cross entropy of x bf16 [n_tokens, cols] over the `rows` rows of a 4-bit matrix, without keeping the logits.  targets int64
+    [n_tokens]; negative ones are ignored (loss 0, dx 0).  dloss fp32 [n_tokens] (None: ones) is what the gradient of the loss is
+    multiplied by, `out` receives dx.  -> (loss fp32 [n_tokens], log-sum-exp fp32 [n_tokens], dx bf16 [n_tokens, cols] or None,
+    status int32[1]); status 2: a target of `rows` or more, which was ignored."""
+    return _native().cross_entropy(codes, scales, rows, cols, block_size, levels, x, targets, dloss, want_dx, outliers, out, workspace)
 
 
 def bof4_moe_workspace_bytes(n_tokens: int, hidden: int, ffn: int, n_experts: int, top_k: int) -> int:

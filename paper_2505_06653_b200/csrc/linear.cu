@@ -4,54 +4,6 @@
 
 namespace bof4 {
 
-constexpr int kDzCols = 256;    // columns of a CTA: 32 lanes of eight
-constexpr int kDzTokens = 32;   // tokens of a CTA, four a warp
-
-// Eight values from column c of a row as they are in memory; those past the end are zero.
-template <class T>
-struct Dz8;
-template <>
-struct Dz8<BF16> {
-    uint32_t w[4];
-    __device__ __forceinline__ void load(const void* p, int64_t at, int count, bool vec)
-    {
-        const uint16_t* q = static_cast<const uint16_t*>(p) + at;
-        if (vec) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(q));
-            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w[k] = (2 * k < count ? (uint32_t)__ldg(q + 2 * k) : 0u) | (2 * k + 1 < count ? (uint32_t)__ldg(q + 2 * k + 1) << 16 : 0u);
-        }
-    }
-    __device__ __forceinline__ void values(float (&v)[8]) const
-    {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[2 * k] = __uint_as_float(w[k] << 16), v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-    }
-};
-template <>
-struct Dz8<F32> {
-    float w[8];
-    __device__ __forceinline__ void load(const void* p, int64_t at, int count, bool vec)
-    {
-        const float* q = static_cast<const float*>(p) + at;
-        if (vec) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(q)), b = __ldg(reinterpret_cast<const float4*>(q) + 1);
-            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = k < count ? __ldg(q + k) : 0.0f;
-        }
-    }
-    __device__ __forceinline__ void values(float (&v)[8]) const
-    {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = w[k];
-    }
-};
-
 // dz = dy * act'(pre), rounded to bf16 for the tensor cores, and the sums of the unrounded dz over a CTA's tokens.  One pass
 // over dy and pre; a warp's four tokens are requested at once, and small CTAs leave a short last wave (2048 tokens of
 // 14336 columns by SILU: 33 us, 5.3 TB/s; 64 tokens a CTA, two of a warp's at a time, and expf with rounded quotients took 67).  The tanh form
@@ -146,11 +98,13 @@ __global__ void __launch_bounds__(256) linear_empty_kernel(const LinearOut out, 
     }
 }
 
-namespace {
+// Adds up the CTAs' parts of a bias gradient, [chunks][n].
+void linear_dbias(const float* sums, int64_t n, int64_t chunks, float* dbias, cudaStream_t st)
+{
+    launch_after(dbias_kernel, (int)((n + 31) / 32), 256, 0, st, sums, n, chunks, dbias);
+}
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// The checks that the two entry points share.
+// The checks that the entry points share.
 int linear_check(const char* fn, LinearW* w, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size, int64_t n_tokens,
                  int activation, const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity)
 {
@@ -199,6 +153,8 @@ int linear_check(const char* fn, LinearW* w, const void* d_scales, int scale_dty
     w->capacity = d_out_idx ? capacity : 0;
     return BOF4_OK;
 }
+
+namespace {
 
 // What the backward pass keeps behind the product's workspace: dz, then the sums of dz.
 struct DzPlan {
@@ -360,7 +316,7 @@ extern "C" int bof4_linear_backward(const uint8_t* d_codes, const void* d_scales
         const bool vec = aligned16(d_dy) && ld_dy % 8 == 0 && (!pre || (aligned16(pre) && ld_pre % 8 == 0));
         launch_after(dy_dtype == BOF4_F32 ? dz_kernel<F32> : dz_kernel<BF16>, (int)(plan.chunks * col_blocks), 256, 0, st, d_dy, ld_dy, pre, ld_pre,
                      activation, rows, n_tokens, vec, make_dz ? dz : nullptr, plan.ld, d_dbias ? sums : nullptr, col_blocks);
-        if (d_dbias && plan.chunks > 1) launch_after(dbias_kernel, (int)((rows + 31) / 32), 256, 0, st, sums, rows, plan.chunks, d_dbias);
+        if (d_dbias && plan.chunks > 1) linear_dbias(sums, rows, plan.chunks, d_dbias, st);
         BOF4_CUDA_TRY(cudaGetLastError());
     }
     if (!product) return BOF4_OK;

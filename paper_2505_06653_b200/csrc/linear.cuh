@@ -109,8 +109,78 @@ __device__ __forceinline__ void activate_slopes(float (&g)[N], const float (&z)[
     }
 }
 
+// act(z) and act'(z) together: the logistic and the normal distribution's part is evaluated once (accurate as above).
+__device__ __forceinline__ void activate_both(float z, int act, float& a, float& slope)
+{
+    switch (act) {
+        case BOF4_ACT_RELU: a = activate(z, BOF4_ACT_RELU), slope = activate_slope(z, BOF4_ACT_RELU); break;
+        case BOF4_ACT_GELU: {
+            const float cdf = 0.5f * erfcf(-0.70710678118654752f * z), d = cdf + z * 0.3989422804014327f * expf(-0.5f * z * z);
+            a = z * cdf, slope = fabsf(z) > 20.0f ? (z > 0.0f ? 1.0f : 0.0f) : d;
+            break;
+        }
+        case BOF4_ACT_GELU_TANH: {
+            const float v = 1.5957691216057308f * (z + 0.044715f * z * z * z), t = __expf(-fabsf(v)), big = __fdividef(1.0f, 1.0f + t), little = t * big;
+            const float s = z > 0.0f ? big : little, d = s + z * (1.5957691216057308f * (1.0f + 0.134145f * z * z)) * (big * little);
+            a = z * s, slope = fabsf(z) > 12.0f ? (z > 0.0f ? 1.0f : 0.0f) : d;
+            break;
+        }
+        case BOF4_ACT_SILU: {
+            const float t = __expf(-fabsf(z)), big = __fdividef(1.0f, 1.0f + t), little = t * big, s = z > 0.0f ? big : little;
+            a = z * s, slope = fabsf(z) > 100.0f ? (z > 0.0f ? 1.0f : 0.0f) : s + z * (big * little);
+            break;
+        }
+        default: a = z, slope = 1.0f;
+    }
+}
+
+// Eight values from column c of a row as they are in memory; those past the end are zero.
+template <class T>
+struct Dz8;
+template <>
+struct Dz8<BF16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count, bool vec)
+    {
+        const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+        if (vec) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4*>(q));
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[k] = (2 * k < count ? (uint32_t)__ldg(q + 2 * k) : 0u) | (2 * k + 1 < count ? (uint32_t)__ldg(q + 2 * k + 1) << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[2 * k] = __uint_as_float(w[k] << 16), v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+};
+template <>
+struct Dz8<F32> {
+    float w[8];
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count, bool vec)
+    {
+        const float* q = static_cast<const float*>(p) + at;
+        if (vec) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(q)), b = __ldg(reinterpret_cast<const float4*>(q) + 1);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = k < count ? __ldg(q + k) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = w[k];
+    }
+};
+
 // Where a sum goes: z = sum + bias (kept as bf16 where a backward pass will want it), y = act(z) + residual.  Element
-// (t, o) of a matrix is at t * ld + o.
+// (t, o) of a matrix is at t * ld + o.  Gated: n columns f of y, for which z has 2 n, y = act(z[f]) * z[n + f]; bias and pre hold 2 n too.
 struct LinearOut {
     const void* bias;      // [n] or NULL
     const void* residual;  // type of y, or NULL
@@ -121,6 +191,8 @@ struct LinearOut {
     bool bias_bf16, y_bf16;
     // rows of y, residual and pre begin at addresses that hold pairs of bf16 values / 16 bytes of their type
     bool pairs, wide;
+    bool gated;
+    bool keep_status;  // *status is set where a wait runs out, and not cleared before
     void set_alignment()
     {
         const uintptr_t a = reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(residual) | reinterpret_cast<uintptr_t>(pre);
@@ -147,6 +219,15 @@ struct LinearOut {
         const float v = activate(z, act) + r;
         if (y_bf16) static_cast<uint16_t*>(y)[t * ldy + o] = bf16_round(v);
         else static_cast<float*>(y)[t * ldy + o] = v;
+    }
+    // gated: the sums of columns f and n + f
+    __device__ __forceinline__ void store_pair(float g, float u, int64_t t, int64_t f) const
+    {
+        g += bias_at(f), u += bias_at(n + f);
+        if (pre) pre[t * ld_pre + f] = bf16_round(g), pre[t * ld_pre + n + f] = bf16_round(u);
+        const float v = activate(g, act) * u;
+        if (y_bf16) static_cast<uint16_t*>(y)[t * ldy + f] = bf16_round(v);
+        else static_cast<float*>(y)[t * ldy + f] = v;
     }
 };
 
@@ -195,6 +276,8 @@ struct LinearFour {
     }
 };
 
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
 // Parts of a workspace begin at multiples of 256 bytes.
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -210,6 +293,13 @@ struct LinearW {
     const int64_t* n_out;
     int64_t capacity;
 };
+
+// The checks that the entry points share; fills *w but for codes and levels.
+int linear_check(const char* fn, LinearW* w, const void* d_scales, int scale_dtype, int64_t rows, int64_t cols, int block_size, int64_t n_tokens,
+                 int activation, const int32_t* d_out_idx, const void* d_out_val, const int64_t* d_n_out, int64_t capacity);
+constexpr int kDzCols = 256;    // columns of a CTA that forms gradients of activations: 32 lanes of eight
+constexpr int kDzTokens = 32;   // its tokens, four a warp
+void linear_dbias(const float* sums, int64_t n, int64_t chunks, float* dbias, cudaStream_t st);
 
 // The tensor-core form: bytes of its workspace (0: too large), and the launch.  z[t, o] = sum_k operand[t, k] W^[o, k]
 // (forward) or W^[k, o] (backward), then `out`.  operand: bf16, `ld` elements between tokens.

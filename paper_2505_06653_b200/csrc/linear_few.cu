@@ -40,7 +40,9 @@ struct FewWork {
     unsigned long long epoch;
 };
 
-template <int NT, class ST, bool HALF>
+// GATED: a row tile holds eight gate rows and the eight up rows of the same columns of the result, so that a lane of the product
+// has both.
+template <int NT, class ST, bool HALF, bool GATED>
 __global__ void __launch_bounds__(FewGeo<NT>::threads, 1)
 linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __restrict__ scales, int64_t rows, int64_t cols, int block_shift,
                   const float* __restrict__ levels, const uint16_t* __restrict__ x, int64_t ldx, const LinearOut out,
@@ -72,21 +74,24 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
     }
     bool failed = false;  // a wait ran out
     if (tid == 0) {
-        if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
+        if (blockIdx.x == 0 && !out.keep_status) *status = 0;  // long before any wait can have run out
         if (work.slices > 1) tc_ticket_open(tickets + peer, work.epoch);
     }
     // The group's row tiles in order: codes and constants are requested kFewAhead of them before they are used.
     const uint32_t ring = kFewRing + (uint32_t)(warp * kFewSlots * kFewUnit), lanes = (live0 ? 5u : 0u) | (live1 ? 10u : 0u);
     const int mine = busy && first < work.tiles ? (work.tiles - 1 - first) / step + 1 : 0;  // row tiles of this group
-    const int64_t per_row = cols >> block_shift, jump = (int64_t)step * 16 * per_row;
-    int64_t at = ((int64_t)first * 16 + g) * per_row + (c0 >> block_shift);
-    int left = (int)(rows - (int64_t)first * 16) - g, row = first * 16, asked = 0;
+    constexpr int R = GATED ? 8 : 16;  // rows of the matrix (of each half of it) in a row tile
+    const int64_t per_row = cols >> block_shift, jump = (int64_t)step * R * per_row, other = (GATED ? out.n : 8) * per_row;
+    int64_t at = ((int64_t)first * R + g) * per_row + (c0 >> block_shift);
+    int left = (int)((GATED ? out.n : rows) - (int64_t)first * R) - g, row = first * R, asked = 0;
     FewConst<ST, HALF> m[kFewAhead + 1];  // of the next units, the oldest first
     auto request = [&](int slot, FewConst<ST, HALF>& c) {
-        if (asked < mine && lane == 0 && !failed)
-            tc_load_box(ring + (uint32_t)(slot * kFewUnit), &code_map, &s_full[warp][slot], kFewUnit, (int)(c0 >> 1), row);
-        c.load(scales, at, at + 8 * per_row, ((left > 0 ? 3u : 0u) | (left > 8 ? 12u : 0u)) & lanes);
-        ++asked, row += step * 16, left -= step * 16, at += jump;
+        if (asked < mine && lane == 0 && !failed) {
+            if (GATED) tc_load_box3(ring + (uint32_t)(slot * kFewUnit), &code_map, &s_full[warp][slot], kFewUnit, (int)(c0 >> 1), row, 0);
+            else tc_load_box(ring + (uint32_t)(slot * kFewUnit), &code_map, &s_full[warp][slot], kFewUnit, (int)(c0 >> 1), row);
+        }
+        c.load(scales, at, at + other, ((left > 0 ? 3u : 0u) | (left > (GATED ? 0 : 8) ? 12u : 0u)) & lanes);
+        ++asked, row += step * R, left -= step * R, at += jump;
     };
     if (lane < kFewSlots) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_full[warp][lane])) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -127,7 +132,24 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
         if (k == D - 1 || i + 1 == rounds) {
             __syncthreads();
             // the k + 1 row tiles of each group since the last time; rows along the lanes, so that neighbours write neighbours
-            for (uint32_t w = (uint32_t)tid >> 4; w < (uint32_t)((k + 1) * work.groups * tokens); w += FewGeo<NT>::threads / 16) {
+            if (GATED) {
+                for (uint32_t w = (uint32_t)tid >> 3; w < (uint32_t)((k + 1) * work.groups * tokens); w += FewGeo<NT>::threads / 8) {
+                    const uint32_t rest = w / (uint32_t)tokens, t = w - rest * (uint32_t)tokens, j = rest / (uint32_t)work.groups, gr = rest - j * (uint32_t)work.groups;
+                    const int64_t tile = (int64_t)peer * work.groups + gr + (int64_t)(i - k + (int)j) * step, f = tile * 8 + (lane & 7);
+                    const float* p = s_part + ((buf * D + j) * W + gr * work.stripes) * P + t * kFewPitch + (lane & 7);
+                    if (f >= out.n) continue;
+                    float gate = 0.0f, up = 0.0f;
+#pragma unroll 8
+                    for (int s = 0; s < work.stripes; ++s) gate += p[s * P], up += p[s * P + 8];
+                    if (work.slices > 1) {
+                        float* const to = sums + ((int64_t)slice * tokens + t) * (work.tiles * 16) + tile * 16 + (lane & 7);
+                        to[0] = gate, to[8] = up;
+                    } else {
+                        const float* const c = correction ? correction + (int64_t)t * rows + f : nullptr;
+                        out.store_pair(gate + (c ? c[0] : 0.0f), up + (c ? c[out.n] : 0.0f), t, f);
+                    }
+                }
+            } else for (uint32_t w = (uint32_t)tid >> 4; w < (uint32_t)((k + 1) * work.groups * tokens); w += FewGeo<NT>::threads / 16) {
                 const uint32_t rest = w / (uint32_t)tokens, t = w - rest * (uint32_t)tokens, j = rest / (uint32_t)work.groups, gr = rest - j * (uint32_t)work.groups;
                 const int64_t r = ((int64_t)peer * work.groups + gr + (int64_t)(i - k + (int)j) * step) * 16 + (lane & 15);
                 const float* p = s_part + ((buf * D + j) * W + gr * work.stripes) * P + t * kFewPitch + (lane & 15);
@@ -179,6 +201,20 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
             for (int u = 0; u < 4; ++u) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
         }
         const float z[4] = {sum.x, sum.y, sum.z, sum.w};
+        if (GATED) {  // the lane two further has the up rows of the first two lanes' columns (it takes part in whatever they do)
+            const unsigned int four = 0xfu << (lane & ~3);
+            float up[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) up[u] = __shfl_down_sync(four, z[u], 2);
+            if (lane & 2) continue;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t f = tile * 8 + 4 * (lane & 1) + u;
+                const float* const c = correction ? correction + (int64_t)t * rows + f : nullptr;
+                if (f < out.n) out.store_pair(z[u] + (c ? c[0] : 0.0f), up[u] + (c ? c[out.n] : 0.0f), t, f);
+            }
+            continue;
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (r + u < rows)
@@ -328,20 +364,25 @@ int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, co
     p.work.epoch = tc_next_epoch();
     int rc;
     CUtensorMap code_map;
-    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 128, 16, &code_map))) return rc;
-#define BOF4_FEW_GO(NT_, ST_, HALF_)                                                                                                              \
+    const int64_t ffn = w.rows / 2;
+    if ((rc = out.gated ? tc_make_map3(who, w.codes, 1, w.cols / 2, ffn, 2, w.cols / 2, ffn * (w.cols / 2), 128, 8, 2, &code_map)
+                        : tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 128, 16, &code_map)))
+        return rc;
+#define BOF4_FEW_GO(NT_, ST_, HALF_, GATED_)                                                                                                              \
     {                                                                                                                                             \
-        constexpr auto kern = linear_few_kernel<NT_, ST_, HALF_>;                                                                                 \
+        constexpr auto kern = linear_few_kernel<NT_, ST_, HALF_, GATED_>;                                                                                 \
         constexpr int smem = (int)kFewRing + FewGeo<NT_>::ring - kFewBegin;  \
         if ((rc = ensure_dynamic_smem<kern>(smem))) return rc;                                                                       \
         launch_after(kern, p.grid, FewGeo<NT_>::threads, smem, st, code_map, w.scales, w.rows, w.cols, w.block_shift, w.levels, xb,   \
                      ldx, out, correction, status, p.work, reinterpret_cast<unsigned long long*>(base), reinterpret_cast<float*>(base + p.sums)); \
     }
-#define BOF4_FEW_S(NT_, ST_) { if (w.block_size == 32) BOF4_FEW_GO(NT_, ST_, true) else BOF4_FEW_GO(NT_, ST_, false) }
+#define BOF4_FEW_H(NT_, ST_, HALF_) { if (out.gated) BOF4_FEW_GO(NT_, ST_, HALF_, true) else BOF4_FEW_GO(NT_, ST_, HALF_, false) }
+#define BOF4_FEW_S(NT_, ST_) { if (w.block_size == 32) BOF4_FEW_H(NT_, ST_, true) else BOF4_FEW_H(NT_, ST_, false) }
 #define BOF4_FEW_N(NT_) { if (w.scale_dtype == BOF4_F32) BOF4_FEW_S(NT_, F32) else BOF4_FEW_S(NT_, BF16) }
     if (out.tokens > 8) BOF4_FEW_N(2) else BOF4_FEW_N(1)
 #undef BOF4_FEW_N
 #undef BOF4_FEW_S
+#undef BOF4_FEW_H
 #undef BOF4_FEW_GO
     BOF4_CUDA_TRY(cudaGetLastError());
     return BOF4_OK;

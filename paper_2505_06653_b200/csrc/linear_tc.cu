@@ -93,7 +93,7 @@ __device__ __forceinline__ void lt_load16(uint32_t addr, uint32_t (&v)[16])
 // weights of the tile << 16 | value}.  Positions are distinct, so the order within a list does not matter.
 __global__ void __launch_bounds__(256)
 linear_outlier_lists(const int32_t* __restrict__ idx, const uint16_t* __restrict__ val, const int64_t* __restrict__ n_out, int64_t capacity,
-                     int64_t rows, int64_t cols, bool backward, int blocks, int* __restrict__ heads, int2* __restrict__ nodes)
+                     int64_t rows, int64_t cols, bool backward, bool gated, int blocks, int* __restrict__ heads, int2* __restrict__ nodes)
 {
     if (!after_previous()) return;
     int64_t end = *n_out;
@@ -102,7 +102,8 @@ linear_outlier_lists(const int32_t* __restrict__ idx, const uint16_t* __restrict
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < end; k += (int64_t)gridDim.x * 256) {
         const int64_t i = idx[k];
         if (i < 0 || i >= n) continue;
-        const int r = (int)(i / cols), c = (int)(i - (int64_t)r * cols);
+        const int row = (int)(i / cols), c = (int)(i - (int64_t)row * cols), ffn = (int)(rows >> 1);
+        const int r = !gated ? row : row < ffn ? 2 * row : 2 * (row - ffn) + 1;  // gated tiles have gate and up rows in turn
         const int thread = backward ? (c >> 6 & 1) * 64 + (r & 63) : r & 127;
         const int64_t tile = backward ? c >> 7 : r >> 7, block = backward ? r >> 6 : c >> 6;
         const int next = atomicExch(heads + (tile * blocks + block) * 4 + (thread >> 5), (int)k);
@@ -196,8 +197,41 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, in
     }
 }
 
+// The same of a gated tile: lane pairs have column f of the gate and of the up rows; the even lane takes the even tokens.
+__device__ __forceinline__ void lt_result_pair(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t f, bool live, int lane)
+{
+    float z[16];
+    __syncwarp();
+    lt_sums(src, accs, z);
+    const bool odd = lane & 1;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z[k] += b;
+    if (out.pre && live) {
+        uint16_t* const p = out.pre + t0 * out.ld_pre + (odd ? out.n : 0) + f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (k < count) p[k * out.ld_pre] = bf16_round(z[k]);
+    }
+    float g[8], u[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float other = __shfl_xor_sync(kFull, odd ? z[2 * k] : z[2 * k + 1], 1);
+        g[k] = odd ? other : z[2 * k], u[k] = odd ? z[2 * k + 1] : other;
+    }
+    activate_all(g, out.act);
+    const int64_t at = (t0 + odd) * out.ldy + f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (!live || 2 * k + odd >= count) continue;
+        const float v = g[k] * u[k];
+        if (out.y_bf16) static_cast<uint16_t*>(out.y)[at + 2 * k * out.ldy] = bf16_round(v);
+        else static_cast<float*>(out.y)[at + 2 * k * out.ldy] = v;
+    }
+}
+
 // HALF: blocks of 32 weights, two constants per thread and k-block.  LUT: half of the codes are looked up in a table of pairs.
-template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT>
+// GATED (forward): a tile holds 64 gate rows and the 64 up rows of the same columns of the result, in turn.
+template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT, bool GATED>
 __global__ void __launch_bounds__(kLtThreads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap token_map, const void* __restrict__ scales,
                  int64_t cols, int block_shift, int64_t last_scale, const float* __restrict__ levels, const LinearOut out,
@@ -232,7 +266,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
     };
     if (tid == 0) {
-        if (blockIdx.x == 0) *status = 0;  // long before any wait can have run out
+        if (blockIdx.x == 0 && !out.keep_status) *status = 0;  // long before any wait can have run out
         s_fail = s_sums = 0;
         for (int s = 0; s < kLtGroups; ++s) init(&s_full[s], 4 + 1), init(&s_empty[s], 1);  // four warps of producers, and the tokens
         for (int s = 0; s < work.halves; ++s) init(&s_half_full[s], 1), init(&s_half_empty[s], 8);
@@ -260,6 +294,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
         int ct = tile0, ci = in0, unasked = lines;
         auto first_of = [&](int t, int i) -> int64_t {
             const int64_t tm = (uint32_t)t / (uint32_t)work.tiles_n, k = (int64_t)i * kLtGroups + group;
+            if (GATED) return ((row & 1) * out.n + tm * (kLtM / 2) + (row >> 1)) * cols + k * kLtK;
             return BWD ? (k * kLtK + row) * cols + tm * kLtM + half * 64 : (tm * kLtM + row) * cols + k * kLtK;
         };
         int64_t weight = first_of(ct, ci);
@@ -430,15 +465,21 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             for (int n = 0; ok && n < lines; ++n) {
                 if (n + kLtAhead < lines) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&code_map)),
+                    for (int h = 0; h < 2; ++h) {
+                        if (GATED)
+                            asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, 0, %2}];" ::"l"(reinterpret_cast<uint64_t>(&code_map)),
+                                         "r"(x_of(pt, pi, h)), "r"(y_of(pt, pi, h) >> 1)
+                                         : "memory");
+                        else asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&code_map)),
                                      "r"(x_of(pt, pi, h)), "r"(y_of(pt, pi, h))
                                      : "memory");
+                    }
                     if (++pi == per_tile) pi = 0, ++pt;
                 }
                 for (int h = 0; h < 2; ++h) {
                     if (!(ok = tc_wait(smem_u32(&s_half_empty[slot]), par ^ 1u))) break;
-                    tc_load_box(code_ring + (uint32_t)slot * kLtHalfBytes, &code_map, &s_half_full[slot], kLtHalfBytes, x_of(tile, in, h), y_of(tile, in, h));
+                    if (GATED) tc_load_box3(code_ring + (uint32_t)slot * kLtHalfBytes, &code_map, &s_half_full[slot], kLtHalfBytes, x_of(tile, in, h), 0, y_of(tile, in, h) >> 1);
+                    else tc_load_box(code_ring + (uint32_t)slot * kLtHalfBytes, &code_map, &s_half_full[slot], kLtHalfBytes, x_of(tile, in, h), y_of(tile, in, h));
                     if (++slot == work.halves) slot = 0, par ^= 1u;
                 }
                 if (++in == per_tile) in = 0, ++tile;
@@ -467,7 +508,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             const int tile = tile0 + seg, t0 = tile * per_tile;
             const int64_t o = (int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * kLtM + m, token0 = (int64_t)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
             const int count = (int)(out.tokens - token0 < box_n ? out.tokens - token0 : box_n);
-            const bool all = begin <= t0 && finish >= t0 + per_tile, live = o < out.n;
+            const bool all = begin <= t0 && finish >= t0 + per_tile, live = (GATED ? o >> 1 : o) < out.n;
             const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * kLtMaxN);
             float* const part = parts + (2 * (int64_t)blockIdx.x + (begin <= t0 ? 1 : 0)) * kLtM * box_n;
             if (!all) {
@@ -479,8 +520,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                     for (int k = 0; k < 16; ++k) to[k * kLtM] = z[k];  // (count is padded to 16 in the workspace)
                 }
             } else {
-                const float b = live ? out.bias_at(o) : 0.0f;
-                for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
+                const float b = live ? out.bias_at(GATED ? (o & 1) * out.n + (o >> 1) : o) : 0.0f;
+                if (GATED)
+                    for (int q = 0; q < count; q += 16) lt_result_pair(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o >> 1, live, lane);
+                else for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -532,6 +575,17 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 for (int w = 0; w < 2; ++w)
 #pragma unroll
                     for (int u = 0; u < B; ++u) sum[u].x += v[w][u].x, sum[u].y += v[w][u].y, sum[u].z += v[w][u].z, sum[u].w += v[w][u].w;
+            }
+            if (GATED) {
+#pragma unroll
+                for (int u = 0; u < B; ++u) {
+                    const int e = e0 + u * kLtThreads;
+                    const int64_t f = (o0 >> 1) + (e & 31) * 2;
+                    if (e >= count * (kLtM / 4)) continue;
+                    if (f < out.n) out.store_pair(sum[u].x, sum[u].y, token0 + (e >> 5), f);
+                    if (f + 1 < out.n) out.store_pair(sum[u].z, sum[u].w, token0 + (e >> 5), f + 1);
+                }
+                continue;
             }
             LinearFour four[B];
 #pragma unroll
@@ -632,7 +686,9 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
     p.work.epoch = tc_next_epoch();
     CUtensorMap code_map, token_map;
     int rc;
-    if ((rc = tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 64, kLtM, &code_map)) ||
+    const int64_t ffn = w.rows / 2;
+    if ((rc = out.gated ? tc_make_map3(who, w.codes, 1, w.cols / 2, 2, ffn, ffn * (w.cols / 2), w.cols / 2, 64, 2, kLtM / 2, &code_map)
+                        : tc_make_map(who, w.codes, 1, w.cols / 2, w.rows, w.cols / 2, 64, kLtM, &code_map)) ||
         (rc = tc_make_map(who, operand, 2, backward ? w.rows : w.cols, out.tokens, ld * 2, 128, p.work.box_n, &token_map)))
         return rc;
     int* heads = nullptr;
@@ -643,23 +699,25 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
         BOF4_CUDA_TRY(cudaMemsetAsync(heads, 0xff, (size_t)p.tiles_m * p.blocks * 16, st));
         const int64_t want = (w.capacity + 255) / 256;
         launch_after(linear_outlier_lists, (int)(want < 4 * kSMs ? want : 4 * kSMs), 256, 0, st, w.out_idx, w.out_val, w.n_out, w.capacity, w.rows,
-                     w.cols, backward, p.blocks, heads, nodes);
+                     w.cols, backward, out.gated, p.blocks, heads, nodes);
         BOF4_CUDA_TRY(cudaGetLastError());
     }
     const int64_t last_scale = w.rows * w.cols / w.block_size - 1;
     float* const parts = reinterpret_cast<float*>(base + p.parts);
-#define BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, LUT_)                                                                                                  \
+#define BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, LUT_, GATED_)                                                                                                  \
     {                                                                                                                                             \
-        constexpr auto kern = linear_tc_kernel<BWD_, ST_, HALF_, OPQ_, LUT_>;                                                                     \
+        constexpr auto kern = linear_tc_kernel<BWD_, ST_, HALF_, OPQ_, LUT_, GATED_>;                                                                     \
         if ((rc = ensure_dynamic_smem<kern>(kLtSmem))) return rc;                                                                                 \
         launch_after(kern, p.ctas, kLtThreads, kLtSmem, st, code_map, token_map, w.scales, w.cols, w.block_shift, last_scale, w.levels, out,      \
                      status, heads, nodes, p.work, base, parts);                                                                                  \
     }
-#define BOF4_LT_T(BWD_, ST_, HALF_, OPQ_) { if (p.work.table) BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, true) else BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, false) }
-#define BOF4_LT_O(BWD_, ST_, HALF_) { if (opq) BOF4_LT_T(BWD_, ST_, HALF_, true) else BOF4_LT_T(BWD_, ST_, HALF_, false) }
-#define BOF4_LT_H(BWD_, ST_) { if (w.block_size == 32) BOF4_LT_O(BWD_, ST_, true) else BOF4_LT_O(BWD_, ST_, false) }
-#define BOF4_LT_S(BWD_) { if (w.scale_dtype == BOF4_F32) BOF4_LT_H(BWD_, F32) else BOF4_LT_H(BWD_, BF16) }
-    if (backward) BOF4_LT_S(true) else BOF4_LT_S(false)
+#define BOF4_LT_T(BWD_, ST_, HALF_, OPQ_, GATED_) { if (p.work.table) BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, true, GATED_) else BOF4_LT_GO(BWD_, ST_, HALF_, OPQ_, false, GATED_) }
+#define BOF4_LT_O(BWD_, ST_, HALF_, GATED_) { if (opq) BOF4_LT_T(BWD_, ST_, HALF_, true, GATED_) else BOF4_LT_T(BWD_, ST_, HALF_, false, GATED_) }
+#define BOF4_LT_H(BWD_, ST_, GATED_) { if (w.block_size == 32) BOF4_LT_O(BWD_, ST_, true, GATED_) else BOF4_LT_O(BWD_, ST_, false, GATED_) }
+#define BOF4_LT_S(BWD_, GATED_) { if (w.scale_dtype == BOF4_F32) BOF4_LT_H(BWD_, F32, GATED_) else BOF4_LT_H(BWD_, BF16, GATED_) }
+    if (backward) BOF4_LT_S(true, false)
+    else if (out.gated) BOF4_LT_S(false, true)
+    else BOF4_LT_S(false, false)
 #undef BOF4_LT_S
 #undef BOF4_LT_H
 #undef BOF4_LT_O

@@ -100,6 +100,15 @@ __device__ __forceinline__ void tc_arrive(unsigned long long* bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void tc_load_box3(uint32_t dst, const CUtensorMap* map, unsigned long long* bar, uint32_t bytes, int x, int y, int z)
+{
+    const uint32_t b = smem_u32(bar);
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 :
+                 : "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(b), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
 __device__ __forceinline__ void tc_load_box(uint32_t dst, const CUtensorMap* map, unsigned long long* bar, uint32_t bytes, int x, int y)
 {
     const uint32_t b = smem_u32(bar);
@@ -149,8 +158,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 // Tensor map of a row-major matrix of 2-byte (bf16) or 1-byte elements, `pitch` bytes between rows, with a box of `box_bytes`
 // (128 or 64) x box_rows and the swizzle of that width: operands land in the layout that the tcgen05 descriptors name, codes
 // in one that sixteen-byte reads of neighbouring rows find without bank conflicts.  Elements outside the matrix read as zero.
-inline int tc_make_map(const char* who, const void* p, int esize, int64_t cols, int64_t rows, int64_t pitch, int box_bytes, int box_rows,
-                       CUtensorMap* map)
+// With a third dimension: `count` such matrices, `stride` bytes apart, and a box of box_bytes x box_rows x box_count.
+inline int tc_make_map3(const char* who, const void* p, int esize, int64_t cols, int64_t rows, int64_t count, int64_t pitch, int64_t stride, int box_bytes,
+                        int box_rows, int box_count, CUtensorMap* map)
 {
     static std::atomic<EncodeTiledFn> known{nullptr};
     EncodeTiledFn fn = known.load(std::memory_order_relaxed);
@@ -165,11 +175,11 @@ inline int tc_make_map(const char* who, const void* p, int esize, int64_t cols, 
         fn = reinterpret_cast<EncodeTiledFn>(f);
         known.store(fn, std::memory_order_relaxed);
     }
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {(cuuint32_t)(box_bytes / esize), (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(map, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims,
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch, (cuuint64_t)stride};
+    const cuuint32_t box[3] = {(cuuint32_t)(box_bytes / esize), (cuuint32_t)box_rows, (cuuint32_t)box_count};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, count ? 3 : 2, const_cast<void*>(p), dims,
                           strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -178,6 +188,12 @@ inline int tc_make_map(const char* who, const void* p, int esize, int64_t cols, 
         return BOF4_ERR_CUDA;
     }
     return BOF4_OK;
+}
+
+inline int tc_make_map(const char* who, const void* p, int esize, int64_t cols, int64_t rows, int64_t pitch, int box_bytes, int box_rows,
+                       CUtensorMap* map)
+{
+    return tc_make_map3(who, p, esize, cols, rows, 0, pitch, 0, box_bytes, box_rows, 0, map);
 }
 
 // A name for every launch, no two alike: 56 bits that mix a counter with the time the library was loaded.

@@ -579,6 +579,151 @@ PyObject* linear_backward(PyObject* const* a)
     return PyTuple_Pack(3, rdx.p, rdb.p, rs.p);
 }
 
+// (codes, scales, ffn, cols, block_size, levels, x, bias, activation, out_dtype, pre, outliers, out, workspace)
+PyObject* gated(PyObject* const* a)
+{
+    check_grad("bof4_gated", a, {{1, "scales"}, {5, "levels"}, {6, "x"}, {7, "bias"}, {10, "pre"}, {11, "outliers"}, {12, "out"}});
+    const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
+    const int64_t ffn = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
+    if (ffn < 0 || ffn > INT32_MAX / 2) fail(PyExc_ValueError, "ffn must be in 0 ... 2^30 - 1");
+    check_matrix(codes, scales, 2 * ffn, cols, block);
+    const at::Device d = codes.device();
+    if (tensor(a[6], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, cols]");
+    const int64_t n = tensor(a[6], "x").size(0);
+    const Rows x(a[6], "x", n, cols, at::kBFloat16, d);
+    const int od = small(a[9], "out_dtype"), act = small(a[8], "activation"), sd = dtype_code(scales);
+    if (od != BOF4_F32 && od != BOF4_BF16) fail(PyExc_ValueError, "out_dtype must be F32 or BF16");
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[5], d);
+    const Outliers o(a[11]);
+    check_outliers(o, d);
+    at::Tensor bias;
+    int bd = BOF4_F32;
+    if (!none(a[7])) {
+        bias = dev(a[7], "bias");
+        bd = dtype_code(bias);
+        if (bias.numel() != 2 * ffn || bias.device() != d) fail(PyExc_ValueError, "bias must hold one value per row, on the device of the weights");
+    }
+    std::optional<Rows> pre, out;
+    if (!none(a[10])) pre.emplace(a[10], "pre", n, 2 * ffn, at::kBFloat16, d);
+    if (!none(a[12])) out.emplace(a[12], "out", n, ffn, torch_dtype(od), d);
+    at::Tensor made[3], ws;  // the status (written by the call), the workspace, the result
+    Spec spec[3];
+    size_t k = 0;
+    spec[k++] = {1, at::kInt};
+    const size_t i_ws = k;
+    if (none(a[13])) spec[k++] = {(int64_t)bof4_gated_workspace_bytes(ffn, cols, n, 0, o.idx ? o.cap : 0), at::kByte};
+    else ws = given_workspace(a[13], d);
+    const size_t i_h = k;
+    if (!out) spec[k++] = {n * ffn, torch_dtype(od)};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        return bof4_gated(static_cast<const uint8_t*>(codes.const_data_ptr()), scales.const_data_ptr(), sd, ffn, cols, (int)block, levels_ptr(cb), x.ptr(),
+                          x.ld, n, bias.defined() ? bias.const_data_ptr() : nullptr, bd, act, o.idx, o.val, o.cnt, o.cap,
+                          out ? out->ptr() : made[i_h].data_ptr(), od, out ? out->ld : ffn, pre ? pre->ptr() : nullptr, pre ? pre->ld : 0,
+                          static_cast<int*>(made[0].data_ptr()), w.data_ptr(), (size_t)w.numel(), stream_of(d));
+    });
+    Ref rs(wrap(made[0])), rh(out ? Py_NewRef(a[12]) : wrap(made[i_h].view({n, ffn})));
+    return PyTuple_Pack(2, rh.p, rs.p);
+}
+
+// (codes, scales, ffn, cols, block_size, levels, dh, pre, activation, want_dx, want_dbias, outliers, out, workspace)
+PyObject* gated_backward(PyObject* const* a)
+{
+    check_grad("bof4_gated_backward", a, {{1, "scales"}, {5, "levels"}, {6, "dh"}, {7, "pre"}, {11, "outliers"}, {12, "out"}});
+    const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales");
+    const int64_t ffn = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
+    if (ffn < 0 || ffn > INT32_MAX / 2) fail(PyExc_ValueError, "ffn must be in 0 ... 2^30 - 1");
+    check_matrix(codes, scales, 2 * ffn, cols, block);
+    const at::Device d = codes.device();
+    if (tensor(a[6], "dh").dim() != 2) fail(PyExc_ValueError, "dh must be [n_tokens, ffn]");
+    const int hd = dtype_code(tensor(a[6], "dh")), act = small(a[8], "activation"), sd = dtype_code(scales);
+    const int64_t n = tensor(a[6], "dh").size(0);
+    const Rows dh(a[6], "dh", n, ffn, torch_dtype(hd), d), pre(a[7], "pre", n, 2 * ffn, at::kBFloat16, d);
+    const bool want_dx = truth(a[9]), want_db = truth(a[10]);
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[5], d);
+    const Outliers o(a[11]);
+    check_outliers(o, d);
+    std::optional<Rows> out;
+    if (!none(a[12])) out.emplace(a[12], "out", n, cols, at::kBFloat16, d);
+    at::Tensor made[4], ws;
+    Spec spec[4];
+    size_t k = 0;
+    spec[k++] = {1, at::kInt};
+    const size_t i_db = k;
+    if (want_db) spec[k++] = {2 * ffn, at::kFloat};
+    const size_t i_ws = k;
+    if (none(a[13])) spec[k++] = {(int64_t)bof4_gated_workspace_bytes(ffn, cols, n, 1, o.idx ? o.cap : 0), at::kByte};
+    else ws = given_workspace(a[13], d);
+    const size_t i_dx = k;
+    if (want_dx && !out) spec[k++] = {n * cols, at::kBFloat16};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        void* const dx = !want_dx ? nullptr : out ? out->ptr() : made[i_dx].data_ptr();
+        return bof4_gated_backward(static_cast<const uint8_t*>(codes.const_data_ptr()), scales.const_data_ptr(), sd, ffn, cols, (int)block, levels_ptr(cb),
+                                   dh.ptr(), hd, dh.ld, n, pre.ptr(), pre.ld, act, o.idx, o.val, o.cnt, o.cap, dx, out ? out->ld : cols,
+                                   want_db ? static_cast<float*>(made[i_db].data_ptr()) : nullptr, static_cast<int*>(made[0].data_ptr()), w.data_ptr(),
+                                   (size_t)w.numel(), stream_of(d));
+    });
+    Ref rs(wrap(made[0]));
+    Ref rdx(!want_dx ? Py_NewRef(Py_None) : out ? Py_NewRef(a[12]) : wrap(made[i_dx].view({n, cols})));
+    Ref rdb(want_db ? wrap(made[i_db]) : Py_NewRef(Py_None));
+    return PyTuple_Pack(3, rdx.p, rdb.p, rs.p);
+}
+
+// (codes, scales, rows, cols, block_size, levels, x, targets, dloss, want_dx, outliers, out, workspace)
+PyObject* cross_entropy(PyObject* const* a)
+{
+    check_grad("bof4_cross_entropy", a, {{1, "scales"}, {5, "levels"}, {6, "x"}, {8, "dloss"}, {10, "outliers"}, {11, "out"}});
+    const at::Tensor codes = dev(a[0], "codes"), scales = dev(a[1], "scales"), targets = dev(a[7], "targets");
+    const int64_t rows = integer(a[2]), cols = integer(a[3]), block = integer(a[4]);
+    check_matrix(codes, scales, rows, cols, block);
+    const at::Device d = codes.device();
+    if (tensor(a[6], "x").dim() != 2) fail(PyExc_ValueError, "x must be [n_tokens, cols]");
+    const int64_t n = tensor(a[6], "x").size(0);
+    const Rows x(a[6], "x", n, cols, at::kBFloat16, d);
+    if (targets.scalar_type() != at::kLong || targets.dim() != 1 || targets.size(0) != n || targets.device() != d)
+        fail(PyExc_ValueError, "targets must be int64 [n_tokens] on the device of the weights");
+    at::Tensor dloss;
+    if (!none(a[8])) {
+        dloss = dev(a[8], "dloss");
+        if (dloss.scalar_type() != at::kFloat || dloss.dim() != 1 || dloss.size(0) != n || dloss.device() != d)
+            fail(PyExc_ValueError, "dloss must be float32 [n_tokens] on the device of the weights");
+    }
+    const int sd = dtype_code(scales);
+    const bool want_dx = truth(a[9]);
+    const c10::cuda::CUDAGuard guard(d);
+    const at::Tensor cb = codebook(a[5], d);
+    const Outliers o(a[10]);
+    check_outliers(o, d);
+    std::optional<Rows> out;
+    if (!none(a[11])) {
+        if (!want_dx) fail(PyExc_ValueError, "out is for dx, which is not wanted");
+        out.emplace(a[11], "out", n, cols, at::kBFloat16, d);
+    }
+    at::Tensor made[5], ws;
+    Spec spec[5] = {{1, at::kInt}, {n, at::kFloat}, {n, at::kFloat}};
+    size_t k = 3;
+    const size_t i_ws = k;
+    if (none(a[12])) spec[k++] = {(int64_t)bof4_cross_entropy_workspace_bytes(rows, cols, n, want_dx, o.idx ? o.cap : 0), at::kByte};
+    else ws = given_workspace(a[12], d);
+    const size_t i_dx = k;
+    if (want_dx && !out) spec[k++] = {n * cols, at::kBFloat16};
+    make_and_call(made, spec, k, d, [&] {
+        const at::Tensor& w = ws.defined() ? ws : made[i_ws];
+        void* const dx = !want_dx ? nullptr : out ? out->ptr() : made[i_dx].data_ptr();
+        return bof4_cross_entropy(static_cast<const uint8_t*>(codes.const_data_ptr()), scales.const_data_ptr(), sd, rows, cols, (int)block, levels_ptr(cb),
+                                  x.ptr(), x.ld, n, static_cast<const int64_t*>(targets.const_data_ptr()),
+                                  dloss.defined() ? static_cast<const float*>(dloss.const_data_ptr()) : nullptr, o.idx, o.val, o.cnt, o.cap,
+                                  static_cast<float*>(made[1].data_ptr()), static_cast<float*>(made[2].data_ptr()), dx, out ? out->ld : cols,
+                                  static_cast<int*>(made[0].data_ptr()), w.data_ptr(), (size_t)w.numel(), stream_of(d));
+    });
+    Ref rs(wrap(made[0])), rl(wrap(made[1])), re(wrap(made[2]));
+    Ref rdx(!want_dx ? Py_NewRef(Py_None) : out ? Py_NewRef(a[11]) : wrap(made[i_dx].view({n, cols})));
+    return PyTuple_Pack(4, rl.p, re.p, rdx.p, rs.p);
+}
+
 // (x, router, gate_up, down, ffn, block_size, levels, top_k, activation, score, renormalize, scale, out_dtype, out, workspace)
 PyObject* moe(PyObject* const* a)
 {
@@ -882,7 +1027,8 @@ PyMethodDef g_methods[] = {
     BOF4_ENTRY(set_hooks, 2), BOF4_ENTRY(set_allocator, 1), BOF4_ENTRY(quantize, 6), BOF4_ENTRY(dequantize, 8),
     BOF4_ENTRY(gemv, 9), BOF4_ENTRY(gemm_tc, 10), BOF4_ENTRY(quantize_opq, 9), BOF4_ENTRY(outlier_count, 2),
     BOF4_ENTRY(quantize_batch, 6), BOF4_ENTRY(dequantize_batch, 7), BOF4_ENTRY(scales_compress, 2), BOF4_ENTRY(scales_expand, 3),
-    BOF4_ENTRY(fit_codebook, 10), BOF4_ENTRY(linear, 15), BOF4_ENTRY(moe, 15), BOF4_ENTRY(linear_backward, 14), {nullptr, nullptr, 0, nullptr}};
+    BOF4_ENTRY(fit_codebook, 10), BOF4_ENTRY(linear, 15), BOF4_ENTRY(moe, 15), BOF4_ENTRY(linear_backward, 14), BOF4_ENTRY(gated, 14),
+    BOF4_ENTRY(gated_backward, 14), BOF4_ENTRY(cross_entropy, 13), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bof4_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
