@@ -7,9 +7,10 @@
 // loss = log(1 + S e^-a) and p_y - 1 = -S / (S + e^a), so that nothing cancels where the target has next to all of the probability.
 //
 // Few tokens: the logits of all rows (fp32) fit a workspace; the products are those of bof4_linear and its backward pass, which decode as
-// they multiply.  Two kernels between them: sums of 2048 logits each, and dz = g (p - [v = y]) in bf16.
+// they multiply.  Two kernels between them: sums of 2048 logits each, and dz in bf16, in units of g (1 - p_y): the target's entry, often the
+// largest by far, is -1 and needs no rounding, and the second product's results are multiplied by the unit.
 //
-// Many tokens: the vocabulary in pieces of at most 16384 rows, so that neither logits nor a decoded matrix is kept.  A piece is
+// Many tokens: the vocabulary in pieces of at most 32768 rows, so that neither logits nor a decoded matrix is kept.  A piece is
 // decoded once and multiplied twice (dense_tc.cu): the first product's results become E = exp(z - r) in bf16 and its sums in the
 // same kernel, the second adds E W^ to a running sum in fp32, as attention does with its keys as values:
 //   dx = g (sum_v E_v W^_v - S W^_y) / (S + e^a)
@@ -21,7 +22,7 @@
 namespace bof4 {
 
 constexpr int kCeChunk = 2048;        // logits of a CTA
-constexpr int kCePiece = 16384;       // rows of a piece
+constexpr int kCePiece = 32768;       // rows of a piece: half as many cost 29 us more per 4096 x 4096 running sums, which are read and written
 constexpr int kCePart = 64;           // columns of an entry of the product's sums
 constexpr int kCeParts = kCePiece / kCePart;
 
@@ -141,7 +142,7 @@ loss_token_kernel(const float2* __restrict__ stats, const float* __restrict__ ow
 __global__ void __launch_bounds__(256)
 loss_gradient_kernel(const float* __restrict__ logits, int64_t ld, int64_t n, int chunks, const float2* __restrict__ stats, const float* __restrict__ own,
                      const int64_t* __restrict__ targets, const float* __restrict__ dloss, float* __restrict__ loss, float* __restrict__ lse,
-                     uint16_t* __restrict__ dz, int* __restrict__ status)
+                     float* __restrict__ scale, uint16_t* __restrict__ dz, int* __restrict__ status)
 {
     if (!after_previous()) return;
     const int chunk = (int)(blockIdx.x % (unsigned)chunks), tid = threadIdx.x;
@@ -155,11 +156,11 @@ loss_gradient_kernel(const float* __restrict__ logits, int64_t ld, int64_t n, in
         ce_counted(target, n, status);
         loss[t] = c.loss;
         if (lse) lse[t] = c.lse;
+        scale[t] = counted ? (dloss ? dloss[t] : 1.0f) * c.rest : 0.0f;
     }
     if (c0 >= n) return;
-    const float g = dloss ? dloss[t] : 1.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = !counted ? 0.0f : target == c0 + k ? -g * c.rest : g * (c.scale * __expf(v[k] - s.x));
+    for (int k = 0; k < 8; ++k) v[k] = !counted || c.rest == 0.0f ? 0.0f : target == c0 + k ? -1.0f : __fdividef(c.scale, c.rest) * __expf(v[k] - s.x);
     // (rows are padded to eight)
     *reinterpret_cast<uint4*>(dz + t * ld + c0) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
@@ -326,9 +327,10 @@ __global__ void __launch_bounds__(256) loss_dx_kernel(const LossFinal f)
 namespace {
 
 #ifndef BOF4_LOSS_DENSE
-#define BOF4_LOSS_DENSE 512
+#define BOF4_LOSS_DENSE 385
 #endif
-// Tokens from which the vocabulary is taken in pieces.
+// Tokens from which the vocabulary is taken in pieces.  Both forms with the gradient, us: 32000 x 4096 by 256 tokens 207 against 258, 384 313 against 325, 512
+// 372 against 335, 1024 753 against 572; 128256 x 4096 by 384 1373 against 1317; without it 194 against 195 for 384, 239 against 184 for 512.
 bool loss_dense(int64_t tokens) { return tokens >= BOF4_LOSS_DENSE; }
 
 struct LossPlan {
@@ -337,7 +339,7 @@ struct LossPlan {
     int chunks;                  // few tokens
     int64_t pieces, piece;       // many
     size_t forward, backward;    // bytes of the products' workspaces, which share a place
-    size_t logits, stats, own, dz, w, ref, sum, factor, acc, total;
+    size_t logits, stats, own, scale, dz, w, ref, sum, factor, acc, total;
 };
 bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t capacity, LossPlan* p)
 {
@@ -362,6 +364,7 @@ bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t ca
         p->logits = take(t * p->ld * 4);
         p->stats = take(t * chunks * 8);
         p->own = take(t * 4);
+        p->scale = take(t * 4);
         p->dz = take(grad ? t * p->ld * 2 : 0);
         p->total = at;
         return true;
@@ -450,7 +453,6 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
     float2* const stats = reinterpret_cast<float2*>(base + p.stats);
     float* const own = floats(p.own);
     uint16_t* const dz = reinterpret_cast<uint16_t*>(base + p.dz);
-    BOF4_CUDA_TRY(cudaMemsetAsync(d_status, 0, sizeof(int), st));
     int rc;
     if (!p.dense) {
         float* const logits = floats(p.logits);
@@ -459,11 +461,11 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         out.ldy = p.ld;
         out.n = rows;
         out.tokens = n_tokens;
-        out.keep_status = true;
         out.set_alignment();
         if (linear_few_applies(rows, cols, n_tokens, w.capacity > 0)) rc = linear_few(fn, w, d_x, ldx, out, d_status, base, p.forward, st);
         else rc = linear_tc(fn, w, false, d_x, ldx, out, d_status, base, p.forward, st);
         if (rc) return rc;
+        float* const scale = floats(p.scale);
         launch_after(loss_chunk_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, d_targets, stats, own);
         if (!grad) {
             launch_after(loss_token_kernel, (int)((n_tokens + 7) / 8), 256, 0, st, stats, own, rows, p.chunks, d_targets, n_tokens, d_loss, d_lse, d_status);
@@ -471,7 +473,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
             return BOF4_OK;
         }
         launch_after(loss_gradient_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, stats, own, d_targets, d_dloss, d_loss, d_lse,
-                     dz, d_status);
+                     scale, dz, d_status);
         BOF4_CUDA_TRY(cudaGetLastError());
         LinearOut to{};
         to.y = d_dx;
@@ -480,12 +482,12 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         to.n = cols;
         to.tokens = n_tokens;
         to.keep_status = true;
+        to.scale = scale;
         to.set_alignment();
         return linear_tc(fn, w, true, dz, p.ld, to, d_status, base, p.backward, st);
     }
     float *const ref = floats(p.ref), *const sum = floats(p.sum), *const factor = floats(p.factor), *const acc = floats(p.acc);
     void* const decoded = base + p.w;
-    BOF4_CUDA_TRY(cudaMemsetAsync(ref, 0, (size_t)n_tokens * 4, st));
     for (int64_t r0 = 0; r0 < rows; r0 += p.piece) {
         const int64_t n = rows - r0 < p.piece ? rows - r0 : p.piece;
         const bool first = r0 == 0;
@@ -509,6 +511,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         out.stats = stats;
         out.target_logit = own;
         out.first = first;
+        out.keep_status = !first;
         if ((rc = dense_product(fn, DenseProduct{d_x, ldx, decoded, 0, cols, n, false, kDenseLoss}, out, d_status, base, p.forward, st))) return rc;
         launch_after(loss_combine_kernel, (int)((n_tokens + 31) / 32), 1024, 0, st, stats, (int)((n + kCePart - 1) / kCePart), n_tokens, first, ref, sum, factor,
                      grad ? dz : nullptr, p.ld, n);
@@ -520,6 +523,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         to.y = acc;
         to.ldy = cols;
         to.factor = first ? nullptr : factor;
+        to.keep_status = true;
         if ((rc = dense_product(fn, DenseProduct{dz, p.ld, decoded, 0, n, cols, true, kDenseAdd}, to, d_status, base, p.forward, st))) return rc;
     }
     LossFinal f{};

@@ -11,13 +11,15 @@
 //   16 results a warp has 32 tokens and a quarter of the columns of a finished accumulator (there are two); a lane keeps the 64
 //              sums of its token in registers
 //
-// The tensor cores cut a sum off at every step of 16 of K, so an accumulator takes 2048 of K at most, and the parts are added in
-// registers, rounded (1.8e-6 of the result in 2-norms for any K, where one accumulator has 7e-6 at K = 8192).  The accumulators
-// alternate, so this costs the tensor cores nothing.
+// The tensor cores cut a sum off at every step of 16 of K, so an accumulator takes a segment of K only, and the segments are added in
+// registers, rounded.  Results in fp32 (and logits) have segments of 1024 of K: losses with K = 4096 are off by 0.6e-6 in 2-norms, by 1.4e-6 with segments of
+// 2048, 3.6e-6 with one accumulator.  That is nothing beside a rounding to bf16 (1.7e-3), and each reading of an accumulator costs power, by which long products
+// are bound: 4096 tokens by 16384 x 4096 took 390 us with segments of 1024 and 353 with 2048 or 4096.
 //
-// Tiles: as many whole rounds of all clusters as there are but for the last one or two, whose tiles are dealt first, in equal
-// contiguous parts of their k-blocks; a tile that several clusters share is summed in their order by the one that completes it
-// last (a ticket: nobody waits).  256 tiles on 74 clusters would otherwise take four rounds for 3.46.
+// Tiles go to the clusters in turn.  What is left after the last whole round is cut along K into as many parts as there are clusters for
+// (74 / tiles, at most eight) where K is long enough to pay for it.  They come first; the sums of a
+// tile's parts are added in order by the SM that completes it last (a ticket: nobody waits).  256 tiles on 74 clusters take 3.5 rounds that way.  Equal shares of all k-blocks for every cluster (3.46 rounds) lost more
+// than that: clusters that stand at different places of K find nothing of one another's in L2 (4096 x 4096, K = 16384: 412 us).
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
 #include "dense_tc.cuh"
@@ -29,7 +31,6 @@ constexpr int kDnStages = 7;
 constexpr int kDnHalf = 128 * kDnK * 2;         // an SM's part of an operand in a stage
 constexpr int kDnStage = 2 * kDnHalf;
 constexpr int kDnSmem = kDnStages * kDnStage + 1024;
-constexpr int kDnSegment = 32;                  // k-blocks of an accumulator
 constexpr int kDnResults = 16, kDnCols = 64;    // warps that read results, columns of each
 constexpr int kDnLoads = kDnResults, kDnIssue = kDnResults + 1;
 constexpr int kDnThreads = 32 * (kDnResults + 2);
@@ -82,28 +83,24 @@ __device__ __forceinline__ void dn_read16(uint32_t addr, uint32_t (&v)[16])
         : "memory");
 }
 
-// The parts of tiles of a cluster in order: k-blocks k0 ... k1 - 1 of a tile.
+// The units of work of a cluster in order: k-blocks k0 ... k1 - 1 of a tile.
 struct DenseWalk {
-    int line, finish;  // k-blocks of the streamed tiles that are left
-    int next;          // whole tile
-    int tile, k0, k1;
-    __device__ __forceinline__ DenseWalk(const DenseWork& w, int cluster)
-    {
-        line = finish = 0;
-        if (cluster < w.parts) line = w.start(cluster), finish = w.start(cluster + 1);
-        next = w.streamed + cluster;
-    }
+    int next;
+    int unit, tile, k0, k1;
+    __device__ __forceinline__ explicit DenseWalk(int cluster) : next(cluster) {}
     __device__ __forceinline__ bool step(const DenseWork& w)
     {
-        if (line < finish) {
-            tile = (int)((uint32_t)line / (uint32_t)w.per_tile);
-            k0 = line - tile * w.per_tile;
-            k1 = w.per_tile < k0 + finish - line ? w.per_tile : k0 + finish - line;
-            line += k1 - k0;
-            return true;
+        unit = next;
+        const int cut = w.split * w.parts;
+        if (unit < cut) {
+            tile = unit / w.parts;
+            const int part = unit - tile * w.parts;
+            k0 = w.per_tile * part / w.parts, k1 = w.per_tile * (part + 1) / w.parts;
+        } else {
+            tile = unit - cut + w.split;
+            if (tile >= w.tiles_m * w.tiles_n) return false;
+            k0 = 0, k1 = w.per_tile;
         }
-        if (next >= w.tiles_m * w.tiles_n) return false;
-        tile = next, k0 = 0, k1 = w.per_tile;
         next += w.clusters;
         return true;
     }
@@ -225,7 +222,7 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCol
             top = fmaxf(top, z[k]);
         }
         if (inside) out.target_logit[t] = own;
-        float ref = out.ref[t];
+        float ref = out.first ? 0.0f : out.ref[t];
         if (top > ref + 24.0f || (out.first && top < ref - 24.0f && top > -INFINITY)) ref = top;
         if (ref == -INFINITY) ref = 0.0f;  // nothing but infinitely unlikely rows so far
         float sum = 0.0f;
@@ -263,6 +260,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
     };
     if (tid == 0) {
+        if (blockIdx.x == 0 && !out.keep_status) *status = 0;  // long before any wait can have run out
         s_fail = 0;
         for (int s = 0; s < kDnStages; ++s) init(&s_full[s], 1), init(&s_empty[s], 1);
         for (int b = 0; b < 2; ++b) init(&s_acc_full[b], 1), init(&s_acc_empty[b], 2 * kDnResults);
@@ -277,7 +275,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     dn_cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
-    DenseWalk walk(work, cluster);
+    DenseWalk walk(cluster);
 
     if (warp == kDnLoads) {
         if (tc_elect()) {
@@ -322,7 +320,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                     if (!(ok = tc_wait(smem_u32(&s_acc_empty[seg & 1]), (uint32_t)((seg >> 1) & 1) ^ 1u))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d = tmem + (uint32_t)((seg & 1) * kDnN);
-                    const int end = walk.k1 < k + kDnSegment ? walk.k1 : k + kDnSegment;
+                    const int end = walk.k1 < k + work.segment ? walk.k1 : k + work.segment;
                     for (uint32_t acc = 0u; k < end; ++k, acc = 1u) {
                         if (!(ok = tc_wait(smem_u32(&s_full[stage]), turn))) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -354,21 +352,15 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 512, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(ok ? 1u : 0u) : "memory");
             return r != 0u;
         };
-        if (tid == 0 && cluster < work.parts) {  // the tickets of the tiles that this cluster has parts of
-            const int first = work.start(cluster), last = work.start(cluster + 1) - 1;
-            if (last >= first) {
-                const int a = first / work.per_tile, b = last / work.per_tile;
-                tc_ticket_open(tickets + 2 * a + rank, work.epoch);
-                if (b != a) tc_ticket_open(tickets + 2 * b + rank, work.epoch);
-            }
-        }
+        if (tid == 0)
+            for (int u = cluster; u < work.split * work.parts; u += work.clusters) tc_ticket_open(tickets + 2 * (u / work.parts) + rank, work.epoch);
         int seg = 0;
         bool ok = true;
         while (ok && walk.step(work)) {
             float z[kDnCols];
 #pragma unroll
             for (int i = 0; i < kDnCols; ++i) z[i] = 0.0f;
-            for (int k = walk.k0; k < walk.k1; k += kDnSegment, ++seg) {
+            for (int k = walk.k0; k < walk.k1; k += work.segment, ++seg) {
                 const int buf = seg & 1;
                 ok = __all_sync(kFull, tc_wait(smem_u32(&s_acc_full[buf]), (uint32_t)(seg >> 1) & 1u));
                 if (!ok) break;
@@ -395,17 +387,16 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                 continue;
             }
             // a part of a tile
-            const int l0 = walk.tile * work.per_tile, i0 = work.owner(l0), i1 = work.owner(l0 + work.per_tile - 1);
             constexpr int64_t slab = 128 * kDnN;
-            auto slab_of = [&](int i) { return parts + ((int64_t)(2 * i + rank) * 2 + (work.start(i) < l0 ? 1 : 0)) * slab + part * kDnCols * 128 + row; };
-            float* const mine = slab_of(cluster);
+            auto slab_of = [&](int unit) { return parts + (int64_t)(2 * unit + rank) * slab + part * kDnCols * 128 + row; };
+            float* const mine = slab_of(walk.unit);
 #pragma unroll
             for (int k = 0; k < kDnCols; ++k) __stcg(mine + k * 128, z[k]);
             __threadfence();
             sync();
             if (tid == 0) {
                 unsigned long long* const cell = tickets + 2 * walk.tile + rank;
-                s_last = (int)(atomicAdd(cell, 1ull) & 255ull) == i1 - i0;
+                s_last = (int)(atomicAdd(cell, 1ull) & 255ull) == work.parts - 1;
                 if (s_last) *cell = 0ull;
             }
             sync();
@@ -413,8 +404,8 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             __threadfence();
 #pragma unroll
             for (int k = 0; k < kDnCols; ++k) z[k] = 0.0f;
-            for (int i = i0; i <= i1; ++i) {
-                const float* const p = slab_of(i);
+            for (int i = 0; i < work.parts; ++i) {
+                const float* const p = slab_of(walk.tile * work.parts + i);
 #pragma unroll
                 for (int k = 0; k < kDnCols; ++k) z[k] += __ldcg(p + k * 128);
             }
@@ -453,18 +444,18 @@ bool dense_plan(int64_t tokens, int64_t n, int64_t k, DensePlan* p)
     w.tiles_m = (int)tm;
     w.tiles_n = (int)tn;
     w.per_tile = (int)per;
-    const int64_t rounds = tiles / kDnClusters;
-    w.streamed = tiles % kDnClusters == 0 ? 0 : (int)(tiles - (rounds > 1 ? rounds - 1 : 0) * kDnClusters);
-    const int64_t lines = w.streamed * per;
-    if (lines > 0x3fffffff) return false;
-    int64_t parts = lines < kDnClusters ? lines : kDnClusters;
-    if (parts > (int64_t)w.streamed * kDnMaxParts) parts = (int64_t)w.streamed * kDnMaxParts;
+    const int64_t left = tiles % kDnClusters;
+    int64_t parts = left ? kDnClusters / left : 1;
+    if (parts > kDnMaxParts) parts = kDnMaxParts;
+    // a k-block takes 0.27 us, a part's sums 2.5 and those of the first two 6 more
+    while (parts > 1 && per < 10 * parts * parts) --parts;
+    if (per < 96) parts = 1;
     w.parts = (int)parts;
-    w.each = parts ? (int)(lines / parts) : 0;
-    w.extra = parts ? (int)(lines % parts) : 0;
-    w.clusters = (int)(tiles > w.streamed ? kDnClusters : parts);
-    p->parts = up256((size_t)w.streamed * 16);
-    p->total = p->parts + (size_t)w.parts * 4 * 128 * kDnN * 4;
+    w.split = parts > 1 ? (int)left : 0;
+    const int64_t units = tiles + w.split * (parts - 1);
+    w.clusters = (int)(units < kDnClusters ? units : kDnClusters);
+    p->parts = up256((size_t)w.split * 16);
+    p->total = p->parts + (size_t)w.split * w.parts * 2 * 128 * kDnN * 4;
     return true;
 }
 
@@ -482,7 +473,7 @@ size_t dense_ws_bytes(int64_t tokens, int64_t n, int64_t k)
     return dense_plan(tokens, n, k, &p) ? p.total + 256 : 0;
 }
 
-size_t dense_ws_most() { return up256((size_t)2 * kDnClusters * 16) + (size_t)kDnClusters * 4 * 128 * kDnN * 4; }
+size_t dense_ws_most() { return up256((size_t)kDnClusters * 16) + (size_t)kDnClusters * 2 * 128 * kDnN * 4; }
 
 int dense_product(const char* who, const DenseProduct& q, const DenseOut& out, int* status, void* ws, size_t ws_bytes, cudaStream_t st)
 {
@@ -496,6 +487,7 @@ int dense_product(const char* who, const DenseProduct& q, const DenseOut& out, i
         return BOF4_ERR_WORKSPACE;
     }
     p.work.epoch = tc_next_epoch();
+    p.work.segment = q.use == kDenseLoss || (q.use == kDenseGated && !out.y_bf16) ? 16 : q.use == kDenseStore ? 32 : 64;
     unsigned char* const base = static_cast<unsigned char*>(ws);
     CUtensorMap a_map, b_map;
     int rc;

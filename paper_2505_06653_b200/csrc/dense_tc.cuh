@@ -34,22 +34,16 @@ struct DenseOut {
     float* target_logit;     // [t]
     // add
     const float* factor;     // [t], NULL: y is written, not added to
-    bool first;              // loss: `ref` is a guess
+    bool first;              // loss: no reference yet, the guess is 0
+    bool keep_status;        // *status is set where a wait runs out, and not cleared before
 };
 
 struct DenseWork {
     int tiles_m, tiles_n, per_tile;  // tiles of 256 tokens, of 256 columns of z, k-blocks of 64 of a tile
-    int streamed;                    // the first tiles are dealt in equal parts of their k-blocks, the others a tile at a time
-    int parts;                       // clusters that take a part of the streamed tiles
-    int each, extra;                 // k-blocks of such a part, and the remainder
+    int split, parts;                // the first `split` tiles are cut into so many parts along K, which are the first units of work
+    int segment;                     // k-blocks of an accumulator
     int clusters;
     unsigned long long epoch;
-    __host__ __device__ int start(int i) const { return i * each + (i < extra ? i : extra); }
-    __device__ int owner(int l) const
-    {
-        const uint32_t longer = (uint32_t)extra * (uint32_t)(each + 1);
-        return (uint32_t)l < longer ? (int)((uint32_t)l / (uint32_t)(each + 1)) : extra + (int)(((uint32_t)l - longer) / (uint32_t)each);
-    }
 };
 
 // z[t, o] = sum_k a[t, k] B[o, k], or B[k, o] with n_major.  a: bf16, `lda` elements between tokens; b: bf16, rows without gaps.
@@ -64,7 +58,6 @@ struct DenseProduct {
 };
 size_t dense_ws_bytes(int64_t tokens, int64_t n, int64_t k);  // 0: too large
 size_t dense_ws_most();                                       // of any sizes
-// Sets *status to 1 where a wait ran out, and leaves it otherwise.
 int dense_product(const char* who, const DenseProduct& p, const DenseOut& out, int* status, void* ws, size_t ws_bytes, cudaStream_t st);
 
 }  // namespace bof4

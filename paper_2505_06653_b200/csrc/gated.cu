@@ -12,70 +12,90 @@
 
 namespace bof4 {
 
+// d, gate, up of eight elements -> the two gradients in the places of gate and up; one branch for all of them.
+__device__ __forceinline__ void activate_gradients(const float (&d)[8], float (&g)[8], float (&up)[8], int act)
+{
+    auto all = [&](int which) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float v, slope;
+            activate_both(g[k], which, v, slope);
+            g[k] = d[k] * up[k] * slope, up[k] = d[k] * v;
+        }
+    };
+    switch (act) {
+        case BOF4_ACT_RELU: all(BOF4_ACT_RELU); break;
+        case BOF4_ACT_GELU: all(BOF4_ACT_GELU); break;
+        case BOF4_ACT_GELU_TANH: all(BOF4_ACT_GELU_TANH); break;
+        case BOF4_ACT_SILU: all(BOF4_ACT_SILU); break;
+        default: all(BOF4_ACT_NONE);
+    }
+}
+
 // dz of a gated block, rounded to bf16 for the tensor cores, and the sums of the unrounded dz over a CTA's tokens: as dz_kernel
 // (linear.cu), with two results per element.  Sums are added in a fixed order.
-template <class DT>
-__global__ void __launch_bounds__(256, 2)
+template <class DT, bool SUMS>
+__global__ void __launch_bounds__(256, SUMS ? 2 : DT::code == BOF4_F32 ? 3 : 4)
 gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __restrict__ pre, int64_t ld_pre, int act, int64_t n, int64_t tokens,
                 bool vec, uint16_t* __restrict__ dz, int64_t ld_dz, float* __restrict__ sums, int col_blocks)
 {
     if (!after_previous()) return;
-    __shared__ float s_sum[8][2 * kDzCols + 4];
+    __shared__ float s_sum[SUMS ? 8 : 1][2 * kDzCols + 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t chunk = blockIdx.x / col_blocks, c0 = (int64_t)(blockIdx.x % col_blocks) * kDzCols + lane * 8;
     const int count = (int)(n - c0 < 8 ? n - c0 : 8);
     const bool v8 = vec && count == 8;
     float sum[16] = {};
     if (count > 0) {
-        constexpr int N = kDzTokens / 8;
-        const int64_t t0 = chunk * kDzTokens + warp;
-        Dz8<DT> a[N];
-        Dz8<BF16> b[N], c[N];
+        constexpr int N = 2;  // tokens on their way at a time: more cost warps
+#pragma unroll 1
+        for (int64_t t0 = chunk * kDzTokens + warp; t0 < chunk * kDzTokens + kDzTokens && t0 < tokens; t0 += 8 * N) {
+            Dz8<DT> a[N];
+            Dz8<BF16> b[N], c[N];
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            if (t0 + 8 * u >= tokens) break;
-            a[u].load(dh, (t0 + 8 * u) * ld_dh + c0, count, v8);
-            b[u].load(pre, (t0 + 8 * u) * ld_pre + c0, count, v8);
-            c[u].load(pre, (t0 + 8 * u) * ld_pre + n + c0, count, v8);
-        }
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-            if (t0 + 8 * u >= tokens) break;
-            float d[8], g[8], up[8];
-            a[u].values(d);
-            b[u].values(g);
-            c[u].values(up);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float v, slope;
-                activate_both(g[k], act, v, slope);
-                g[k] = d[k] * up[k] * slope, up[k] = d[k] * v;
-                if (k < count) sum[k] += g[k], sum[8 + k] += up[k];
+            for (int u = 0; u < N; ++u) {
+                if (t0 + 8 * u >= tokens) break;
+                a[u].load(dh, (t0 + 8 * u) * ld_dh + c0, count, v8);
+                b[u].load(pre, (t0 + 8 * u) * ld_pre + c0, count, v8);
+                c[u].load(pre, (t0 + 8 * u) * ld_pre + n + c0, count, v8);
             }
-            if (!dz) continue;
-            uint16_t* const p = dz + (t0 + 8 * u) * ld_dz + c0;
-            if (v8) {
-                *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4], g[5]), bf16_pair(g[6], g[7]));
-                *reinterpret_cast<uint4*>(p + n) = make_uint4(bf16_pair(up[0], up[1]), bf16_pair(up[2], up[3]), bf16_pair(up[4], up[5]), bf16_pair(up[6], up[7]));
-            } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                if (t0 + 8 * u >= tokens) break;
+                float d[8], g[8], up[8];
+                a[u].values(d);
+                b[u].values(g);
+                c[u].values(up);
+                activate_gradients(d, g, up, act);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (k < count) p[k] = bf16_round(g[k]), p[n + k] = bf16_round(up[k]);
+                    if (SUMS && k < count) sum[k] += g[k], sum[8 + k] += up[k];
+                if (!dz) continue;
+                uint16_t* const p = dz + (t0 + 8 * u) * ld_dz + c0;
+                if (v8) {
+                    *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4], g[5]), bf16_pair(g[6], g[7]));
+                    *reinterpret_cast<uint4*>(p + n) = make_uint4(bf16_pair(up[0], up[1]), bf16_pair(up[2], up[3]), bf16_pair(up[4], up[5]), bf16_pair(up[6], up[7]));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < count) p[k] = bf16_round(g[k]), p[n + k] = bf16_round(up[k]);
+                }
             }
         }
     }
-    if (!sums) return;
+    if constexpr (SUMS) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s_sum[warp][lane * 8 + k] = sum[k], s_sum[warp][kDzCols + lane * 8 + k] = sum[8 + k];
-    __syncthreads();
-    const int64_t c = (int64_t)(blockIdx.x % col_blocks) * kDzCols + threadIdx.x;
-    if (c < n) {
+        for (int k = 0; k < 8; ++k) s_sum[warp][lane * 8 + k] = sum[k], s_sum[warp][kDzCols + lane * 8 + k] = sum[8 + k];
+        __syncthreads();
+        const int64_t c = (int64_t)(blockIdx.x % col_blocks) * kDzCols + threadIdx.x;
+        if (c < n) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float s = 0.0f;
+            for (int h = 0; h < 2; ++h) {
+                float s = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) s += s_sum[w][h * kDzCols + threadIdx.x];
-            sums[chunk * 2 * n + h * n + c] = s;
+                for (int w = 0; w < 8; ++w) s += s_sum[w][h * kDzCols + threadIdx.x];
+                sums[chunk * 2 * n + h * n + c] = s;
+            }
         }
     }
 }
@@ -92,10 +112,16 @@ __global__ void __launch_bounds__(256) gated_empty_kernel(const LinearOut out, i
 namespace {
 
 #ifndef BOF4_GATED_DENSE
-#define BOF4_GATED_DENSE 768
+#define BOF4_GATED_DENSE 0
 #endif
-// Tokens from which a matrix is decoded once and multiplied as plain bf16.
-bool gated_dense(int64_t tokens) { return tokens >= BOF4_GATED_DENSE; }
+// Whether a matrix is decoded once and multiplied as plain bf16.  Both forms, us, ffn x columns by tokens: forward 11008 x 4096 by 512 119 against 121, 768 154
+// against 140, 1024 213 against 173, 28672 x 8192 by 768 633 against 692, 1024 834 against 834, 2048 1677 against 1444; backward 11008 x 4096 by 768 161
+// against 181, 1024 205 against 192, and where rows of the decoded matrix are long 28672 x 8192 by 384 508 against 545, 512 608 against 561, 768 991 against 721.
+bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
+{
+    if (BOF4_GATED_DENSE) return tokens >= BOF4_GATED_DENSE;
+    return tokens >= (!backward ? 768 : rows * cols >= (int64_t)1 << 28 ? 448 : 896);
+}
 
 // Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.
 struct GatedPlan {
@@ -107,7 +133,7 @@ struct GatedPlan {
 bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_t capacity, GatedPlan* p)
 {
     const int64_t rows = 2 * ffn;
-    p->dense = gated_dense(tokens);
+    p->dense = gated_dense(rows, cols, tokens, backward);
     p->product = 256;
     if (cols) {
         if (p->dense) p->product = backward ? dense_ws_bytes(tokens, cols, rows) : dense_ws_bytes(tokens, rows, cols);
@@ -218,7 +244,6 @@ extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scal
         return linear_tc(fn, w, false, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
     }
     unsigned char* const base = static_cast<unsigned char*>(d_ws);
-    BOF4_CUDA_TRY(cudaMemsetAsync(d_status, 0, sizeof(int), st));
     if (const int rc = gated_decode(w, base + p.w, st)) return rc;
     const DenseProduct q{d_x, ldx, base + p.w, 0, cols, w.rows, false, kDenseGated};
     DenseOut to{};
@@ -281,7 +306,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
         return BOF4_ERR_WORKSPACE;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!product || p.dense) BOF4_CUDA_TRY(cudaMemsetAsync(d_status, 0, sizeof(int), st));  // (the other product's kernel writes it)
+    if (!product) BOF4_CUDA_TRY(cudaMemsetAsync(d_status, 0, sizeof(int), st));  // (the product's kernel writes it)
     if (nothing) {  // sums over nothing
         if (d_dx && cols && n_tokens)
             BOF4_CUDA_TRY(cudaMemset2DAsync(d_dx, (size_t)(n_tokens > 1 ? ld_dx : cols) * 2, 0, (size_t)cols * 2, (size_t)n_tokens, st));
@@ -294,7 +319,9 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     uint16_t* const dz = reinterpret_cast<uint16_t*>(base + p.dz);
     float* const sums = p.chunks > 1 ? reinterpret_cast<float*>(base + p.sums) : d_dbias;
     const bool vec = aligned16(d_dh) && ld_dh % 8 == 0 && aligned16(d_pre) && ld_pre % 8 == 0 && ffn % 8 == 0;
-    launch_after(dh_dtype == BOF4_F32 ? gated_dz_kernel<F32> : gated_dz_kernel<BF16>, (int)(p.chunks * col_blocks), 256, 0, st, d_dh, ld_dh,
+    auto* const kern = dh_dtype == BOF4_F32 ? (d_dbias ? gated_dz_kernel<F32, true> : gated_dz_kernel<F32, false>)
+                                            : (d_dbias ? gated_dz_kernel<BF16, true> : gated_dz_kernel<BF16, false>);
+    launch_after(kern, (int)(p.chunks * col_blocks), 256, 0, st, d_dh, ld_dh,
                  static_cast<const uint16_t*>(d_pre), ld_pre, activation, ffn, n_tokens, vec, product ? dz : nullptr, p.ld, d_dbias ? sums : nullptr, col_blocks);
     if (d_dbias && p.chunks > 1) linear_dbias(sums, 2 * ffn, p.chunks, d_dbias, st);
     BOF4_CUDA_TRY(cudaGetLastError());

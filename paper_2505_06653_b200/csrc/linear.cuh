@@ -191,6 +191,7 @@ struct LinearOut {
     bool bias_bf16, y_bf16;
     // rows of y, residual and pre begin at addresses that hold pairs of bf16 values / 16 bytes of their type
     bool pairs, wide;
+    const float* scale;  // backward: what the sums of a token are multiplied by, or NULL
     bool gated;
     bool keep_status;  // *status is set where a wait runs out, and not cleared before
     void set_alignment()

@@ -129,11 +129,16 @@ __device__ __forceinline__ void lt_sums(uint32_t src, int accs, float (&z)[16])
 
 // Sixteen tokens (the first `count` of them) of a finished accumulator: row o of the output in each lane.  Of bf16 values, the
 // lanes of a pair exchange one for every two tokens, so that each stores two rows of a token; their residual is read the same way.
+template <bool SCALED>
 __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t o, bool live, int lane)
 {
     float z[16];
     __syncwarp();
     lt_sums(src, accs, z);
+    if (SCALED && out.scale) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) z[k] *= k < count ? __ldg(out.scale + t0 + k) : 0.0f;
+    }
     const bool odd = lane & 1, both = (o | 1) < out.n, one = (o & ~(int64_t)1) < out.n;  // the pair's two rows exist, its first
     const bool paired = out.y_bf16 && out.pairs && count >= 16;
     float r[16];
@@ -523,7 +528,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 const float b = live ? out.bias_at(GATED ? (o & 1) * out.n + (o >> 1) : o) : 0.0f;
                 if (GATED)
                     for (int q = 0; q < count; q += 16) lt_result_pair(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o >> 1, live, lane);
-                else for (int q = 0; q < count; q += 16) lt_result(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
+                else for (int q = 0; q < count; q += 16) lt_result<BWD>(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -597,6 +602,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             for (int u = 0; u < B; ++u) {
                 const int e = e0 + u * kLtThreads;
                 const int64_t o = o0 + (e & 31) * 4;
+                if (BWD && out.scale && e < count * (kLtM / 4)) {
+                    const float f = __ldg(out.scale + token0 + (e >> 5));
+                    sum[u].x *= f, sum[u].y *= f, sum[u].z *= f, sum[u].w *= f;
+                }
                 if (e < count * (kLtM / 4) && o < out.n) four[u].store(out, sum[u], token0 + (e >> 5), o);
             }
         }

@@ -27,7 +27,9 @@ def bof4():
 # part of a line; several slices of columns for few tokens
 SHAPES = [(1, 32, 64, 64), (1, 5, 32, 32), (2, 65, 256, 64), (5, 200, 4096, 128), (8, 96, 1024, 1024), (9, 7, 512, 64), (16, 130, 10240, 64), (17, 129, 320, 64),
           (33, 64, 4096, 4096), (64, 1000, 512, 64), (130, 100, 4032, 32), (256, 333, 1536, 64), (300, 1025, 512, 256), (767, 192, 96, 32), (768, 127, 64, 64),
-          (1000, 200, 4128, 32), (1300, 1111, 2080, 32), (2049, 64, 512, 64), (769, 4736, 256, 64)]
+          (1000, 200, 4128, 32), (1300, 1111, 2080, 32), (2049, 64, 512, 64), (769, 4736, 256, 64),
+          # tiles of the form for many tokens that are cut along K: into three, two goes of all clusters (forward; backward)
+          (1000, 1500, 4096, 64), (1000, 2100, 2944, 64)]
 
 
 @pytest.mark.parametrize("tokens,ffn,cols,block", SHAPES)
