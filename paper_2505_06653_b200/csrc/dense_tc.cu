@@ -171,7 +171,7 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCol
                 dn_store8(p, g, left - 8 * c, out.wide);
                 dn_store8(p + out.n, u, left - 8 * c, out.wide);
             }
-            activate_all(g, out.act);
+            activate_gate(g, out.act);
 #pragma unroll
             for (int k = 0; k < 8; ++k) g[k] *= u[k];
             const int64_t at = t * out.ldy + f0 + 8 * c;

@@ -37,7 +37,7 @@ __device__ __forceinline__ void activate_gradients(const float (&d)[8], float (&
 template <class DT, bool SUMS>
 __global__ void __launch_bounds__(256, SUMS ? 2 : DT::code == BOF4_F32 ? 3 : 4)
 gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __restrict__ pre, int64_t ld_pre, int act, int64_t n, int64_t tokens,
-                bool vec, uint16_t* __restrict__ dz, int64_t ld_dz, float* __restrict__ sums, int col_blocks)
+                bool vec, uint16_t* __restrict__ dz, int64_t ld_dz, float* __restrict__ sums, int col_blocks, int per)
 {
     if (!after_previous()) return;
     __shared__ float s_sum[SUMS ? 8 : 1][2 * kDzCols + 4];
@@ -49,19 +49,19 @@ gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __re
     if (count > 0) {
         constexpr int N = 2;  // tokens on their way at a time: more cost warps
 #pragma unroll 1
-        for (int64_t t0 = chunk * kDzTokens + warp; t0 < chunk * kDzTokens + kDzTokens && t0 < tokens; t0 += 8 * N) {
+        for (int64_t t0 = chunk * per + warp; t0 < chunk * per + per && t0 < tokens; t0 += 8 * N) {
             Dz8<DT> a[N];
             Dz8<BF16> b[N], c[N];
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                if (t0 + 8 * u >= tokens) break;
+                if (t0 + 8 * u >= tokens || t0 + 8 * u >= chunk * per + per) break;
                 a[u].load(dh, (t0 + 8 * u) * ld_dh + c0, count, v8);
                 b[u].load(pre, (t0 + 8 * u) * ld_pre + c0, count, v8);
                 c[u].load(pre, (t0 + 8 * u) * ld_pre + n + c0, count, v8);
             }
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                if (t0 + 8 * u >= tokens) break;
+                if (t0 + 8 * u >= tokens || t0 + 8 * u >= chunk * per + per) break;
                 float d[8], g[8], up[8];
                 a[u].values(d);
                 b[u].values(g);
@@ -126,6 +126,7 @@ bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
 // Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.
 struct GatedPlan {
     bool dense;
+    int per;  // tokens of a CTA that forms dz: fewer where there would be less than four CTAs an SM (131 tokens of 11008: 15 us with 32)
     int64_t chunks, ld;
     size_t product, w, dz, sums, total;
 };
@@ -141,7 +142,10 @@ bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_
         else p->product = linear_tc_ws_bytes(rows, cols, tokens, backward, capacity);
         if (!p->product) return false;
     }
-    p->chunks = (tokens + kDzTokens - 1) / kDzTokens;
+    const int64_t blocks = (ffn + kDzCols - 1) / kDzCols;
+    p->per = kDzTokens;
+    while (p->per > 8 && (tokens + p->per - 1) / p->per * blocks < 4 * kSMs) p->per /= 2;
+    p->chunks = (tokens + p->per - 1) / p->per;
     p->ld = (rows + 7) & ~(int64_t)7;
     p->w = up256(p->product);
     p->dz = p->w + (p->dense ? up256((size_t)rows * cols * 2) : 0);
@@ -322,7 +326,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     auto* const kern = dh_dtype == BOF4_F32 ? (d_dbias ? gated_dz_kernel<F32, true> : gated_dz_kernel<F32, false>)
                                             : (d_dbias ? gated_dz_kernel<BF16, true> : gated_dz_kernel<BF16, false>);
     launch_after(kern, (int)(p.chunks * col_blocks), 256, 0, st, d_dh, ld_dh,
-                 static_cast<const uint16_t*>(d_pre), ld_pre, activation, ffn, n_tokens, vec, product ? dz : nullptr, p.ld, d_dbias ? sums : nullptr, col_blocks);
+                 static_cast<const uint16_t*>(d_pre), ld_pre, activation, ffn, n_tokens, vec, product ? dz : nullptr, p.ld, d_dbias ? sums : nullptr, col_blocks, p.per);
     if (d_dbias && p.chunks > 1) linear_dbias(sums, 2 * ffn, p.chunks, d_dbias, st);
     BOF4_CUDA_TRY(cudaGetLastError());
     if (!product) return BOF4_OK;

@@ -202,32 +202,35 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, in
     }
 }
 
-// The same of a gated tile: lane pairs have column f of the gate and of the up rows; the even lane takes the even tokens.
+// N tokens of a gated tile: lane pairs have column f of the gate and of the up rows; the even lane takes the even tokens.
+template <int N>
 __device__ __forceinline__ void lt_result_pair(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t f, bool live, int lane)
 {
-    float z[16];
+    float z[N];
     __syncwarp();
-    lt_sums(src, accs, z);
+#pragma unroll
+    for (int q = 0; q < N; q += 16) lt_sums(src + (uint32_t)q, accs, *reinterpret_cast<float(*)[16]>(z + q));
     const bool odd = lane & 1;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) z[k] += b;
+    for (int k = 0; k < N; ++k) z[k] += b;
     if (out.pre && live) {
         uint16_t* const p = out.pre + t0 * out.ld_pre + (odd ? out.n : 0) + f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
+        for (int k = 0; k < N; ++k)
             if (k < count) p[k * out.ld_pre] = bf16_round(z[k]);
     }
-    float g[8], u[8];
+    float g[N / 2], u[N / 2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < N / 2; ++k) {
         const float other = __shfl_xor_sync(kFull, odd ? z[2 * k] : z[2 * k + 1], 1);
         g[k] = odd ? other : z[2 * k], u[k] = odd ? z[2 * k + 1] : other;
     }
-    activate_all(g, out.act);
+    activate_gate(g, out.act);
+    if (!live) return;
     const int64_t at = (t0 + odd) * out.ldy + f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (!live || 2 * k + odd >= count) continue;
+    for (int k = 0; k < N / 2; ++k) {
+        if (2 * k + odd >= count) continue;
         const float v = g[k] * u[k];
         if (out.y_bf16) static_cast<uint16_t*>(out.y)[at + 2 * k * out.ldy] = bf16_round(v);
         else static_cast<float*>(out.y)[at + 2 * k * out.ldy] = v;
@@ -526,9 +529,11 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 }
             } else {
                 const float b = live ? out.bias_at(GATED ? (o & 1) * out.n + (o >> 1) : o) : 0.0f;
-                if (GATED)
-                    for (int q = 0; q < count; q += 16) lt_result_pair(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o >> 1, live, lane);
-                else for (int q = 0; q < count; q += 16) lt_result<BWD>(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
+                if (GATED) {
+                    int q = 0;
+                    for (; q + 16 < count; q += 32) lt_result_pair<32>(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o >> 1, live, lane);
+                    if (q < count) lt_result_pair<16>(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o >> 1, live, lane);
+                } else for (int q = 0; q < count; q += 16) lt_result<BWD>(out, src + (uint32_t)q, accs, b, token0 + q, count - q, o, live, lane);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -585,10 +590,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
 #pragma unroll
                 for (int u = 0; u < B; ++u) {
                     const int e = e0 + u * kLtThreads;
-                    const int64_t f = (o0 >> 1) + (e & 31) * 2;
-                    if (e >= count * (kLtM / 4)) continue;
-                    if (f < out.n) out.store_pair(sum[u].x, sum[u].y, token0 + (e >> 5), f);
-                    if (f + 1 < out.n) out.store_pair(sum[u].z, sum[u].w, token0 + (e >> 5), f + 1);
+                    if (e < count * (kLtM / 4)) out.store_pairs(sum[u], token0 + (e >> 5), (o0 >> 1) + (e & 31) * 2);
                 }
                 continue;
             }
