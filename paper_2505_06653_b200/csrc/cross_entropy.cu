@@ -159,8 +159,9 @@ loss_gradient_kernel(const float* __restrict__ logits, int64_t ld, int64_t n, in
         scale[t] = counted ? (dloss ? dloss[t] : 1.0f) * c.rest : 0.0f;
     }
     if (c0 >= n) return;
+    const float unit = 1.0f / s.y;  // p_v / (1 - p_y) = exp(z_v - r) / S
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = !counted || c.rest == 0.0f ? 0.0f : target == c0 + k ? -1.0f : __fdividef(c.scale, c.rest) * __expf(v[k] - s.x);
+    for (int k = 0; k < 8; ++k) v[k] = !counted || s.y == 0.0f ? 0.0f : target == c0 + k ? -1.0f : unit * __expf(v[k] - s.x);
     // (rows are padded to eight)
     *reinterpret_cast<uint4*>(dz + t * ld + c0) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
@@ -352,7 +353,7 @@ bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t ca
     };
     const size_t t = (size_t)tokens;
     if (!p->dense) {
-        p->forward = linear_few_applies(rows, cols, tokens, capacity > 0) ? linear_few_ws_bytes(rows, cols, tokens, capacity)
+        p->forward = few_pays(rows, cols, tokens, capacity > 0) ? linear_few_ws_bytes(rows, cols, tokens, capacity)
                                                                           : linear_tc_ws_bytes(rows, cols, tokens, false, capacity);
         p->backward = grad ? linear_tc_ws_bytes(rows, cols, tokens, true, capacity) : 0;
         if (!p->forward || (grad && !p->backward)) return false;
@@ -462,7 +463,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         out.n = rows;
         out.tokens = n_tokens;
         out.set_alignment();
-        if (linear_few_applies(rows, cols, n_tokens, w.capacity > 0)) rc = linear_few(fn, w, d_x, ldx, out, d_status, base, p.forward, st);
+        if (few_pays(rows, cols, n_tokens, w.capacity > 0)) rc = linear_few(fn, w, d_x, ldx, out, d_status, base, p.forward, st);
         else rc = linear_tc(fn, w, false, d_x, ldx, out, d_status, base, p.forward, st);
         if (rc) return rc;
         float* const scale = floats(p.scale);

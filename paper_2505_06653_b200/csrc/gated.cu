@@ -138,7 +138,7 @@ bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_
     p->product = 256;
     if (cols) {
         if (p->dense) p->product = backward ? dense_ws_bytes(tokens, cols, rows) : dense_ws_bytes(tokens, rows, cols);
-        else if (!backward && linear_few_applies(rows, cols, tokens, capacity > 0)) p->product = linear_few_ws_bytes(rows, cols, tokens, capacity);
+        else if (!backward && few_pays(rows, cols, tokens, capacity > 0)) p->product = linear_few_ws_bytes(rows, cols, tokens, capacity);
         else p->product = linear_tc_ws_bytes(rows, cols, tokens, backward, capacity);
         if (!p->product) return false;
     }
@@ -244,7 +244,7 @@ extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scal
     w.codes = d_codes;
     w.levels = d_codebook;
     if (!p.dense) {
-        if (linear_few_applies(w.rows, cols, n_tokens, w.capacity > 0)) return linear_few(fn, w, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
+        if (few_pays(w.rows, cols, n_tokens, w.capacity > 0)) return linear_few(fn, w, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
         return linear_tc(fn, w, false, d_x, ldx, out, d_status, d_ws, ws_bytes, st);
     }
     unsigned char* const base = static_cast<unsigned char*>(d_ws);

@@ -81,7 +81,8 @@ def targets_of(tokens, rows, seed, ignored=0.2):
 # tokens on both sides of 6, 8, 16, 64, 128, 256 and of the form for many tokens; vocabularies of one row, one chunk, one piece and a little more, tiles cut along K
 SHAPES = [(1, 1, 32, 32), (1, 1000, 64, 64), (2, 2049, 256, 64), (7, 333, 4096, 128), (13, 5000, 1024, 1024), (17, 127, 320, 64), (40, 2048, 64, 32), (130, 16385, 96, 32),
           (300, 700, 512, 256), (511, 999, 64, 64), (512, 1000, 96, 32), (513, 16385, 128, 64), (700, 1, 64, 64), (1000, 300, 2080, 32), (1537, 33000, 64, 64),
-          (600, 63, 256, 64), (2049, 1025, 512, 64), (1000, 3000, 4096, 64)]
+          (600, 63, 256, 64), (2049, 1025, 512, 64), (1000, 3000, 4096, 64),
+          (14, 16400, 4096, 64)]
 
 
 @pytest.mark.parametrize("tokens,rows,cols,block", SHAPES)
@@ -294,3 +295,49 @@ def test_refusals(bof4):
                dict(workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(bof4.Bof4Error):
             bof4.bof4_cross_entropy(**{**good, **kw})
+
+
+@pytest.mark.parametrize("tokens", [3, 40, 500])
+def test_offsets_beyond_32_bits(bof4, tokens):
+    """More than 2^32 weights.  x has a few values that are not zero, so that the reference needs a few columns for the logits; dx is compared in some."""
+    rows, cols, block = 135000, 32768, 1024
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    lv = ((torch.arange(16) - 7.5) / 8).tolist()
+    codes = torch.randint(0, 256, (rows * cols // 2,), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(0, 3, (rows * cols // block,), generator=g, device="cuda").bfloat16() - 1
+    level = torch.tensor(lv, device="cuda", dtype=torch.float64)
+
+    def part(columns):
+        byte = codes.view(rows, cols // 2)[:, columns // 2]
+        return level[torch.where(columns % 2 == 0, byte >> 4, byte & 15).long()] * scales.view(rows, cols // block)[:, columns // block].double()
+
+    columns = torch.tensor([0, 1, 777, 16385, 32767], device="cuda")
+    x = torch.zeros(tokens, cols, dtype=torch.bfloat16, device="cuda")
+    x[:, columns] = torch.randint(-2, 3, (tokens, 5), generator=g, device="cuda").bfloat16()
+    targets = targets_of(tokens, rows, 3, 0.1)
+    targets[0] = rows - 3
+    some = torch.cat((columns, torch.arange(9000, 9100, device="cuda"), torch.arange(32700, 32767, device="cuda")))
+    w = part(some)
+    small = torch.zeros(tokens, len(some), device="cuda")
+    small[:, :5] = x[:, columns].float()
+    loss, lse, dx, mag, most = plain(small, w, targets, torch.ones(tokens, device="cuda"))
+    got = bof4.bof4_cross_entropy(codes, scales, rows, cols, block, lv, x, targets, want_dx=True)
+    assert int(got[3].item()) == 0
+    assert bool(((got[0].double() - loss).abs() <= most).all()) and bool(((got[1].double() - lse).abs() <= TOL * (1 + lse.abs())).all())
+    assert bool(((got[2][:, some].double() - dx).abs() <= mag * (2.0 ** -8 + 2.0 ** -13) + 2.0 ** -8 * dx.abs()).all())
+
+
+def test_many_tokens(bof4):
+    """More than 2^31 exponentials in a piece; three blocks of tokens are compared."""
+    tokens, rows, cols, block = 70000, 33000, 32, 32
+    case = integer_case(rows, cols, block, 8)
+    g = torch.Generator().manual_seed(1)
+    x, targets = ints(g, tokens, cols), targets_of(tokens, rows, 6)
+    got = bof4.bof4_cross_entropy(case[1], case[2], rows, cols, block, case[0], x, targets, want_dx=True)
+    w = decode(case[1], case[2], block, case[0], rows, cols)
+    assert int(got[3].item()) == 0
+    for at in (0, 40000, 69000):
+        t = slice(at, at + 1000)
+        loss, lse, dx, mag, most = plain(x[t], w, targets[t], torch.ones(1000, device="cuda"))
+        assert bool(((got[0][t].double() - loss).abs() <= most).all()) and bool(((got[1][t].double() - lse).abs() <= TOL * (1 + lse.abs())).all())
+        assert bool(((got[2][t].double() - dx).abs() <= mag * (2.0 ** -8 + 2.0 ** -13) + 2.0 ** -8 * dx.abs()).all())

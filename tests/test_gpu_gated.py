@@ -29,7 +29,9 @@ SHAPES = [(1, 32, 64, 64), (1, 5, 32, 32), (2, 65, 256, 64), (5, 200, 4096, 128)
           (33, 64, 4096, 4096), (64, 1000, 512, 64), (130, 100, 4032, 32), (256, 333, 1536, 64), (300, 1025, 512, 256), (767, 192, 96, 32), (768, 127, 64, 64),
           (1000, 200, 4128, 32), (1300, 1111, 2080, 32), (2049, 64, 512, 64), (769, 4736, 256, 64),
           # tiles of the form for many tokens that are cut along K: into three, two goes of all clusters (forward; backward)
-          (1000, 1500, 4096, 64), (1000, 2100, 2944, 64)]
+          (1000, 1500, 4096, 64), (1000, 2100, 2944, 64),
+          # a large matrix by more than twelve tokens
+          (14, 8200, 4096, 64)]
 
 
 @pytest.mark.parametrize("tokens,ffn,cols,block", SHAPES)
@@ -282,3 +284,37 @@ def test_refusals(bof4):
         bof4.bof4_gated_backward(**{**good, "pre": torch.zeros(4, 128, device="cuda")})
     with pytest.raises(bof4.Bof4Error):
         bof4.bof4_gated_backward(**{**good, "activation": -1})
+
+
+@pytest.mark.parametrize("tokens", [3, 40, 800])
+def test_offsets_beyond_32_bits(bof4, tokens):
+    """More than 2^32 weights: codes, constants, the decoded matrix and z.  x and dh have a few values that are not zero, so that the reference needs a few columns
+    and rows of the matrix only."""
+    ffn, cols, block = 68000, 32768, 1024
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    lv = ((torch.arange(16) - 7.5) / 8).tolist()
+    codes = torch.randint(0, 256, (ffn * cols,), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(0, 3, (2 * ffn * cols // block,), generator=g, device="cuda").bfloat16() - 1
+    level = torch.tensor(lv, device="cuda", dtype=torch.float64)
+
+    def part(rows, columns):
+        byte = codes.view(2 * ffn, cols // 2)[rows][:, columns // 2]
+        code = torch.where(columns % 2 == 0, byte >> 4, byte & 15)
+        return level[code.long()] * scales.view(2 * ffn, cols // block)[rows][:, columns // block].double()
+
+    columns = torch.tensor([0, 1, 777, 16385, 32767], device="cuda")
+    x = torch.zeros(tokens, cols, dtype=torch.bfloat16, device="cuda")
+    x[:, columns] = torch.randint(-2, 3, (tokens, 5), generator=g, device="cuda").bfloat16()
+    z = x[:, columns].double() @ part(torch.arange(2 * ffn, device="cuda"), columns).T
+    pre = torch.empty(tokens, 2 * ffn, dtype=torch.bfloat16, device="cuda")
+    h, status = bof4.bof4_gated(codes, scales, ffn, cols, block, lv, x, activation=bof4.ACT_NONE, out_dtype=bof4.F32, pre=pre)
+    assert int(status.item()) == 0 and torch.equal(h, (z[:, :ffn] * z[:, ffn:]).float()) and torch.equal(pre, z.bfloat16())
+    del h, z, pre
+    rows = torch.tensor([0, 5, 33333, 67999], device="cuda")
+    dh, pre = torch.zeros(tokens, ffn, device="cuda"), torch.zeros(tokens, 2 * ffn, dtype=torch.bfloat16, device="cuda")
+    dh[:, rows] = torch.randint(-2, 3, (tokens, 4), generator=g, device="cuda").float()
+    both = torch.cat((rows, rows + ffn))
+    pre[:, both] = torch.randint(-2, 3, (tokens, 8), generator=g, device="cuda").bfloat16()
+    dz = dh[:, rows].double().repeat(1, 2) * pre[:, both].double().roll(4, 1)
+    dx, _, status = bof4.bof4_gated_backward(codes, scales, ffn, cols, block, lv, dh, pre, activation=bof4.ACT_NONE)
+    assert int(status.item()) == 0 and torch.equal(dx, (dz @ part(both, torch.arange(cols, device="cuda"))).bfloat16())
