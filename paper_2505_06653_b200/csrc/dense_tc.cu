@@ -113,36 +113,81 @@ __device__ __forceinline__ void dn_place(const DenseWork& w, int tile, int& m, i
     m = g * kDnGroup + in - n * width;
 }
 
-__device__ __forceinline__ uint4 dn_pack8(const float* v)
+// A lane's results lie in its token's row, 32 bytes of it at a time where they can: whole sectors, half of the instructions.
+__device__ __forceinline__ void dn_put32(void* p, const uint32_t (&v)[8])
 {
-    return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+                 "r"(v[7])
+                 : "memory");
 }
-// Eight neighbouring bf16 values, `count` of them in the row.
-__device__ __forceinline__ void dn_store8(uint16_t* p, const float* v, int count, bool wide)
+__device__ __forceinline__ void dn_get32(const void* p, uint32_t (&v)[8])
 {
-    if (wide && count >= 8) {
-        *reinterpret_cast<uint4*>(p) = dn_pack8(v);
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(p)
+                 : "memory");
+}
+// Sixteen neighbouring values, `count` of them in the row.
+__device__ __forceinline__ void dn_store16(uint16_t* p, const float* v, int count, int align)
+{
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
+    if (align >= 32 && count >= 16) {
+        dn_put32(p, w);
+    } else if (align >= 16 && count >= 8) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (count >= 16) {
+            *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+#pragma unroll
+            for (int k = 8; k < 16; ++k)
+                if (k < count) p[k] = bf16_round(v[k]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < 16; ++k)
             if (k < count) p[k] = bf16_round(v[k]);
     }
 }
-__device__ __forceinline__ void dn_store8(float* p, const float* v, int count, bool wide)
+__device__ __forceinline__ void dn_store16(float* p, const float* v, int count, int align)
 {
-    if (wide && count >= 8) {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < count) p[k] = v[k];
+    for (int h = 0; h < 16; h += 8) {
+        if (align >= 32 && count >= h + 8) {
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[h + k]);
+            dn_put32(p + h, w);
+        } else {
+#pragma unroll
+            for (int k = h; k < h + 8; ++k)
+                if (k < count) p[k] = v[k];
+        }
     }
+}
+
+// What is known of a token before its sums are.
+struct DenseToken {
+    int64_t target;
+    float ref;  // add: the factor
+};
+template <int USE>
+__device__ __forceinline__ DenseToken dn_token(const DenseOut& out, int64_t t)
+{
+    DenseToken k{-1, 0.0f};
+    if (t >= out.tokens) return k;
+    if (USE == kDenseLoss) {
+        k.target = __ldg(out.targets + t);
+        if (!out.first) k.ref = __ldg(out.ref + t);
+    }
+    if (USE == kDenseAdd && out.factor) k.ref = __ldg(out.factor + t);
+    return k;
 }
 
 // A token's sums of columns o0 ... o0 + 63 of z (gated: gate and up in turn, of columns o0 / 2 ... of y).
 template <int USE>
-__device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCols], int64_t t, int64_t o0)
+__device__ __forceinline__ void dn_finish(const DenseOut& out, const DenseToken& token, float (&z)[kDnCols], int64_t t, int64_t o0)
 {
     if (t >= out.tokens) return;
     if (USE == kDenseGated) {
@@ -161,22 +206,22 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCol
             }
         }
 #pragma unroll
-        for (int c = 0; c < kDnCols / 16; ++c) {
-            if (8 * c >= left) break;
-            float g[8], u[8];
+        for (int c = 0; c < kDnCols / 32; ++c) {
+            if (16 * c >= left) break;
+            float g[16], u[16];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) g[k] = z[16 * c + 2 * k], u[k] = z[16 * c + 2 * k + 1];
+            for (int k = 0; k < 16; ++k) g[k] = z[32 * c + 2 * k], u[k] = z[32 * c + 2 * k + 1];
             if (out.pre) {
-                uint16_t* const p = out.pre + t * out.ld_pre + f0 + 8 * c;
-                dn_store8(p, g, left - 8 * c, out.wide);
-                dn_store8(p + out.n, u, left - 8 * c, out.wide);
+                uint16_t* const p = out.pre + t * out.ld_pre + f0 + 16 * c;
+                dn_store16(p, g, left - 16 * c, out.align);
+                dn_store16(p + out.n, u, left - 16 * c, out.align);
             }
             activate_gate(g, out.act);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) g[k] *= u[k];
-            const int64_t at = t * out.ldy + f0 + 8 * c;
-            if (out.y_bf16) dn_store8(static_cast<uint16_t*>(out.y) + at, g, left - 8 * c, out.wide);
-            else dn_store8(static_cast<float*>(out.y) + at, g, left - 8 * c, out.wide);
+            for (int k = 0; k < 16; ++k) g[k] *= u[k];
+            const int64_t at = t * out.ldy + f0 + 16 * c;
+            if (out.y_bf16) dn_store16(static_cast<uint16_t*>(out.y) + at, g, left - 16 * c, out.align);
+            else dn_store16(static_cast<float*>(out.y) + at, g, left - 16 * c, out.align);
         }
         return;
     }
@@ -185,33 +230,30 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCol
     if (USE == kDenseStore) {
         uint16_t* const p = static_cast<uint16_t*>(out.y) + t * out.ldy + o0;
 #pragma unroll
-        for (int c = 0; c < kDnCols / 8; ++c) dn_store8(p + 8 * c, z + 8 * c, left - 8 * c, out.wide);
+        for (int c = 0; c < kDnCols / 16; ++c)
+            if (16 * c < left) dn_store16(p + 16 * c, z + 16 * c, left - 16 * c, out.align);
     }
-    if (USE == kDenseAdd) {  // (rows of y are padded to eight and aligned)
+    if (USE == kDenseAdd) {  // (rows of y hold multiples of 32 values)
         float* const p = static_cast<float*>(out.y) + t * out.ldy + o0;
-        if (out.factor) {
-            const float f = __ldg(out.factor + t);
 #pragma unroll
-            for (int c = 0; c < kDnCols / 16; ++c) {
-                float4 v[4];
+        for (int c = 0; c < kDnCols / 8; ++c) {
+            if (8 * c >= left) break;
+            uint32_t v[8];
+            if (out.factor) {
+                dn_get32(p + 8 * c, v);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = 16 * c + 4 * k < left ? *reinterpret_cast<const float4*>(p + 16 * c + 4 * k) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float* const s = z + 16 * c + 4 * k;
-                    s[0] = fmaf(v[k].x, f, s[0]), s[1] = fmaf(v[k].y, f, s[1]), s[2] = fmaf(v[k].z, f, s[2]), s[3] = fmaf(v[k].w, f, s[3]);
-                }
+                for (int k = 0; k < 8; ++k) z[8 * c + k] = fmaf(__uint_as_float(v[k]), token.ref, z[8 * c + k]);
             }
-        }
 #pragma unroll
-        for (int c = 0; c < kDnCols / 4; ++c)
-            if (4 * c < left) *reinterpret_cast<float4*>(p + 4 * c) = make_float4(z[4 * c], z[4 * c + 1], z[4 * c + 2], z[4 * c + 3]);
+            for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(z[8 * c + k]);
+            dn_put32(p + 8 * c, v);
+        }
     }
     if (USE == kDenseLoss) {
         // Exponentials against the token's reference, or this part's own maximum where it lies far above (or, where the reference is only a
         // guess, far below): any reference within a factor e^24 leaves sums and products far inside the range of fp32 and bf16.
         // The target's logit is kept, and has no part in the sums.
-        const int64_t target = out.targets[t] - out.first_row - o0;
+        const int64_t target = token.target - out.first_row - o0;
         const bool inside = target >= 0 && target < left;
         const int at = inside ? (int)target : -1;
         float top = -INFINITY, own = 0.0f;
@@ -222,22 +264,23 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, float (&z)[kDnCol
             top = fmaxf(top, z[k]);
         }
         if (inside) out.target_logit[t] = own;
-        float ref = out.first ? 0.0f : out.ref[t];
+        float ref = token.ref;
         if (top > ref + 24.0f || (out.first && top < ref - 24.0f && top > -INFINITY)) ref = top;
         if (ref == -INFINITY) ref = 0.0f;  // nothing but infinitely unlikely rows so far
         float sum = 0.0f;
         uint16_t* const p = static_cast<uint16_t*>(out.y) + t * out.ldy + o0;
 #pragma unroll
-        for (int c = 0; c < kDnCols / 8; ++c) {
+        for (int c = 0; c < kDnCols / 16; ++c) {
             float s = 0.0f;
+            uint32_t e[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                float& v = z[8 * c + k];
-                v = __expf(v - ref);
-                s += v;
+                const float a = __expf(z[16 * c + 2 * k] - ref), b = __expf(z[16 * c + 2 * k + 1] - ref);
+                s += a, s += b;
+                e[k] = bf16_pair(a, b);
             }
             sum += s;
-            if (out.y && 8 * c < left) *reinterpret_cast<uint4*>(p + 8 * c) = dn_pack8(z + 8 * c);  // (rows are padded to eight)
+            if (out.y && 16 * c < left) dn_put32(p + 16 * c, e);  // (rows are padded to 256)
         }
         out.stats[(o0 / kDnCols) * out.tokens + t] = make_float2(ref, sum);
     }
@@ -357,6 +400,10 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         int seg = 0;
         bool ok = true;
         while (ok && walk.step(work)) {
+            int m, n;
+            dn_place(work, walk.tile, m, n);
+            const int64_t t = (int64_t)m * kDnM + rank * 128 + row, o0 = (int64_t)n * kDnN + part * kDnCols;
+            const DenseToken token = dn_token<USE>(out, t);
             float z[kDnCols];
 #pragma unroll
             for (int i = 0; i < kDnCols; ++i) z[i] = 0.0f;
@@ -378,12 +425,9 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                 if (lane == 0)
                     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(dn_first_sm(smem_u32(&s_acc_empty[buf]))) : "memory");
             }
-            int m, n;
-            dn_place(work, walk.tile, m, n);
-            const int64_t t = (int64_t)m * kDnM + rank * 128 + row, o0 = (int64_t)n * kDnN + part * kDnCols;
             if (!(ok = all16(ok))) break;
             if (walk.k0 == 0 && walk.k1 == work.per_tile) {
-                dn_finish<USE>(out, z, t, o0);
+                dn_finish<USE>(out, token, z, t, o0);
                 continue;
             }
             // a part of a tile
@@ -409,7 +453,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 #pragma unroll
                 for (int k = 0; k < kDnCols; ++k) z[k] += __ldcg(p + k * 128);
             }
-            dn_finish<USE>(out, z, t, o0);
+            dn_finish<USE>(out, token, z, t, o0);
         }
         if (!ok && lane == 0) s_fail = 1;
     }

@@ -19,7 +19,13 @@ struct DenseOut {
     void* y;
     int64_t ldy, n, tokens;  // n: columns of z (gated: of y)
     bool y_bf16;
-    bool wide;               // rows of y, pre begin at multiples of 16 bytes
+    int align;               // bytes that rows of y (and both halves of those of pre) begin at multiples of: 32, 16 or less
+    template <class... L>
+    void set_align(uintptr_t addresses, L... elements)  // of y and pre, combined by or; strides and lengths in elements of 2 bytes or more
+    {
+        const uintptr_t all = addresses | (2 * (uintptr_t)(0 | ... | elements));
+        align = all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : 1;
+    }
     // gated
     const void* bias;        // [2 n] or NULL
     bool bias_bf16;
