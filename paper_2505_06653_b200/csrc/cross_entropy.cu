@@ -327,12 +327,10 @@ __global__ void __launch_bounds__(256) loss_dx_kernel(const LossFinal f)
 
 namespace {
 
-#ifndef BOF4_LOSS_DENSE
-#define BOF4_LOSS_DENSE 385
-#endif
-// Tokens from which the vocabulary is taken in pieces.  Both forms with the gradient, us: 32000 x 4096 by 256 tokens 207 against 258, 384 313 against 325, 512
-// 372 against 335, 1024 753 against 572; 128256 x 4096 by 384 1373 against 1317; without it 194 against 195 for 384, 239 against 184 for 512.
-bool loss_dense(int64_t tokens) { return tokens >= BOF4_LOSS_DENSE; }
+// Whether the vocabulary is taken in pieces.  Both forms, us, decoding as it multiplies against this: with the gradient 16000 x 4096 by 256 125 against 123, 32000 x 4096 by 257
+// 278 against 274, 512 379 against 285, 128256 x 4096 by 257 1046 against 1083, 384 1331 against 1165, 128256 x 8192 by 257 2242 against 1926; without it 32000 x 4096 by 384
+// 173 against 182, 448 194 against 195, 512 239 against 178, 50000 x 4096 by 384 243 against 249, 448 270 against 251.
+bool loss_dense(int64_t tokens, bool grad) { return tokens > (grad ? 256 : 384); }
 
 struct LossPlan {
     bool dense;
@@ -344,7 +342,7 @@ struct LossPlan {
 };
 bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t capacity, LossPlan* p)
 {
-    p->dense = loss_dense(tokens);
+    p->dense = loss_dense(tokens, grad);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;

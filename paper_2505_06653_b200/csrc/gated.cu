@@ -111,16 +111,16 @@ __global__ void __launch_bounds__(256) gated_empty_kernel(const LinearOut out, i
 
 namespace {
 
-#ifndef BOF4_GATED_DENSE
-#define BOF4_GATED_DENSE 0
-#endif
-// Whether a matrix is decoded once and multiplied as plain bf16.  Both forms, us, ffn x columns by tokens: forward 11008 x 4096 by 512 119 against 121, 768 154
-// against 140, 1024 213 against 173, 28672 x 8192 by 768 633 against 692, 1024 834 against 834, 2048 1677 against 1444; backward 11008 x 4096 by 768 161
-// against 181, 1024 205 against 192, and where rows of the decoded matrix are long 28672 x 8192 by 384 508 against 545, 512 608 against 561, 768 991 against 721.
+// Whether a matrix is decoded once and multiplied as plain bf16.  Both forms, us, ffn x columns by tokens, decoding as it multiplies against this:
+//   forward    2048 x 2048 by 257 28 against 28, 512 34 against 28; 4096 x 2048 by 512 39 against 32; 8192 x 4096 by 512 80 against 85, 768 105 against 103;
+//              11008 x 4096 by 512 104 against 118, 768 139 against 140, 1024 185 against 167; 28672 x 8192 by 896 768 against 814, 1024 841 against 827
+//   backward   2048 x 2048 by 448 42 against 40; 4096 x 4096 by 512 63 against 60; 8192 x 4096 by 768 118 against 128; 11008 x 4096 by 768 165 against 175,
+//              1024 218 against 194; 28672 x 8192, where the parts of a tile are many, by 384 509 against 544, 512 621 against 556, 1024 1328 against 902
 bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
 {
-    if (BOF4_GATED_DENSE) return tokens >= BOF4_GATED_DENSE;
-    return tokens >= (!backward ? 768 : rows * cols >= (int64_t)1 << 28 ? 448 : 896);
+    const int64_t n = rows * cols;
+    if (backward) return tokens >= (n <= (int64_t)1 << 25 || n >= (int64_t)1 << 28 ? 448 : 896);
+    return tokens >= (n <= (int64_t)1 << 24 ? 257 : 768);
 }
 
 // Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.

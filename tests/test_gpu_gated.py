@@ -31,7 +31,9 @@ SHAPES = [(1, 32, 64, 64), (1, 5, 32, 32), (2, 65, 256, 64), (5, 200, 4096, 128)
           # tiles of the form for many tokens that are cut along K: into three, two goes of all clusters (forward; backward)
           (1000, 1500, 4096, 64), (1000, 2100, 2944, 64),
           # a large matrix by more than twelve tokens
-          (14, 8200, 4096, 64)]
+          (14, 8200, 4096, 64),
+          # several tiles of tokens of the form that decodes as it multiplies
+          (300, 2100, 4096, 64), (600, 4200, 4096, 64)]
 
 
 @pytest.mark.parametrize("tokens,ffn,cols,block", SHAPES)
