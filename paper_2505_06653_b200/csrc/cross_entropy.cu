@@ -166,6 +166,80 @@ loss_gradient_kernel(const float* __restrict__ logits, int64_t ld, int64_t n, in
     *reinterpret_cast<uint4*>(dz + t * ld + c0) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
 
+// All of this for a token whose logits one CTA can keep in its registers: loss, log-sum, and dz where it is wanted.
+constexpr int kCeRow = 32768;  // 1024 threads, four times eight logits each
+template <bool GRAD>
+__global__ void __launch_bounds__(1024)
+loss_row_kernel(const float* __restrict__ logits, int64_t ld, int n, const int64_t* __restrict__ targets, const float* __restrict__ dloss, float* __restrict__ loss,
+                float* __restrict__ lse, float* __restrict__ scale, uint16_t* __restrict__ dz, int* __restrict__ status)
+{
+    if (!after_previous()) return;
+    __shared__ float s_top[32], s_sum[32], s_own;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t t = blockIdx.x, target = targets[t];
+    const float* const row = logits + t * ld;
+    constexpr int N = kCeRow / 8192;
+    float v[N][8], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if ((tid + i * 1024) * 8 < n) ce_load8(row, (tid + i * 1024) * 8, n, v[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (tid + i * 1024) * 8;
+        if (c >= n) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (target == c + k && c + k < n) s_own = v[i][k], v[i][k] = -INFINITY;
+            top = fmaxf(top, v[i][k]);
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+    top = s_top[lane];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+    const float r = top > -INFINITY ? top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if ((tid + i * 1024) * 8 >= n) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            v[i][k] = __expf(v[i][k] - r);
+            sum += v[i][k];
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    sum = s_sum[lane];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+    const bool counted = target >= 0 && target < n;
+    if (tid == 0) {
+        ce_counted(target, n, status);
+        const CeToken c = ce_token(r, sum, counted ? s_own : 0.0f, counted);
+        loss[t] = c.loss;
+        if (lse) lse[t] = c.lse;
+        if (GRAD) scale[t] = counted ? (dloss ? dloss[t] : 1.0f) * c.rest : 0.0f;
+    }
+    if (!GRAD) return;
+    const float unit = 1.0f / sum;  // p_v / (1 - p_y) = exp(z_v - r) / S
+    const bool any = counted && sum != 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (tid + i * 1024) * 8;
+        if (c >= n) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[i][k] = !any ? 0.0f : target == c + k ? -1.0f : unit * v[i][k];
+        *reinterpret_cast<uint4*>(dz + t * ld + c) =
+            make_uint4(bf16_pair(v[i][0], v[i][1]), bf16_pair(v[i][2], v[i][3]), bf16_pair(v[i][4], v[i][5]), bf16_pair(v[i][6], v[i][7]));
+    }
+}
+
 // ---------------------------------------------------------------- many tokens
 
 // A piece's sums joined with those of the pieces before; E of parts that used another reference is put right.  32 tokens a CTA.
@@ -465,15 +539,19 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         else rc = linear_tc(fn, w, false, d_x, ldx, out, d_status, base, p.forward, st);
         if (rc) return rc;
         float* const scale = floats(p.scale);
-        launch_after(loss_chunk_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, d_targets, stats, own);
-        if (!grad) {
-            launch_after(loss_token_kernel, (int)((n_tokens + 7) / 8), 256, 0, st, stats, own, rows, p.chunks, d_targets, n_tokens, d_loss, d_lse, d_status);
-            BOF4_CUDA_TRY(cudaGetLastError());
-            return BOF4_OK;
+        if (rows <= kCeRow) {
+            if (grad) launch_after(loss_row_kernel<true>, (int)n_tokens, 1024, 0, st, logits, p.ld, (int)rows, d_targets, d_dloss, d_loss, d_lse, scale, dz, d_status);
+            else launch_after(loss_row_kernel<false>, (int)n_tokens, 1024, 0, st, logits, p.ld, (int)rows, d_targets, nullptr, d_loss, d_lse, nullptr, nullptr, d_status);
+        } else {
+            launch_after(loss_chunk_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, d_targets, stats, own);
+            if (grad)
+                launch_after(loss_gradient_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, stats, own, d_targets, d_dloss, d_loss,
+                             d_lse, scale, dz, d_status);
+            else
+                launch_after(loss_token_kernel, (int)((n_tokens + 7) / 8), 256, 0, st, stats, own, rows, p.chunks, d_targets, n_tokens, d_loss, d_lse, d_status);
         }
-        launch_after(loss_gradient_kernel, (int)(p.chunks * n_tokens), 256, 0, st, logits, p.ld, rows, p.chunks, stats, own, d_targets, d_dloss, d_loss, d_lse,
-                     scale, dz, d_status);
         BOF4_CUDA_TRY(cudaGetLastError());
+        if (!grad) return BOF4_OK;
         LinearOut to{};
         to.y = d_dx;
         to.ldy = ld_dx;

@@ -127,43 +127,56 @@ __device__ __forceinline__ void dn_get32(const void* p, uint32_t (&v)[8])
                  : "l"(p)
                  : "memory");
 }
-// Sixteen neighbouring values, `count` of them in the row.
+// Sixteen neighbouring values, `count` of them in the row, which begins at a multiple of `align` bytes.  (Rows of odd length begin at odd places in turn.)
 __device__ __forceinline__ void dn_store16(uint16_t* p, const float* v, int count, int align)
 {
-    uint32_t w[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
-    if (align >= 32 && count >= 16) {
-        dn_put32(p, w);
-    } else if (align >= 16 && count >= 8) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        if (count >= 16) {
-            *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        } else {
-#pragma unroll
-            for (int k = 8; k < 16; ++k)
-                if (k < count) p[k] = bf16_round(v[k]);
-        }
-    } else {
+    if (count < 16) {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
             if (k < count) p[k] = bf16_round(v[k]);
+        return;
+    }
+    if (align < 4 && (reinterpret_cast<uintptr_t>(p) & 2u)) {
+        p[0] = bf16_round(v[0]), p[15] = bf16_round(v[15]);
+#pragma unroll
+        for (int k = 1; k < 15; k += 2) *reinterpret_cast<uint32_t*>(p + k) = bf16_pair(v[k], v[k + 1]);
+        return;
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
+    if (align >= 32) {
+        dn_put32(p, w);
+    } else if (align >= 16) {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]), reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else if (align >= 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) reinterpret_cast<uint2*>(p)[k] = make_uint2(w[2 * k], w[2 * k + 1]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) reinterpret_cast<uint32_t*>(p)[k] = w[k];
     }
 }
 __device__ __forceinline__ void dn_store16(float* p, const float* v, int count, int align)
 {
+    if (count < 16 || align < 8) {
 #pragma unroll
-    for (int h = 0; h < 16; h += 8) {
-        if (align >= 32 && count >= h + 8) {
+        for (int k = 0; k < 16; ++k)
+            if (k < count) p[k] = v[k];
+    } else if (align >= 32) {
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
             uint32_t w[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[h + k]);
             dn_put32(p + h, w);
-        } else {
-#pragma unroll
-            for (int k = h; k < h + 8; ++k)
-                if (k < count) p[k] = v[k];
         }
+    } else if (align >= 16) {
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(p + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) *reinterpret_cast<float2*>(p + k) = make_float2(v[k], v[k + 1]);
     }
 }
 
@@ -213,8 +226,8 @@ __device__ __forceinline__ void dn_finish(const DenseOut& out, const DenseToken&
             for (int k = 0; k < 16; ++k) g[k] = z[32 * c + 2 * k], u[k] = z[32 * c + 2 * k + 1];
             if (out.pre) {
                 uint16_t* const p = out.pre + t * out.ld_pre + f0 + 16 * c;
-                dn_store16(p, g, left - 16 * c, out.align);
-                dn_store16(p + out.n, u, left - 16 * c, out.align);
+                dn_store16(p, g, left - 16 * c, out.pre_align);
+                dn_store16(p + out.n, u, left - 16 * c, out.pre_align);
             }
             activate_gate(g, out.act);
 #pragma unroll
@@ -295,6 +308,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     __shared__ __align__(8) unsigned long long s_full[kDnStages], s_empty[kDnStages], s_acc_full[2], s_acc_empty[2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_last;
+    if (threadIdx.x == 0) tc_fetch_map(&a_map), tc_fetch_map(&b_map);
     if (!after_previous()) return;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)dn_rank(), cluster = (int)blockIdx.x >> 1;

@@ -19,13 +19,7 @@ struct DenseOut {
     void* y;
     int64_t ldy, n, tokens;  // n: columns of z (gated: of y)
     bool y_bf16;
-    int align;               // bytes that rows of y (and both halves of those of pre) begin at multiples of: 32, 16 or less
-    template <class... L>
-    void set_align(uintptr_t addresses, L... elements)  // of y and pre, combined by or; strides and lengths in elements of 2 bytes or more
-    {
-        const uintptr_t all = addresses | (2 * (uintptr_t)(0 | ... | elements));
-        align = all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : 1;
-    }
+    int align, pre_align;    // bytes that rows of y (and both halves of those of pre) begin at multiples of, up to 32
     // gated
     const void* bias;        // [2 n] or NULL
     bool bias_bf16;
@@ -43,6 +37,13 @@ struct DenseOut {
     bool first;              // loss: no reference yet, the guess is 0
     bool keep_status;        // *status is set where a wait runs out, and not cleared before
 };
+
+// The largest power of two up to 32 that divides an address and a distance in bytes.
+inline int dense_align(const void* p, int64_t bytes)
+{
+    const uintptr_t all = reinterpret_cast<uintptr_t>(p) | (uintptr_t)bytes | 32u;
+    return (int)(all & (~all + 1));
+}
 
 struct DenseWork {
     int tiles_m, tiles_n, per_tile;  // tiles of 256 tokens, of 256 columns of z, k-blocks of 64 of a tile

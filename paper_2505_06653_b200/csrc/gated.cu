@@ -261,8 +261,8 @@ extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scal
     to.pre = out.pre;
     to.ld_pre = ld_pre;
     to.act = activation;
-    if (d_pre) to.set_align(reinterpret_cast<uintptr_t>(d_h) | reinterpret_cast<uintptr_t>(d_pre), ldh, ld_pre, ffn);
-    else to.set_align(reinterpret_cast<uintptr_t>(d_h), ldh);
+    to.align = dense_align(d_h, ldh * (out.y_bf16 ? 2 : 4));
+    to.pre_align = dense_align(d_pre, (ld_pre | ffn) * 2);
     return dense_product(fn, q, to, d_status, base, p.product, st);
 }
 
@@ -342,7 +342,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
         to.n = cols;
         to.tokens = n_tokens;
         to.y_bf16 = true;
-        to.set_align(reinterpret_cast<uintptr_t>(d_dx), ld_dx);
+        to.align = dense_align(d_dx, ld_dx * 2);
         return dense_product(fn, q, to, d_status, base, p.product, st);
     }
     LinearOut out{};

@@ -49,6 +49,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap code_map, const void* __re
                   const float* __restrict__ correction, int* __restrict__ status, const FewWork work, unsigned long long* __restrict__ tickets,
                   float* __restrict__ sums)
 {
+    if (threadIdx.x == 0) tc_fetch_map(&code_map);
     if (!after_previous()) return;
     constexpr int W = FewGeo<NT>::warps;
     const int D = work.defer, P = (int)out.tokens * kFewPitch;

@@ -232,6 +232,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
     __shared__ __align__(16) float2 s_levels[8];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_sums, s_sum[2];
+    if (threadIdx.x == 0) tc_fetch_map(&code_map), tc_fetch_map(&token_map);
     if (!after_previous()) return;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per_tile = work.per_tile, box_n = work.box_n;

@@ -66,6 +66,11 @@ __device__ __forceinline__ bool tc_look(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0u;
 }
+// A launch's own parameters: nothing of the caller's memory is touched.
+__device__ __forceinline__ void tc_fetch_map(const CUtensorMap* map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
 // One lane of a converged warp, always the same one.
 __device__ __forceinline__ bool tc_elect()
 {
