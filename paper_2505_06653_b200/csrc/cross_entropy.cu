@@ -534,6 +534,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         out.ldy = p.ld;
         out.n = rows;
         out.tokens = n_tokens;
+        out.few_parts = true;
         out.set_alignment();
         if (few_pays(rows, cols, n_tokens, w.capacity > 0)) rc = linear_few(fn, w, d_x, ldx, out, d_status, base, p.forward, st);
         else rc = linear_tc(fn, w, false, d_x, ldx, out, d_status, base, p.forward, st);
@@ -560,6 +561,7 @@ extern "C" int bof4_cross_entropy(const uint8_t* d_codes, const void* d_scales, 
         to.tokens = n_tokens;
         to.keep_status = true;
         to.scale = scale;
+        to.few_parts = true;
         to.set_alignment();
         return linear_tc(fn, w, true, dz, p.ld, to, d_status, base, p.backward, st);
     }

@@ -221,6 +221,7 @@ extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scal
     out.n = ffn;
     out.tokens = n_tokens;
     out.gated = true;
+    out.few_parts = true;
     out.set_alignment();
     if (cols == 0) {
         const int64_t want = (ffn * n_tokens + 255) / 256;
@@ -352,6 +353,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     out.act = BOF4_ACT_NONE;
     out.n = cols;
     out.tokens = n_tokens;
+    out.few_parts = true;
     out.set_alignment();
     return linear_tc(fn, w, true, dz, p.ld, out, d_status, base, p.product, st);
 }

@@ -208,6 +208,7 @@ struct LinearOut {
     bool pairs, wide;
     const float* scale;  // backward: what the sums of a token are multiplied by, or NULL
     bool gated;
+    bool few_parts;    // tiles are cut along K only as far as it pays (gated, loss)
     bool keep_status;  // *status is set where a wait runs out, and not cleared before
     void set_alignment()
     {

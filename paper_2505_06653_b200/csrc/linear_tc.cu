@@ -39,7 +39,7 @@ struct LtPlan {
 };
 
 // False: too large for 32-bit line numbers.
-bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp32, int64_t capacity, LtPlan* p)
+bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp32, int64_t capacity, LtPlan* p, bool few_parts = false)
 {
     const int64_t m = backward ? cols : rows, k = backward ? rows : cols;
     // (k-blocks past the end of K have zeros for the tokens)
@@ -70,6 +70,19 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp3
     const int64_t lines = tiles * per_tile, most = tiles * kLtMaxParts;
     int64_t ctas = lines < kSMs ? lines : kSMs;
     if (ctas > most) ctas = most;
+    if (few_parts && tiles < ctas) {
+        // A line takes 1.7 us; a tile that is cut is written, waited for and read again, 2.5 us and 0.3 to 1.3 a part.  So a small matrix is not cut, and a few tiles
+        // of a long K are not cut into all the CTAs there are, where equal parts of each tile save a seventh by this reckoning: gated 752 x 5568 by 201 tokens 38
+        // us with every CTA at work, 31 this way; backward 3208 x 640 by 353 49 and 42.
+        const double part = 0.3 + (double)box / 256.0, full = (double)lines / (double)ctas * 1.7 + 2.5 + ((double)ctas / (double)tiles + 1.0) * part;
+        double best = 0.0;
+        int64_t each = 0;
+        for (int64_t j = 1; tiles * j <= ctas; ++j) {
+            const double t = (double)((per_tile + j - 1) / j) * 1.7 + (j > 1 ? 2.5 + (double)j * part : 0.0);
+            if (!each || t < best) best = t, each = j;
+        }
+        if (best < 0.85 * full) ctas = tiles * each;
+    }
     p->ctas = (int)ctas;
     w.each = (int)(lines / ctas);
     w.extra = (int)(lines % ctas);
@@ -96,7 +109,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
 {
     LtPlan p;
     const bool opq = w.out_idx && w.capacity > 0;
-    if (!lt_plan(w.rows, w.cols, out.tokens, backward, !out.y_bf16, opq ? w.capacity : 0, &p)) {
+    if (!lt_plan(w.rows, w.cols, out.tokens, backward, !out.y_bf16, opq ? w.capacity : 0, &p, out.few_parts)) {
         set_error("%s: matrix or batch too large", who);
         return BOF4_ERR_SHAPE;
     }
