@@ -79,7 +79,7 @@ __device__ __forceinline__ void ce_load8(const float* __restrict__ row, int64_t 
         for (int k = 0; k < 8; ++k) v[k] = c + k < n ? __ldcg(row + c + k) : -INFINITY;
     }
 }
-// Reference and sum of a chunk of a token's logits but for the target's, which is kept.
+// Reference and sum of a chunk of a token's logits but for the target's, which is kept (13 tokens of 128256: 5.6 us, and 7.7 for the gradients; latency and launches).
 __global__ void __launch_bounds__(256)
 loss_chunk_kernel(const float* __restrict__ logits, int64_t ld, int64_t n, int chunks, const int64_t* __restrict__ targets, float2* __restrict__ stats,
                   float* __restrict__ own)
@@ -242,7 +242,8 @@ loss_row_kernel(const float* __restrict__ logits, int64_t ld, int n, const int64
 
 // ---------------------------------------------------------------- many tokens
 
-// A piece's sums joined with those of the pieces before; E of parts that used another reference is put right.  32 tokens a CTA.
+// A piece's sums joined with those of the pieces before; E of parts that used another reference is put right.  32 tokens a CTA, a warp every 32nd part of the
+// piece, kept in registers (4096 tokens, 512 parts: 9 us, latency).
 __global__ void __launch_bounds__(1024)
 loss_combine_kernel(const float2* __restrict__ stats, int parts, int64_t tokens, bool first, float* __restrict__ ref, float* __restrict__ sum,
                     float* __restrict__ factor, uint16_t* __restrict__ e, int64_t ld, int64_t n)
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(256) loss_value_kernel(const LossFinal f)
     f.loss[t] = c.loss;
     if (f.lse) f.lse[t] = c.lse;
 }
-// dx of a token, a CTA each: the running sum less the target's row, which is decoded here.
+// dx of a token, a CTA each: the running sum less the target's row, which is decoded here (4096 tokens of 4096 columns 18 us, 110 MB).
 template <class ST>
 __global__ void __launch_bounds__(256) loss_dx_kernel(const LossFinal f)
 {

@@ -13,8 +13,12 @@
 //
 // The tensor cores cut a sum off at every step of 16 of K, so an accumulator takes a segment of K only, and the segments are added in
 // registers, rounded.  Results in fp32 (and logits) have segments of 1024 of K: losses with K = 4096 are off by 0.6e-6 in 2-norms, by 1.4e-6 with segments of
-// 2048, 3.6e-6 with one accumulator.  That is nothing beside a rounding to bf16 (1.7e-3), and each reading of an accumulator costs power, by which long products
-// are bound: 4096 tokens by 16384 x 4096 took 390 us with segments of 1024 and 353 with 2048 or 4096.
+// 2048, 3.6e-6 with one accumulator.  That is nothing beside a rounding to bf16 (1.7e-3), and results that wait for an accumulator to be read hold the next
+// one up, so results in bf16 have longer ones (4096 tokens by 128256 x 4096 with the gradient: 1 % between segments of 1024 and 2048).
+//
+// What bounds it: with all SMs at work the power limit, 1.55 to 1.63 PFLOP/s in a cold launch (28672 x 4096 by 4096 tokens 622 us, tensor cores busy 81 to 86 % of the time at
+// 1024 tokens), 1.2 to 1.3 in a row of calls; with 48 of the 74 pairs at work a k-block takes the 512 cycles that it has to.  A lane has a token's results, so that each store
+// of a warp goes to 32 rows: whole sectors of 32 bytes instead of halves took a gated block of 4096 tokens from 847 to 760 us, a loss with its gradient from 7.3 to 7.0 ms.
 //
 // Tiles go to the clusters in turn.  What is left after the last whole round is cut along K into as many parts as there are clusters for
 // (74 / tiles, at most eight) where K is long enough to pay for it.  They come first; the sums of a

@@ -33,7 +33,8 @@ __device__ __forceinline__ void activate_gradients(const float (&d)[8], float (&
 }
 
 // dz of a gated block, rounded to bf16 for the tensor cores, and the sums of the unrounded dz over a CTA's tokens: as dz_kernel
-// (linear.cu), with two results per element.  Sums are added in a fixed order.
+// (linear.cu), with two results per element.  Sums are added in a fixed order.  One pass over dh and pre, bound by memory: 4096 tokens of 14336 columns by SILU 91 us,
+// 587 MB at 6.45 TB/s (170 us with four tokens a warp on their way: 113 registers left two CTAs an SM).
 template <class DT, bool SUMS>
 __global__ void __launch_bounds__(256, SUMS ? 2 : DT::code == BOF4_F32 ? 3 : 4)
 gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __restrict__ pre, int64_t ld_pre, int act, int64_t n, int64_t tokens,
