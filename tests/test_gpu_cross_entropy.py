@@ -254,6 +254,27 @@ def test_streams_graphs_and_workspaces(bof4, tokens):
             assert all(torch.equal(a, b) for a, b in zip(out, want[k]))
 
 
+@pytest.mark.parametrize("tokens", [2, 60, 700])
+def test_two_calls_at_once(bof4, tokens):
+    """On two streams, with workspaces of their own, in turn."""
+    rows, cols, block = 40000, 256, 64
+    lv, codes, scales = real_case(rows, cols, block, 4)
+    levels = torch.from_numpy(LV).cuda()
+    g = torch.Generator().manual_seed(3)
+    xs = [torch.randn(tokens, cols, generator=g).bfloat16().cuda() for _ in range(2)]
+    ys = [targets_of(tokens, rows, k) for k in range(2)]
+    call = lambda k: bof4.bof4_cross_entropy(codes, scales, rows, cols, block, levels, xs[k], ys[k], want_dx=True)  # noqa: E731
+    want = [call(0), call(1)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(10):
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got.append((k, call(k)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k, out in got for a, b in zip(out, want[k]))
+
+
 def test_nothing_to_do(bof4):
     lv, codes, scales = integer_case(64, 64, 64, 1)
     x = torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda")

@@ -241,6 +241,33 @@ def test_streams_graphs_and_workspaces(bof4, tokens):
             assert all(torch.equal(a, b) for a, b in zip(out[:3], want[k])) and int(out[3].item()) == 0 and int(out[4].item()) == 0
 
 
+@pytest.mark.parametrize("tokens", [2, 60, 1000])
+def test_two_calls_at_once(bof4, tokens):
+    """On two streams, with workspaces of their own, in turn: what one computes is none of the other's."""
+    ffn, cols, block = 1200, 1024, 64
+    lv, codes, scales = real_case(2 * ffn, cols, block, 4)
+    levels = torch.from_numpy(lv).cuda()
+    g = torch.Generator().manual_seed(3)
+    xs = [torch.randn(tokens, cols, generator=g).bfloat16().cuda() for _ in range(2)]
+    dhs = [torch.randn(tokens, ffn, generator=g).bfloat16().cuda() for _ in range(2)]
+
+    def call(k):
+        pre = torch.empty(tokens, 2 * ffn, dtype=torch.bfloat16, device="cuda")
+        h, s1 = bof4.bof4_gated(codes, scales, ffn, cols, block, levels, xs[k], pre=pre)
+        dx, db, s2 = bof4.bof4_gated_backward(codes, scales, ffn, cols, block, levels, dhs[k], pre, want_dbias=True)
+        return h, pre, dx, db, s1, s2
+
+    want = [call(0), call(1)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(10):
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got.append((k, call(k)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k, out in got for a, b in zip(out, want[k]))
+
+
 def test_gradient_against_differences(bof4):
     """dx against central differences of the block itself in fp32, summed with weights: a step e leaves e^2 / 6 times the third derivative and
     the roundings 2^-14 mag / e; values are chosen so that both stay below 2^-7 of the gradient's norm."""
