@@ -6,7 +6,7 @@
 // in and out, 512 of the 128-byte cycles of its data path, as long as the products themselves take (a tile of 128 x 256
 // of one SM takes 768: linear_tc.cu).
 //
-//   1 loads    TMA loads of both operands, seven stages; those of both SMs complete the first SM's barrier
+//   1 loads    TMA loads of both operands, six or seven stages; those of both SMs complete the first SM's barrier
 //   1 issuer   in the first SM: four instructions (K = 16) per k-block
 //   16 results a warp has 32 tokens and a quarter of the columns of a finished accumulator (there are two); a lane keeps the 64
 //              sums of its token in registers
@@ -31,10 +31,12 @@
 namespace bof4 {
 
 constexpr int kDnM = 256, kDnN = 256, kDnK = 64;
-constexpr int kDnStages = 7;
+template <int USE>
+constexpr int dn_stages = USE == kDenseGated ? 6 : 7;  // (the gated block's results need room of their own, and six are as fast)
 constexpr int kDnHalf = 128 * kDnK * 2;         // an SM's part of an operand in a stage
 constexpr int kDnStage = 2 * kDnHalf;
-constexpr int kDnSmem = kDnStages * kDnStage + 1024;
+constexpr int kDnSmem = 7 * kDnStage + 1024;
+constexpr int kDnBlock = 32 * 8 * 4;            // a warp's block of results on their way out: 32 rows of 8 words
 constexpr int kDnResults = 16, kDnCols = 64;    // warps that read results, columns of each
 constexpr int kDnLoads = kDnResults, kDnIssue = kDnResults + 1;
 constexpr int kDnThreads = 32 * (kDnResults + 2);
@@ -184,6 +186,64 @@ __device__ __forceinline__ void dn_store16(float* p, const float* v, int count, 
     }
 }
 
+// Eight words of each lane's row, through shared memory: a store of the warp goes to four rows, wherever they begin.  p: the lane's row, `count` elements
+// of bf16 (two a word) or fp32 of it exist; rows of bf16 may begin at odd elements.  All lanes take part.
+template <class T>
+__device__ __forceinline__ void dn_rows(uint32_t block, const uint32_t (&w)[8], T* p, bool live, int count, int lane)
+{
+    constexpr int E = sizeof(T) == 2 ? 2 : 1;
+    __syncwarp();
+#pragma unroll
+    for (uint32_t c = 0; c < 2; ++c)  // without meeting a bank twice
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(block + (uint32_t)(lane * 32) + ((c ^ (uint32_t)(lane >> 2 & 1)) << 4)), "r"(w[4 * c]), "r"(w[4 * c + 1]),
+                     "r"(w[4 * c + 2]), "r"(w[4 * c + 3])
+                     : "memory");
+    __syncwarp();
+    const int l = lane & 7;
+    const unsigned int rows = __ballot_sync(kFull, live);
+#pragma unroll 4
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        uint32_t v;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(block + (uint32_t)(r * 32) + (((uint32_t)(l >> 2) ^ (uint32_t)(r >> 2 & 1)) << 4) + (uint32_t)(l & 3) * 4u) : "memory");
+        T* const q = reinterpret_cast<T*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(p), r)) + E * l;
+        if (!(rows >> r & 1u) || E * l >= count) continue;
+        if (E == 1 || (E * l + 1 < count && !(reinterpret_cast<uintptr_t>(q) & 2u))) {
+            *reinterpret_cast<uint32_t*>(q) = v;
+        } else {
+            uint16_t* const h = reinterpret_cast<uint16_t*>(q);
+            h[0] = (uint16_t)v;
+            if (E * l + 1 < count) h[1] = (uint16_t)(v >> 16);
+        }
+    }
+}
+// Sixteen values of each lane's row: from the lanes where rows begin at multiples of 16 bytes, through shared memory elsewhere.
+__device__ __forceinline__ void dn_put16(uint32_t block, uint16_t* p, const float* v, bool live, int count, int align, int lane)
+{
+    if (align >= 16) {
+        if (live) dn_store16(p, v, count, align);
+        return;
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
+    dn_rows(block, w, p, live, count, lane);
+}
+__device__ __forceinline__ void dn_put16(uint32_t block, float* p, const float* v, bool live, int count, int align, int lane)
+{
+    if (align >= 16) {
+        if (live) dn_store16(p, v, count, align);
+        return;
+    }
+#pragma unroll
+    for (int h = 0; h < 16; h += 8) {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[h + k]);
+        dn_rows(block, w, p + h, live, count - h, lane);
+    }
+}
+
 // What is known of a token before its sums are.
 struct DenseToken {
     int64_t target;
@@ -202,46 +262,50 @@ __device__ __forceinline__ DenseToken dn_token(const DenseOut& out, int64_t t)
     return k;
 }
 
-// A token's sums of columns o0 ... o0 + 63 of z (gated: gate and up in turn, of columns o0 / 2 ... of y).
+// A token's sums of columns o0 ... o0 + 63 of z, gate and up in turn: columns o0 / 2 ... of y.  (All lanes of the warp take part.)
+__device__ __forceinline__ void dn_gated(const DenseOut& out, float (&z)[kDnCols], int64_t t, int64_t o0, uint32_t block, int lane)
+{
+    const int64_t f0 = o0 >> 1;
+    const int left = (int)(out.n - f0 < 32 ? out.n - f0 : 32);
+    const bool live = t < out.tokens;
+    if (left <= 0) return;
+    if (out.bias) {
+#pragma unroll
+        for (int j = 0; j < kDnCols / 2; ++j) {
+            if (j < left) {
+                const int64_t f = f0 + j;
+                z[2 * j] += out.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(out.bias) + f)) : __ldg(static_cast<const float*>(out.bias) + f);
+                z[2 * j + 1] += out.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(out.bias) + out.n + f))
+                                              : __ldg(static_cast<const float*>(out.bias) + out.n + f);
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < kDnCols / 32; ++c) {
+        const int count = left - 16 * c;
+        if (count <= 0) break;
+        float g[16], u[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) g[k] = z[32 * c + 2 * k], u[k] = z[32 * c + 2 * k + 1];
+        if (out.pre) {
+            uint16_t* const p = out.pre + t * out.ld_pre + f0 + 16 * c;
+            dn_put16(block, p, g, live, count, out.pre_align, lane);
+            dn_put16(block, p + out.n, u, live, count, out.pre_align, lane);
+        }
+        activate_gate(g, out.act);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) g[k] *= u[k];
+        const int64_t at = t * out.ldy + f0 + 16 * c;
+        if (out.y_bf16) dn_put16(block, static_cast<uint16_t*>(out.y) + at, g, live, count, out.align, lane);
+        else dn_put16(block, static_cast<float*>(out.y) + at, g, live, count, out.align, lane);
+    }
+}
+
+// The same of the other products.
 template <int USE>
 __device__ __forceinline__ void dn_finish(const DenseOut& out, const DenseToken& token, float (&z)[kDnCols], int64_t t, int64_t o0)
 {
     if (t >= out.tokens) return;
-    if (USE == kDenseGated) {
-        const int64_t f0 = o0 >> 1;
-        const int left = (int)(out.n - f0 < 32 ? out.n - f0 : 32);
-        if (left <= 0) return;
-        if (out.bias) {
-#pragma unroll
-            for (int j = 0; j < kDnCols / 2; ++j) {
-                if (j < left) {
-                    const int64_t f = f0 + j;
-                    z[2 * j] += out.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(out.bias) + f)) : __ldg(static_cast<const float*>(out.bias) + f);
-                    z[2 * j + 1] += out.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(out.bias) + out.n + f))
-                                                  : __ldg(static_cast<const float*>(out.bias) + out.n + f);
-                }
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < kDnCols / 32; ++c) {
-            if (16 * c >= left) break;
-            float g[16], u[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) g[k] = z[32 * c + 2 * k], u[k] = z[32 * c + 2 * k + 1];
-            if (out.pre) {
-                uint16_t* const p = out.pre + t * out.ld_pre + f0 + 16 * c;
-                dn_store16(p, g, left - 16 * c, out.pre_align);
-                dn_store16(p + out.n, u, left - 16 * c, out.pre_align);
-            }
-            activate_gate(g, out.act);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) g[k] *= u[k];
-            const int64_t at = t * out.ldy + f0 + 16 * c;
-            if (out.y_bf16) dn_store16(static_cast<uint16_t*>(out.y) + at, g, left - 16 * c, out.align);
-            else dn_store16(static_cast<float*>(out.y) + at, g, left - 16 * c, out.align);
-        }
-        return;
-    }
     const int left = (int)(out.n - o0 < kDnCols ? out.n - o0 : kDnCols);
     if (left <= 0) return;
     if (USE == kDenseStore) {
@@ -308,6 +372,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDnThreads, 1)
 dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const DenseOut out, int* __restrict__ status,
              const DenseWork work, unsigned long long* __restrict__ tickets, float* __restrict__ parts)
 {
+    constexpr int kDnStages = dn_stages<USE>;
     extern __shared__ unsigned char s_dyn[];
     __shared__ __align__(8) unsigned long long s_full[kDnStages], s_empty[kDnStages], s_acc_full[2], s_acc_empty[2];
     __shared__ uint32_t s_tmem;
@@ -417,6 +482,10 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             for (int u = cluster; u < work.split * work.parts; u += work.clusters) tc_ticket_open(tickets + 2 * (u / work.parts) + rank, work.epoch);
         int seg = 0;
         bool ok = true;
+        auto finish = [&](float (&sums)[kDnCols], const DenseToken& token, int64_t t, int64_t o0) {
+            if (USE == kDenseGated) dn_gated(out, sums, t, o0, ring + (uint32_t)(kDnStages * kDnStage + warp * kDnBlock), lane);
+            else dn_finish<USE>(out, token, sums, t, o0);
+        };
         while (ok && walk.step(work)) {
             int m, n;
             dn_place(work, walk.tile, m, n);
@@ -445,7 +514,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             }
             if (!(ok = all16(ok))) break;
             if (walk.k0 == 0 && walk.k1 == work.per_tile) {
-                dn_finish<USE>(out, token, z, t, o0);
+                finish(z, token, t, o0);
                 continue;
             }
             // a part of a tile
@@ -471,7 +540,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 #pragma unroll
                 for (int k = 0; k < kDnCols; ++k) z[k] += __ldcg(p + k * 128);
             }
-            dn_finish<USE>(out, token, z, t, o0);
+            finish(z, token, t, o0);
         }
         if (!ok && lane == 0) s_fail = 1;
     }
