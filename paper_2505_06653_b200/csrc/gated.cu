@@ -8,6 +8,8 @@
 // for few tokens (linear_few.cu), the one that decodes as it multiplies (linear_tc.cu), and, for many tokens, a decoded matrix and
 // a product of plain operands (dense_tc.cu).  z itself is written where a backward pass will want it and never read here.
 // The backward product is that of bof4_linear_backward over all 2 F rows at once.
+#include <type_traits>
+
 #include "dense_tc.cuh"
 
 namespace bof4 {
@@ -35,30 +37,58 @@ __device__ __forceinline__ void activate_gradients(const float (&d)[8], float (&
 // dz of a gated block, rounded to bf16 for the tensor cores, and the sums of the unrounded dz over a CTA's tokens: as dz_kernel
 // (linear.cu), with two results per element.  Sums are added in a fixed order.  One pass over dh and pre, bound by memory: 4096 tokens of 14336 columns by SILU 91 us,
 // 587 MB at 6.45 TB/s (170 us with four tokens a warp on their way: 113 registers left two CTAs an SM).
-template <class DT, bool SUMS>
-__global__ void __launch_bounds__(256, SUMS ? 2 : DT::code == BOF4_F32 ? 3 : 4)
+// VEC: a lane has eight neighbouring columns, in one load; where rows begin at odd places or end inside of eight, every 32nd column, so that the lanes of
+// a load are neighbours (a whole backward pass of 2653 tokens, 22957 columns by GELU with the bias gradient and K = 640: 682 us with eight neighbours a lane, 411 this way).
+template <class DT>
+struct DzLoads {  // of the lane's eight columns, as they are in memory
+    typename std::conditional<DT::code == BOF4_F32, float, uint16_t>::type v[8];
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count)
+    {
+        using T = typename std::conditional<DT::code == BOF4_F32, float, uint16_t>::type;
+        const T* const q = static_cast<const T*>(p) + at;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 32 * k < count ? __ldg(q + 32 * k) : T(0);
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (DT::code == BOF4_F32) f[k] = v[k];
+            else f[k] = bf16_value(v[k]);
+        }
+    }
+};
+template <class DT, bool SUMS, bool VEC>
+__global__ void __launch_bounds__(256, SUMS ? 2 : DT::code == BOF4_F32 || !VEC ? 3 : 4)
 gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __restrict__ pre, int64_t ld_pre, int act, int64_t n, int64_t tokens,
-                bool vec, uint16_t* __restrict__ dz, int64_t ld_dz, float* __restrict__ sums, int col_blocks, int per)
+                uint16_t* __restrict__ dz, int64_t ld_dz, float* __restrict__ sums, int col_blocks, int per)
 {
     if (!after_previous()) return;
     __shared__ float s_sum[SUMS ? 8 : 1][2 * kDzCols + 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t chunk = blockIdx.x / col_blocks, c0 = (int64_t)(blockIdx.x % col_blocks) * kDzCols + lane * 8;
-    const int count = (int)(n - c0 < 8 ? n - c0 : 8);
-    const bool v8 = vec && count == 8;
+    constexpr int kLane = VEC ? 8 : 1, kNext = VEC ? 1 : 32;  // between the columns of two lanes, of a lane
+    const int64_t chunk = blockIdx.x / col_blocks, c0 = (int64_t)(blockIdx.x % col_blocks) * kDzCols + lane * kLane;
+    const int count = (int)(n - c0 < kDzCols ? n - c0 : kDzCols);  // columns from the lane's first
     float sum[16] = {};
     if (count > 0) {
         constexpr int N = 2;  // tokens on their way at a time: more cost warps
 #pragma unroll 1
         for (int64_t t0 = chunk * per + warp; t0 < chunk * per + per && t0 < tokens; t0 += 8 * N) {
-            Dz8<DT> a[N];
-            Dz8<BF16> b[N], c[N];
+            typename std::conditional<VEC, Dz8<DT>, DzLoads<DT>>::type a[N];
+            typename std::conditional<VEC, Dz8<BF16>, DzLoads<BF16>>::type b[N], c[N];
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                if (t0 + 8 * u >= tokens || t0 + 8 * u >= chunk * per + per) break;
-                a[u].load(dh, (t0 + 8 * u) * ld_dh + c0, count, v8);
-                b[u].load(pre, (t0 + 8 * u) * ld_pre + c0, count, v8);
-                c[u].load(pre, (t0 + 8 * u) * ld_pre + n + c0, count, v8);
+                const int64_t t = t0 + 8 * u;
+                if (t >= tokens || t >= chunk * per + per) break;
+                if constexpr (VEC) {
+                    a[u].load(dh, t * ld_dh + c0, 8, true);
+                    b[u].load(pre, t * ld_pre + c0, 8, true);
+                    c[u].load(pre, t * ld_pre + n + c0, 8, true);
+                } else {
+                    a[u].load(dh, t * ld_dh + c0, count);
+                    b[u].load(pre, t * ld_pre + c0, count);
+                    c[u].load(pre, t * ld_pre + n + c0, count);
+                }
             }
 #pragma unroll
             for (int u = 0; u < N; ++u) {
@@ -70,23 +100,23 @@ gated_dz_kernel(const void* __restrict__ dh, int64_t ld_dh, const uint16_t* __re
                 activate_gradients(d, g, up, act);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (SUMS && k < count) sum[k] += g[k], sum[8 + k] += up[k];
+                    if (SUMS && (VEC || 32 * k < count)) sum[k] += g[k], sum[8 + k] += up[k];
                 if (!dz) continue;
                 uint16_t* const p = dz + (t0 + 8 * u) * ld_dz + c0;
-                if (v8) {
+                if (VEC) {
                     *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4], g[5]), bf16_pair(g[6], g[7]));
                     *reinterpret_cast<uint4*>(p + n) = make_uint4(bf16_pair(up[0], up[1]), bf16_pair(up[2], up[3]), bf16_pair(up[4], up[5]), bf16_pair(up[6], up[7]));
                 } else {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        if (k < count) p[k] = bf16_round(g[k]), p[n + k] = bf16_round(up[k]);
+                        if (32 * k < count) p[32 * k] = bf16_round(g[k]), p[n + 32 * k] = bf16_round(up[k]);
                 }
             }
         }
     }
     if constexpr (SUMS) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s_sum[warp][lane * 8 + k] = sum[k], s_sum[warp][kDzCols + lane * 8 + k] = sum[8 + k];
+        for (int k = 0; k < 8; ++k) s_sum[warp][lane * kLane + k * kNext] = sum[k], s_sum[warp][kDzCols + lane * kLane + k * kNext] = sum[8 + k];
         __syncthreads();
         const int64_t c = (int64_t)(blockIdx.x % col_blocks) * kDzCols + threadIdx.x;
         if (c < n) {
@@ -326,10 +356,13 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     uint16_t* const dz = reinterpret_cast<uint16_t*>(base + p.dz);
     float* const sums = p.chunks > 1 ? reinterpret_cast<float*>(base + p.sums) : d_dbias;
     const bool vec = aligned16(d_dh) && ld_dh % 8 == 0 && aligned16(d_pre) && ld_pre % 8 == 0 && ffn % 8 == 0;
-    auto* const kern = dh_dtype == BOF4_F32 ? (d_dbias ? gated_dz_kernel<F32, true> : gated_dz_kernel<F32, false>)
-                                            : (d_dbias ? gated_dz_kernel<BF16, true> : gated_dz_kernel<BF16, false>);
-    launch_after(kern, (int)(p.chunks * col_blocks), 256, 0, st, d_dh, ld_dh,
-                 static_cast<const uint16_t*>(d_pre), ld_pre, activation, ffn, n_tokens, vec, product ? dz : nullptr, p.ld, d_dbias ? sums : nullptr, col_blocks, p.per);
+    auto pick = [&](auto type) {
+        using DT = decltype(type);
+        if (vec) return d_dbias ? gated_dz_kernel<DT, true, true> : gated_dz_kernel<DT, false, true>;
+        return d_dbias ? gated_dz_kernel<DT, true, false> : gated_dz_kernel<DT, false, false>;
+    };
+    launch_after(dh_dtype == BOF4_F32 ? pick(F32()) : pick(BF16()), (int)(p.chunks * col_blocks), 256, 0, st, d_dh, ld_dh, static_cast<const uint16_t*>(d_pre), ld_pre,
+                 activation, ffn, n_tokens, product ? dz : nullptr, p.ld, d_dbias ? sums : nullptr, col_blocks, p.per);
     if (d_dbias && p.chunks > 1) linear_dbias(sums, 2 * ffn, p.chunks, d_dbias, st);
     BOF4_CUDA_TRY(cudaGetLastError());
     if (!product) return BOF4_OK;
