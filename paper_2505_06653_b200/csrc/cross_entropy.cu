@@ -426,7 +426,7 @@ bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t ca
     };
     const size_t t = (size_t)tokens;
     if (!p->dense) {
-        p->forward = few_pays(rows, cols, tokens, capacity > 0) ? linear_few_ws_bytes(rows, cols, tokens, capacity)
+        p->forward = few_pays(rows, cols, tokens, capacity > 0) ? linear_few_ws_bytes(rows, cols, tokens, capacity, true)
                                                                           : linear_tc_ws_bytes(rows, cols, tokens, false, capacity);
         p->backward = grad ? linear_tc_ws_bytes(rows, cols, tokens, true, capacity) : 0;
         if (!p->forward || (grad && !p->backward)) return false;

@@ -169,7 +169,7 @@ bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_
     p->product = 256;
     if (cols) {
         if (p->dense) p->product = backward ? dense_ws_bytes(tokens, cols, rows) : dense_ws_bytes(tokens, rows, cols);
-        else if (!backward && few_pays(rows, cols, tokens, capacity > 0)) p->product = linear_few_ws_bytes(rows, cols, tokens, capacity);
+        else if (!backward && few_pays(rows, cols, tokens, capacity > 0)) p->product = linear_few_ws_bytes(rows, cols, tokens, capacity, true);
         else p->product = linear_tc_ws_bytes(rows, cols, tokens, backward, capacity);
         if (!p->product) return false;
     }

@@ -344,7 +344,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
 
 // The form for one to sixteen tokens.
 bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list);
-size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity);
+size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity, bool few_parts = false);
 int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, const LinearOut& out, int* status, void* ws, size_t ws_bytes,
                cudaStream_t st);
 // Where it pays in a gated block or a loss: in large matrices up to twelve tokens only (28672 x 8192 gated by 12 164 us against 158, by 16 186 against 158;

@@ -302,7 +302,7 @@ struct FewPlan {
     size_t sums = 0, correction = 0, total = 0;  // byte offsets (the tickets are at 0), and the bytes of all
 };
 
-FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
+FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list, bool few_parts)
 {
     FewPlan p;
     const int warps = tokens > 8 ? FewGeo<2>::warps : FewGeo<1>::warps;
@@ -312,6 +312,19 @@ FewPlan few_plan(int64_t rows, int64_t cols, int64_t tokens, bool list)
     for (int64_t n = slices; n <= 4 * slices && n <= kSMs && n <= stripes; ++n) {
         const int64_t wide = (stripes + n - 1) / n, used = wide * (warps / wide) * 64 * stripes / (wide * n);  // warps that have a stripe, in 64ths
         if (used > best + warps * 4) best = used, slices = n;
+    }
+    if (few_parts) {
+        // The slices of a row are added up by the CTA that comes last, 64 or 128 rows of a token at a time, so that many slices cost more than idle warps do (13943 x 3328 by
+        // 14 tokens: 70 us in seven slices).  A round of all warps takes 1.75 us, of few of them its latency, a turn of the last sums 0.9 and 0.9 for every four slices.
+        const int64_t least = (stripes + warps - 1) / warps;
+        double least_time = 0.0;
+        for (int64_t n = least; n <= 4 * least && n <= kSMs && n <= stripes; ++n) {
+            const int64_t wide = (stripes + n - 1) / n, groups = warps / wide < tiles ? warps / wide : tiles, want = (tiles + groups - 1) / groups;
+            const int64_t peers = want < kSMs / n ? want : kSMs / n, rounds = (tiles + peers * groups - 1) / (peers * groups);
+            const double round = 1.75 * (double)(groups * wide) / warps, turns = (double)((rounds * groups * tokens * 4 + 32 * warps - 1) / (32 * warps));
+            const double t = (double)rounds * (round > 0.9 ? round : 0.9) + (n > 1 ? 1.5 + turns * (0.9 + 0.9 * (double)((n + 3) / 4)) : 0.0);
+            if (n == least || t < least_time) least_time = t, slices = n;
+        }
     }
     FewWork& w = p.work;
     w.slices = (int)slices;
@@ -340,12 +353,12 @@ bool linear_few_applies(int64_t rows, int64_t cols, int64_t tokens, bool list)
     return tokens <= (list ? kFewListTokens : kFewTokens) && cols <= 32768 && rows <= (1 << 26);
 }
 
-size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity) { return few_plan(rows, cols, tokens, capacity > 0).total; }
+size_t linear_few_ws_bytes(int64_t rows, int64_t cols, int64_t tokens, int64_t capacity, bool few_parts) { return few_plan(rows, cols, tokens, capacity > 0, few_parts).total; }
 
 int linear_few(const char* who, const LinearW& w, const void* x, int64_t ldx, const LinearOut& out, int* status, void* ws, size_t ws_bytes, cudaStream_t st)
 {
     const bool list = w.out_idx && w.capacity > 0;
-    FewPlan p = few_plan(w.rows, w.cols, out.tokens, list);
+    FewPlan p = few_plan(w.rows, w.cols, out.tokens, list, out.few_parts);
     if (ws_bytes < p.total) {
         set_error("%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes, p.total);
         return BOF4_ERR_WORKSPACE;
