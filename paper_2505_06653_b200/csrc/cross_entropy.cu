@@ -405,7 +405,12 @@ namespace {
 // Whether the vocabulary is taken in pieces.  Both forms, us, decoding as it multiplies against this: with the gradient 16000 x 4096 by 256 125 against 123, 32000 x 4096 by 257
 // 278 against 274, 512 379 against 285, 128256 x 4096 by 257 1046 against 1083, 384 1331 against 1165, 128256 x 8192 by 257 2242 against 1926; without it 32000 x 4096 by 384
 // 173 against 182, 448 194 against 195, 512 239 against 178, 50000 x 4096 by 384 243 against 249, 448 270 against 251.
-bool loss_dense(int64_t tokens, bool grad) { return tokens > (grad ? 256 : 384); }
+// With few columns sooner: 60000 x 512 by 130 without the gradient 83 against 62, with it by 200 198 against 171; x 1088 by 130 93 against 83, with it by 200 209 against 204; x 2048 by
+// 200 134 against 132, with it by 256 270 against 255.
+bool loss_dense(int64_t cols, int64_t tokens, bool grad)
+{
+    return tokens > (cols <= 1088 && !grad ? 128 : cols <= 2048 ? 192 : grad ? 256 : 384);
+}
 
 struct LossPlan {
     bool dense;
@@ -417,7 +422,7 @@ struct LossPlan {
 };
 bool loss_plan(int64_t rows, int64_t cols, int64_t tokens, bool grad, int64_t capacity, LossPlan* p)
 {
-    p->dense = loss_dense(tokens, grad);
+    p->dense = loss_dense(cols, tokens, grad);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;

@@ -144,14 +144,16 @@ namespace {
 
 // Whether a matrix is decoded once and multiplied as plain bf16.  Both forms, us, ffn x columns by tokens, decoding as it multiplies against this:
 //   forward    2048 x 2048 by 257 28 against 28, 512 34 against 28; 4096 x 2048 by 512 39 against 32; 8192 x 4096 by 512 80 against 85, 768 105 against 103;
-//              11008 x 4096 by 512 104 against 118, 768 139 against 140, 1024 185 against 167; 28672 x 8192 by 896 768 against 814, 1024 841 against 827
+//              11008 x 4096 by 512 104 against 118, 768 139 against 140, 1024 185 against 167; 28672 x 8192 by 896 768 against 814, 1024 841 against 827;
+//              with few columns its results take longer than its products: 24184 x 832 (z kept) by 200 72 against 55, 450 147 against 82, x 2048 by 256 98 against 104, 300
+//              139 against 131, 600 243 against 156, x 2560 by 300 152 against 160, 450 195 against 165; 8000 x 1088 by 200 27 against 27, 256 29 against 27
 //   backward   2048 x 2048 by 448 42 against 40; 4096 x 4096 by 512 63 against 60; 8192 x 4096 by 768 118 against 128; 11008 x 4096 by 768 165 against 175,
 //              1024 218 against 194; 28672 x 8192, where the parts of a tile are many, by 384 509 against 544, 512 621 against 556, 1024 1328 against 902
 bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
 {
     const int64_t n = rows * cols;
     if (backward) return tokens >= (n <= (int64_t)1 << 25 || n >= (int64_t)1 << 28 ? 448 : 896);
-    return tokens >= (n <= (int64_t)1 << 24 ? 257 : 768);
+    return tokens >= 768 || (tokens > 384 && cols <= 2560) || (tokens > 256 && (cols <= 2048 || n <= (int64_t)1 << 24)) || (tokens > 160 && cols <= 1088);
 }
 
 // Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.

@@ -82,7 +82,9 @@ def targets_of(tokens, rows, seed, ignored=0.2):
 SHAPES = [(1, 1, 32, 32), (1, 1000, 64, 64), (2, 2049, 256, 64), (7, 333, 4096, 128), (13, 5000, 1024, 1024), (17, 127, 320, 64), (40, 2048, 64, 32), (130, 16385, 96, 32),
           (300, 700, 512, 256), (511, 999, 64, 64), (512, 1000, 96, 32), (513, 16385, 128, 64), (700, 1, 64, 64), (1000, 300, 2080, 32), (1537, 33000, 64, 64),
           (600, 63, 256, 64), (2049, 1025, 512, 64), (1000, 3000, 4096, 64),
-          (14, 16400, 4096, 64)]
+          (14, 16400, 4096, 64),
+          # more than 64 tokens of the form that decodes as it multiplies
+          (130, 600, 2080, 32), (250, 300, 2304, 64)]
 
 
 @pytest.mark.parametrize("tokens,rows,cols,block", SHAPES)

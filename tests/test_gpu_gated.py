@@ -33,7 +33,7 @@ SHAPES = [(1, 32, 64, 64), (1, 5, 32, 32), (2, 65, 256, 64), (5, 200, 4096, 128)
           # a large matrix by more than twelve tokens
           (14, 8200, 4096, 64),
           # several tiles of tokens of the form that decodes as it multiplies
-          (300, 2100, 4096, 64), (600, 4200, 4096, 64)]
+          (200, 300, 1280, 64), (300, 2100, 4096, 64), (600, 4200, 4096, 64)]
 
 
 @pytest.mark.parametrize("tokens,ffn,cols,block", SHAPES)
