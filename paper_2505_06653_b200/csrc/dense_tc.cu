@@ -32,7 +32,7 @@ namespace bof4 {
 
 constexpr int kDnM = 256, kDnN = 256, kDnK = 64;
 template <int USE>
-constexpr int dn_stages = USE == kDenseGated ? 6 : 7;  // (the gated block's results need room of their own, and six are as fast)
+constexpr int dn_stages = USE == kDenseGatedRows ? 6 : 7;  // (results that go through shared memory need room of their own)
 constexpr int kDnHalf = 128 * kDnK * 2;         // an SM's part of an operand in a stage
 constexpr int kDnStage = 2 * kDnHalf;
 constexpr int kDnSmem = 7 * kDnStage + 1024;
@@ -213,30 +213,36 @@ __device__ __forceinline__ void dn_rows(uint32_t block, const uint32_t (&w)[8], 
 }
 // Sixteen values of each lane's row: from the lanes where rows begin at multiples of 32 bytes, through shared memory elsewhere (1022 tokens by 1088 columns, z kept:
 // 13376 columns of the result 67 us from the lanes and 77 through shared memory, 13384 95 and 76, 13382 206 and 84).
+template <bool ROWS>
 __device__ __forceinline__ void dn_put16(uint32_t block, uint16_t* p, const float* v, bool live, int count, int align, int lane)
 {
-    if (align >= 32) {
-        if (live) dn_store16(p, v, count, align);
-        return;
-    }
-    uint32_t w[8];
+    if constexpr (ROWS) {
+        if (align < 32) {
+            uint32_t w[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
-    dn_rows(block, w, p, live, count, lane);
+            for (int k = 0; k < 8; ++k) w[k] = bf16_pair(v[2 * k], v[2 * k + 1]);
+            dn_rows(block, w, p, live, count, lane);
+            return;
+        }
+    }
+    if (live) dn_store16(p, v, count, 32);
 }
+template <bool ROWS>
 __device__ __forceinline__ void dn_put16(uint32_t block, float* p, const float* v, bool live, int count, int align, int lane)
 {
-    if (align >= 32) {
-        if (live) dn_store16(p, v, count);
-        return;
-    }
+    if constexpr (ROWS) {
+        if (align < 32) {
 #pragma unroll
-    for (int h = 0; h < 16; h += 8) {
-        uint32_t w[8];
+            for (int h = 0; h < 16; h += 8) {
+                uint32_t w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[h + k]);
-        dn_rows(block, w, p + h, live, count - h, lane);
+                for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[h + k]);
+                dn_rows(block, w, p + h, live, count - h, lane);
+            }
+            return;
+        }
     }
+    if (live) dn_store16(p, v, count);
 }
 
 // What is known of a token before its sums are.
@@ -257,7 +263,9 @@ __device__ __forceinline__ DenseToken dn_token(const DenseOut& out, int64_t t)
     return k;
 }
 
-// A token's sums of columns o0 ... o0 + 63 of z, gate and up in turn: columns o0 / 2 ... of y.  (All lanes of the warp take part.)
+// A token's sums of columns o0 ... o0 + 63 of z, gate and up in turn: columns o0 / 2 ... of y.  (All lanes of the warp take part.)  ROWS: some rows begin at odd places;
+// with the code and the room for them in every launch, 4096 tokens of 28672 x 4096 took 776 us, 745 without.
+template <bool ROWS>
 __device__ __forceinline__ void dn_gated(const DenseOut& out, float (&z)[kDnCols], int64_t t, int64_t o0, uint32_t block, int lane)
 {
     const int64_t f0 = o0 >> 1;
@@ -284,15 +292,15 @@ __device__ __forceinline__ void dn_gated(const DenseOut& out, float (&z)[kDnCols
         for (int k = 0; k < 16; ++k) g[k] = z[32 * c + 2 * k], u[k] = z[32 * c + 2 * k + 1];
         if (out.pre) {
             uint16_t* const p = out.pre + t * out.ld_pre + f0 + 16 * c;
-            dn_put16(block, p, g, live, count, out.pre_align, lane);
-            dn_put16(block, p + out.n, u, live, count, out.pre_align, lane);
+            dn_put16<ROWS>(block, p, g, live, count, out.pre_align, lane);
+            dn_put16<ROWS>(block, p + out.n, u, live, count, out.pre_align, lane);
         }
         activate_gate(g, out.act);
 #pragma unroll
         for (int k = 0; k < 16; ++k) g[k] *= u[k];
         const int64_t at = t * out.ldy + f0 + 16 * c;
-        if (out.y_bf16) dn_put16(block, static_cast<uint16_t*>(out.y) + at, g, live, count, out.align, lane);
-        else dn_put16(block, static_cast<float*>(out.y) + at, g, live, count, out.align, lane);
+        if (out.y_bf16) dn_put16<ROWS>(block, static_cast<uint16_t*>(out.y) + at, g, live, count, out.align, lane);
+        else dn_put16<ROWS>(block, static_cast<float*>(out.y) + at, g, live, count, out.align, lane);
     }
 }
 
@@ -368,6 +376,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
              const DenseWork work, unsigned long long* __restrict__ tickets, float* __restrict__ parts)
 {
     constexpr int kDnStages = dn_stages<USE>;
+    constexpr bool kGated = USE == kDenseGated || USE == kDenseGatedRows;
     extern __shared__ unsigned char s_dyn[];
     __shared__ __align__(8) unsigned long long s_full[kDnStages], s_empty[kDnStages], s_acc_full[2], s_acc_empty[2];
     __shared__ uint32_t s_tmem;
@@ -413,7 +422,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(&s_full[stage])), "r"(2 * kDnStage) : "memory");
                     const uint32_t bar = dn_first_sm(smem_u32(&s_full[stage])), at = ring + (uint32_t)stage * kDnStage;
                     dn_load2(at, &a_map, bar, k * kDnK, t0);
-                    if (USE == kDenseGated) {
+                    if (kGated) {
                         dn_load3(at + kDnHalf, &b_map, bar, k * kDnK, 0, o0 >> 1);
                     } else if (NMAJOR) {
                         dn_load2(at + kDnHalf, &b_map, bar, o0, k * kDnK);
@@ -478,7 +487,7 @@ dense_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         int seg = 0;
         bool ok = true;
         auto finish = [&](float (&sums)[kDnCols], const DenseToken& token, int64_t t, int64_t o0) {
-            if (USE == kDenseGated) dn_gated(out, sums, t, o0, ring + (uint32_t)(kDnStages * kDnStage + warp * kDnBlock), lane);
+            if (kGated) dn_gated<USE == kDenseGatedRows>(out, sums, t, o0, ring + (uint32_t)(kDnStages * kDnStage + warp * kDnBlock), lane);
             else dn_finish<USE>(out, token, sums, t, o0);
         };
         while (ok && walk.step(work)) {
@@ -630,7 +639,9 @@ int dense_product(const char* who, const DenseProduct& q, const DenseOut& out, i
         launch_after(kern, 2 * p.work.clusters, kDnThreads, kDnSmem, st, a_map, b_map, out, status, p.work,                                \
                      reinterpret_cast<unsigned long long*>(base), reinterpret_cast<float*>(base + p.parts));                               \
     }
-    if (q.use == kDenseGated) BOF4_DN_GO(kDenseGated, false)
+    const bool rows = q.use == kDenseGated && (out.align < 32 || (out.pre && out.pre_align < 32));
+    if (rows) BOF4_DN_GO(kDenseGatedRows, false)
+    else if (q.use == kDenseGated) BOF4_DN_GO(kDenseGated, false)
     else if (q.use == kDenseLoss) BOF4_DN_GO(kDenseLoss, false)
     else if (q.use == kDenseAdd) BOF4_DN_GO(kDenseAdd, true)
     else BOF4_DN_GO(kDenseStore, true)

@@ -11,6 +11,7 @@ namespace bof4 {
 enum DenseUse {
     kDenseStore,  // y[t, o] = z, bf16
     kDenseGated,  // y[t, f] = act(z[t, gate f]) * z[t, up f]; gate and up rows of B in turn
+    kDenseGatedRows,  // the same where rows of y or pre do not begin at multiples of 32 bytes (chosen by dense_product)
     kDenseLoss,   // exponentials of logits against a reference per token, and their sums (cross_entropy.cu)
     kDenseAdd     // y[t, o] = y[t, o] * factor[t] + z, fp32
 };
