@@ -7,8 +7,8 @@
 // loss = log(1 + S e^-a) and p_y - 1 = -S / (S + e^a), so that nothing cancels where the target has next to all of the probability.
 //
 // Few tokens: the logits of all rows (fp32) fit a workspace; the products are those of bof4_linear and its backward pass, which decode as
-// they multiply.  Two kernels between them: sums of 2048 logits each, and dz in bf16, in units of g (1 - p_y): the target's entry, often the
-// largest by far, is -1 and needs no rounding, and the second product's results are multiplied by the unit.
+// they multiply.  Between them one kernel, a CTA per row of up to 16384 logits, or two, for sums of 2048 logits each and for dz.  dz is in bf16, in units
+// of g (1 - p_y): the target's entry, often the largest by far, is -1 and needs no rounding, and the second product's results are multiplied by the unit.
 //
 // Many tokens: the vocabulary in pieces of at most 32768 rows, so that neither logits nor a decoded matrix is kept.  A piece is
 // decoded once and multiplied twice (dense_tc.cu): the first product's results become E = exp(z - r) in bf16 and its sums in the

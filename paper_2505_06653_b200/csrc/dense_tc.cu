@@ -4,7 +4,7 @@
 // plain bf16.  Two SMs (a cluster) share a tile of 256 tokens by 256 columns: tcgen05.mma with cta_group::2 and M = 256, each SM
 // holding the rows of 128 tokens and half of the columns' rows.  So a k-block of 64 takes 32 KiB of each SM's shared memory
 // in and out, 512 of the 128-byte cycles of its data path, as long as the products themselves take (a tile of 128 x 256
-// of one SM takes 768: linear_tc.cu).
+// of one SM takes 768: linear_tc.cuh).
 //
 //   1 loads    TMA loads of both operands, six or seven stages; those of both SMs complete the first SM's barrier
 //   1 issuer   in the first SM: four instructions (K = 16) per k-block

@@ -5,7 +5,7 @@
 //   backward  dz[t, f] = dh[t, f] z[t, F + f] act'(z[t, f]),   dz[t, F + f] = dh[t, f] act(z[t, f]),   dx = dz W
 //
 // The products are those of bof4_linear with gate and up rows in turn, so that a tile has both sums of a column of h: the form
-// for few tokens (linear_few.cu), the one that decodes as it multiplies (linear_tc.cu), and, for many tokens, a decoded matrix and
+// for few tokens (linear_few.cu), the one that decodes as it multiplies (linear_tc.cuh), and, for many tokens, a decoded matrix and
 // a product of plain operands (dense_tc.cu).  z itself is written where a backward pass will want it and never read here.
 // The backward product is that of bof4_linear_backward over all 2 F rows at once.
 #include <type_traits>

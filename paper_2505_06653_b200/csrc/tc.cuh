@@ -1,4 +1,4 @@
-// Pieces shared by the kernels that multiply on the tensor cores (gemm_tc.cu, linear_tc.cu): matrix descriptors, bounded
+// Pieces shared by the kernels that multiply on the tensor cores (gemm_tc.cu, linear_tc.cuh, dense_tc.cu): matrix descriptors, bounded
 // waits, TMA loads, tensor-memory reads, tickets of cut tiles.
 #pragma once
 
