@@ -486,8 +486,9 @@ BOF4_API size_t bof4_gated_workspace_bytes(int64_t ffn, int64_t cols, int64_t n_
  *   dx[t] = dloss[t] * (sum_v exp(z[t, v] - lse[t]) W^[v] - W^[targets[t]])
  * W is rows x cols (rows: the vocabulary) as for bof4_linear; W^, products and sums of z as there.  exp and the sums over v are fp32;
  * the second product takes the probabilities rounded to bf16 and adds them up in fp32, dx is rounded once.  The target's own
- * probability enters neither sum, so a loss near zero and its gradient keep their relative precision.  What is not finite among a token's
- * logits makes that token's results not finite, others' not.
+ * probability enters neither sum, so a loss near zero and its gradient keep their relative precision.  A logit of +inf or NaN, the
+ * target's own included, makes the token's loss, lse and dx not finite; one of -inf is a probability of zero (a target's: a loss of +inf; the weight
+ * that is not finite still makes its column of dx so).  Other tokens' results do not change.
  *   d_targets   device, int64 [n_tokens].  A negative target is ignored: loss 0, dx 0 (lse is still written).  One of `rows` or more
  *               is treated the same way and sets *d_status to 2
  *   d_dloss     device, fp32 [n_tokens]: the gradient of the whole with respect to loss[t] (1 / count for a mean); NULL: ones

@@ -42,11 +42,13 @@ __device__ __forceinline__ CeToken ce_token(float r, float s, float own, bool co
     // The others against the target.  Few tokens have r for the largest of the others, so that odds below one mean a > 0; with many tokens r may lie 24 above all of them, and
     // then log(s + e^a) - a would cancel where a < 0 as well.  (Odds of no use, or infinite, where a is far below zero: s is e^-24 at least.)
     const float a = own - r, down = expf(-a), odds = s * down;
+    const float none = own - own;  // zero, or NaN where the target's logit is not finite: infinity less infinity, as the loss is
     if (s == 0.0f) {  // nothing but the target
-        c.lse = own, c.loss = own - own, c.scale = 0.0f, c.rest = 0.0f;
+        c.lse = own, c.loss = c.rest = none, c.scale = 0.0f;
     } else if (a > 0.0f || odds <= 1.0f) {
         const float total = 1.0f + odds;
-        c.loss = log1pf(odds), c.lse = own + c.loss, c.scale = down / total, c.rest = odds / total;
+        const float more = log1pf(odds);
+        c.loss = more + none, c.lse = own + more, c.scale = down / total, c.rest = odds / total + none;
     } else {
         const float total = s + expf(a);
         c.lse = r + logf(total), c.loss = logf(total) - a, c.scale = 1.0f / total, c.rest = s / total;
