@@ -217,6 +217,8 @@ struct LinearOut {
         pairs = (a & 3u) == 0 && (l & 1) == 0;
         wide = (a & 15u) == 0 && (l & 7) == 0;
     }
+    // A scale of zero is an ignored token's: nothing of its sums is wanted, whatever weights that are not finite have made of them.
+    static __device__ __forceinline__ float scaled(float sum, float f) { return f == 0.0f ? 0.0f : sum * f; }
     __device__ __forceinline__ float bias_at(int64_t o) const
     {
         if (!bias) return 0.0f;

@@ -117,7 +117,7 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, in
     lt_sums(src, accs, z);
     if (SCALED && out.scale) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) z[k] *= k < count ? __ldg(out.scale + t0 + k) : 0.0f;
+        for (int k = 0; k < 16; ++k) z[k] = out.scaled(z[k], k < count ? __ldg(out.scale + t0 + k) : 0.0f);
     }
     const bool odd = lane & 1, both = (o | 1) < out.n, one = (o & ~(int64_t)1) < out.n;  // the pair's two rows exist, its first
     const bool paired = out.y_bf16 && out.pairs && count >= 16;
@@ -586,7 +586,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                     const int64_t o = o0 + (e & 31) * 4;
                     if (BWD && out.scale && e < count * (kLtM / 4)) {
                         const float f = __ldg(out.scale + token0 + (e >> 5));
-                        sum[u].x *= f, sum[u].y *= f, sum[u].z *= f, sum[u].w *= f;
+                        sum[u] = make_float4(out.scaled(sum[u].x, f), out.scaled(sum[u].y, f), out.scaled(sum[u].z, f), out.scaled(sum[u].w, f));
                     }
                     if (e < count * (kLtM / 4) && o < out.n) four[u].store(out, sum[u], token0 + (e >> 5), o);
                 }

@@ -91,3 +91,29 @@ def test_infinite_logits(bof4, tokens, rows, kind):  # noqa: F811
                 assert not bool(dx[0::3].isfinite().any()) and not bool(dx[2::3].isfinite().any())
                 if kind == "outlier":  # (other columns have no weights but zeros)
                     assert not bool(dx[1::3, 0].isfinite().any()) and not bool(dx[1::3, 1:].any())
+
+
+@pytest.mark.parametrize("tokens,rows", [(5, 300), (40, 300), (130, 300), (7, 20000), (40, 20000), (600, 300), (600, 40000)])
+@pytest.mark.parametrize("kind", ["outlier", "constant", "nan"])
+def test_ignored_tokens_beside_weights_that_are_not_finite(bof4, tokens, rows, kind):  # noqa: F811
+    """Loss 0 and dx 0 whatever the weights are."""
+    args, kw, _ = with_infinite_weight(bof4, tokens, rows, rows // 2, "outlier" if kind == "outlier" else "constant")
+    if kind == "nan":
+        args[1][5] = float("nan")
+    targets = torch.arange(tokens, device="cuda") % 200
+    targets[::2], targets[-1] = -100, rows
+    ignored = (targets < 0) | (targets >= rows)
+    for dloss in (None, torch.linspace(-2, 3, tokens, device="cuda")):
+        loss, _, dx, status = bof4.bof4_cross_entropy(*args, targets, dloss=dloss, want_dx=True, **kw)
+        assert int(status.item()) == 2
+        assert not bool(loss[ignored].any()) and not bool(dx[ignored].any())
+
+
+@pytest.mark.parametrize("tokens", [20, 130, 190])
+def test_ignored_tokens_in_cut_tiles(bof4, tokens):  # noqa: F811
+    """The same where the second product's tiles are cut along K (the vocabulary)."""
+    args, kw, _ = with_infinite_weight(bof4, tokens, 30000, 29000, "constant")
+    targets = torch.full((tokens,), -1, device="cuda")
+    targets[5::7] = 3
+    loss, _, dx, status = bof4.bof4_cross_entropy(*args, targets, want_dx=True, **kw)
+    assert int(status.item()) == 0 and not bool(loss[targets < 0].any()) and not bool(dx[targets < 0].any())
