@@ -138,7 +138,7 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
         BOF4_CUDA_TRY(cudaGetLastError());
     }
     const LtLaunch go{&code_map, &token_map, &w, &out, status, heads, nodes, &p.work, p.ctas, base, reinterpret_cast<float*>(base + p.parts), st};
-    if ((rc = backward ? linear_tc_backward(go) : out.gated ? linear_tc_gated(go) : linear_tc_forward(go))) return rc;
+    if ((rc = backward ? (out.scale ? linear_tc_scaled(go) : linear_tc_backward(go)) : out.gated ? linear_tc_gated(go) : linear_tc_forward(go))) return rc;
     BOF4_CUDA_TRY(cudaGetLastError());
     return BOF4_OK;
 }
