@@ -109,8 +109,10 @@ __device__ __forceinline__ void activate_slopes(float (&g)[N], const float (&z)[
     }
 }
 
-// act(z) for the gated block: the logistic forms with half of the instructions, within (2 + 1.5 |z|) units in the last place.  (Its results' warps are waited
-// for at the end of a launch: 256 tokens of 11008 x 4096 took 78 us with the rounded quotient and exponential.)
+// act(z) for the gated block: the logistic forms with half of the instructions, within 2^-20 |z| (the argument is beside test_activations_at_every_value).  Relative to the result,
+// which falls off like e^v with v the exponential's argument, that is a precision that falls with |v|: the exponential is off by 2 + 1.2 |v| units and, in the tanh form, v itself by up
+// to two, which is |v| times as many of the result's; where e^-v is above 2^126 the quotient is zero.  (Its results' warps are waited for at the end of a launch: 256 tokens of 11008 x 4096 took 78 us
+// with the rounded quotient and exponential.)
 template <int N>
 __device__ __forceinline__ void activate_gate(float (&z)[N], int act)
 {
