@@ -467,7 +467,8 @@ BOF4_API int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scale_
  *   d_pre     device, bf16, z as bof4_gated left it, token t at t * ld_pre
  *   d_dx      device, out, bf16, token t at t * ld_dx, or NULL: not wanted
  *   d_dbias   device, out, fp32 [2 * ffn], or NULL
- *   d_ws      device workspace of bof4_gated_workspace_bytes(ffn, cols, n_tokens, 1, capacity) bytes, as for bof4_gated
+ *   d_ws      device workspace of bof4_gated_workspace_bytes(ffn, cols, n_tokens, 1, capacity) bytes, as for bof4_gated; without d_dx
+ *             cols = 0 says how many are needed
  */
 BOF4_API int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t ffn, int64_t cols, int block_size,
                                  const float* d_codebook, const void* d_dh, int dh_dtype, int64_t ld_dh, int64_t n_tokens, const void* d_pre,

@@ -148,7 +148,10 @@ namespace {
 //              with few columns its results take longer than its products: 24184 x 832 (z kept) by 200 72 against 55, 450 147 against 82, x 2048 by 256 98 against 104, 300
 //              139 against 131, 600 243 against 156, x 2560 by 300 152 against 160, 450 195 against 165; 8000 x 1088 by 200 27 against 27, 256 29 against 27
 //   backward   2048 x 2048 by 448 42 against 40; 4096 x 4096 by 512 63 against 60; 8192 x 4096 by 768 118 against 128; 11008 x 4096 by 768 165 against 175,
-//              1024 218 against 194; 28672 x 8192, where the parts of a tile are many, by 384 509 against 544, 512 621 against 556, 1024 1328 against 902
+//              1024 218 against 194; 28672 x 8192, where the parts of a tile are many, by 384 509 against 544, 448 561 against 560, 512 621 against 556, 1024 1328 against 902
+//   between and beside them, in a graph on one box: backward 14336 x 4096 by 640 174 against 204, 768 193 against 208, 896 265 against 224, 14336 x 8192 by 448 255 against 274, 640 367
+//              against 345, 896 527 against 456; forward 14336 x 4096 by 512 143 against 157, 640 191 against 174, 28672 x 8192 by 768 613 against 697, 896 777 against 812.  So the one
+//              limit of the forward form costs 9 % at the first of these two shapes and 13 % at the second, next to it, the backward limits 6 % at 14336 x 8192
 bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
 {
     const int64_t n = rows * cols;
@@ -156,7 +159,7 @@ bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
     return tokens >= 768 || (tokens > 384 && cols <= 2560) || (tokens > 256 && (cols <= 2048 || n <= (int64_t)1 << 24)) || (tokens > 160 && cols <= 1088);
 }
 
-// Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.
+// Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.  (cols = 0: no product, and dz is not kept.)
 struct GatedPlan {
     bool dense;
     int per;  // tokens of a CTA that forms dz: fewer where there would be less than four CTAs an SM (131 tokens of 11008: 15 us with 32)
@@ -182,7 +185,7 @@ bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_
     p->ld = (rows + 7) & ~(int64_t)7;
     p->w = up256(p->product);
     p->dz = p->w + (p->dense ? up256((size_t)rows * cols * 2) : 0);
-    p->sums = p->dz + (backward ? up256((size_t)tokens * p->ld * 2) : 0);
+    p->sums = p->dz + (backward && cols ? up256((size_t)tokens * p->ld * 2) : 0);
     p->total = p->sums + (backward && p->chunks > 1 ? up256((size_t)p->chunks * rows * 4) : 0);
     return true;
 }
@@ -336,7 +339,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     }
     GatedPlan p{};
     const int col_blocks = (int)((ffn + kDzCols - 1) / kDzCols);
-    if (!nothing && (!gated_plan(ffn, cols, n_tokens, true, w.capacity, &p) || p.chunks * col_blocks > INT32_MAX)) {
+    if (!nothing && (!gated_plan(ffn, product ? cols : 0, n_tokens, true, w.capacity, &p) || p.chunks * col_blocks > INT32_MAX)) {
         set_error("%s: matrix or batch too large", fn);
         return BOF4_ERR_SHAPE;
     }

@@ -654,7 +654,7 @@ PyObject* gated_backward(PyObject* const* a)
     const size_t i_db = k;
     if (want_db) spec[k++] = {2 * ffn, at::kFloat};
     const size_t i_ws = k;
-    if (none(a[13])) spec[k++] = {(int64_t)bof4_gated_workspace_bytes(ffn, cols, n, 1, o.idx ? o.cap : 0), at::kByte};
+    if (none(a[13])) spec[k++] = {(int64_t)bof4_gated_workspace_bytes(ffn, want_dx ? cols : 0, n, 1, o.idx ? o.cap : 0), at::kByte};
     else ws = given_workspace(a[13], d);
     const size_t i_dx = k;
     if (want_dx && !out) spec[k++] = {n * cols, at::kBFloat16};
