@@ -408,7 +408,7 @@ namespace {
 
 // Whether the vocabulary is taken in pieces.  Both forms, us, decoding as it multiplies against this: with the gradient 16000 x 4096 by 256 125 against 123, 32000 x 4096 by 257
 // 278 against 274, 512 379 against 285, 128256 x 4096 by 257 1046 against 1083, 384 1331 against 1165, 128256 x 8192 by 257 2242 against 1926; without it 32000 x 4096 by 384
-// 173 against 182, 448 194 against 195, 512 239 against 178, 50000 x 4096 by 384 243 against 249, 448 270 against 251.
+// 173 against 182, 448 194 against 195, 512 239 against 178, 50000 x 4096 by 384 243 against 249, 448 270 against 251, 128256 x 4096 by 385 589 against 643, 448 668 against 655.
 // With few columns sooner: 60000 x 512 by 130 without the gradient 83 against 62, with it by 200 198 against 171; x 1088 by 130 93 against 83, with it by 200 209 against 204; x 2048 by
 // 200 134 against 132, with it by 256 270 against 255.
 bool loss_dense(int64_t cols, int64_t tokens, bool grad)

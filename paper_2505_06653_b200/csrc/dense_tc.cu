@@ -19,6 +19,7 @@
 // What bounds it: with all SMs at work the power limit, 1.55 to 1.63 PFLOP/s in a cold launch (28672 x 4096 by 4096 tokens 622 us, tensor cores busy 81 to 86 % of the time at
 // 1024 tokens), 1.2 to 1.3 in a row of calls; with 48 of the 74 pairs at work a k-block takes the 512 cycles that it has to.  A lane has a token's results, so that each store
 // of a warp goes to 32 rows: whole sectors of 32 bytes instead of halves took a gated block of 4096 tokens from 847 to 760 us, a loss with its gradient from 7.3 to 7.0 ms.
+// 18 warps have 96 registers a thread: the products that store or add spill 16 and 24 bytes, the logits 36, the gated ones 236 and (rows at odd places) 324 where they finish a tile.
 //
 // Tiles go to the clusters in turn.  What is left after the last whole round is cut along K into as many parts as there are clusters for
 // (74 / tiles, at most eight) where K is long enough to pay for it.  They come first; the sums of a

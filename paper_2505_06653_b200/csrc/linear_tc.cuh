@@ -39,8 +39,8 @@
 // k-block with shared memory and the integer pipe at 68 % each; at 256 tokens the data path of shared memory, through which both
 // operands go in and out: 832 cycles per k-block, of which the tensor cores need 512.  28672 x 8192: 24 tokens 84 us, 64 89, 128
 // 100, 256 123, 2048 870 (1107 TFLOP/s; the power limit holds the clock down).  Two SMs on one tile (cta_group::2, each decoding
-// half of it) took 1.7 times as long: the producers of both wait for one another at every stage.  24 warps leave a thread 80 registers, of which
-// every instantiation spills 5 to 11.
+// half of it) took 1.7 times as long: the producers of both wait for one another at every stage.  24 warps leave a thread 80 registers; every
+// instantiation spills 5 to 11 more, the gated ones 12 to 15.
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
 #pragma once
