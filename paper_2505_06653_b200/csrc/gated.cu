@@ -152,11 +152,13 @@ namespace {
 //   between and beside them, in a graph on one box: backward 14336 x 4096 by 640 174 against 204, 768 193 against 208, 896 265 against 224, 14336 x 8192 by 448 255 against 274, 640 367
 //              against 345, 896 527 against 456; forward 14336 x 4096 by 512 143 against 157, 640 191 against 174, 28672 x 8192 by 768 613 against 697, 896 777 against 812.  So the one
 //              limit of the forward form costs 9 % at the first of these two shapes and 13 % at the second, next to it, the backward limits 6 % at 14336 x 8192
-bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward)
+//   h in fp32  whose sums have an accumulator per 1024 of K (linear_tc.cuh): 22016 x 4096 by 257 94 against 110, 384 108 against 112, 512 131 against 112, 767 194 against 135; 57344 x 8192 by
+//              384 511 against 520, 512 672 against 536; 11264 x 2048 by 512 53 against 40
+bool gated_dense(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp32)
 {
     const int64_t n = rows * cols;
     if (backward) return tokens >= (n <= (int64_t)1 << 25 || n >= (int64_t)1 << 28 ? 448 : 896);
-    return tokens >= 768 || (tokens > 384 && cols <= 2560) || (tokens > 256 && (cols <= 2048 || n <= (int64_t)1 << 24)) || (tokens > 160 && cols <= 1088);
+    return tokens >= 768 || (tokens > 384 && (cols <= 2560 || fp32)) || (tokens > 256 && (cols <= 2048 || n <= (int64_t)1 << 24)) || (tokens > 160 && cols <= 1088);
 }
 
 // Parts of the workspace behind the product's: the decoded matrix, dz, the sums of dz.  (cols = 0: no product, and dz is not kept.)
@@ -167,10 +169,10 @@ struct GatedPlan {
     size_t product, w, dz, sums, total;
 };
 // False: too large.
-bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, int64_t capacity, GatedPlan* p)
+bool gated_plan(int64_t ffn, int64_t cols, int64_t tokens, bool backward, bool fp32, int64_t capacity, GatedPlan* p)
 {
     const int64_t rows = 2 * ffn;
-    p->dense = gated_dense(rows, cols, tokens, backward);
+    p->dense = gated_dense(rows, cols, tokens, backward, fp32);
     p->product = 256;
     if (cols) {
         if (p->dense) p->product = backward ? dense_ws_bytes(tokens, cols, rows) : dense_ws_bytes(tokens, rows, cols);
@@ -206,8 +208,9 @@ extern "C" size_t bof4_gated_workspace_bytes(int64_t ffn, int64_t cols, int64_t 
     if (ffn < 0 || cols < 0 || n_tokens < 0 || capacity < 0 || ffn > INT32_MAX / 2 || cols > INT32_MAX || n_tokens > INT32_MAX || capacity > INT32_MAX)
         return 0;
     if (ffn == 0 || n_tokens == 0) return 256;
-    GatedPlan p;
-    return gated_plan(ffn, cols, n_tokens, backward != 0, capacity, &p) ? p.total : 0;
+    GatedPlan p, q;  // for results in bf16 and in fp32
+    if (!gated_plan(ffn, cols, n_tokens, backward != 0, false, capacity, &p) || !gated_plan(ffn, cols, n_tokens, backward != 0, true, capacity, &q)) return 0;
+    return p.total > q.total ? p.total : q.total;
 }
 
 extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scale_dtype, int64_t ffn, int64_t cols, int block_size,
@@ -270,7 +273,7 @@ extern "C" int bof4_gated(const uint8_t* d_codes, const void* d_scales, int scal
         return BOF4_ERR_INVALID_ARG;
     }
     GatedPlan p;
-    if (!gated_plan(ffn, cols, n_tokens, false, w.capacity, &p)) {
+    if (!gated_plan(ffn, cols, n_tokens, false, h_dtype == BOF4_F32, w.capacity, &p)) {
         set_error("%s: matrix or batch too large", fn);
         return BOF4_ERR_SHAPE;
     }
@@ -339,7 +342,7 @@ extern "C" int bof4_gated_backward(const uint8_t* d_codes, const void* d_scales,
     }
     GatedPlan p{};
     const int col_blocks = (int)((ffn + kDzCols - 1) / kDzCols);
-    if (!nothing && (!gated_plan(ffn, product ? cols : 0, n_tokens, true, w.capacity, &p) || p.chunks * col_blocks > INT32_MAX)) {
+    if (!nothing && (!gated_plan(ffn, product ? cols : 0, n_tokens, true, false, w.capacity, &p) || p.chunks * col_blocks > INT32_MAX)) {
         set_error("%s: matrix or batch too large", fn);
         return BOF4_ERR_SHAPE;
     }

@@ -48,6 +48,7 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp3
     // result (2-norms) after K = 4096, 7e-6 after 8192.  That is nothing beside a rounding to bf16 (1.7e-3).  Results in fp32 with
     // a longer K have tiles of at most 128 tokens, which leave room for two accumulators that each take half of the steps (tiles
     // of 64 have four): 3.7e-6 at K = 8192, at 1.5 times the time (2048 tokens, 14336 rows: 660 us, 438 with tiles of 256).
+    // Those of a gated block, and logits, go further (`segments` below).
     const int64_t widest = fp32 && k > kLtLongK ? 128 : kLtMaxN, most_n = (tokens + widest - 1) / widest;
     // the tokens are dealt evenly over the tiles, in multiples of 16
     const int64_t box = ((tokens + most_n - 1) / most_n + 15) & ~(int64_t)15, tiles_n = (tokens + box - 1) / box, tiles = tiles_m * tiles_n;
@@ -65,6 +66,11 @@ bool lt_plan(int64_t rows, int64_t cols, int64_t tokens, bool backward, bool fp3
     w.halves = (room - kLtGroups * stage) / kLtHalfBytes & ~1;
     if (w.halves > kLtMaxHalves) w.halves = kLtMaxHalves;
     w.accs = box <= 64 ? 4 : box <= 128 ? 2 : 1;
+    // Results in fp32 of a gated block, and logits: an accumulator takes at most 1024 of K, as in the form for many tokens (dense_tc.cu), and its sums are added in fp32: 0.7e-6
+    // whatever K is, where one accumulator left 3e-6 at K = 4096.  That is more for the warps of the results than a segment of 256 tokens has time for: logits of 128256 rows by 256
+    // tokens, K = 4096, 356 -> 383 us, gated 11008 x 4096 by 100 48.6 -> 51.6, by 256 62.7 -> 74.6.
+    const bool segments = few_parts && fp32 && !backward;
+    w.segment = segments ? kLtSegment * w.accs : (int)per_tile;
     // One CTA per SM, each with an equal part of the lines, but for few tiles of a long K: a tile is not cut into more than kLtMaxParts, which
     // one CTA adds up (128 x 256 sums in fp32 each).
     const int64_t lines = tiles * per_tile, most = tiles * kLtMaxParts;
@@ -138,7 +144,11 @@ int linear_tc(const char* who, const LinearW& w, bool backward, const void* oper
         BOF4_CUDA_TRY(cudaGetLastError());
     }
     const LtLaunch go{&code_map, &token_map, &w, &out, status, heads, nodes, &p.work, p.ctas, base, reinterpret_cast<float*>(base + p.parts), st};
-    if ((rc = backward ? (out.scale ? linear_tc_scaled(go) : linear_tc_backward(go)) : out.gated ? linear_tc_gated(go) : linear_tc_forward(go))) return rc;
+    const bool segments = p.work.segment < p.work.per_tile;
+    if (backward) rc = out.scale ? linear_tc_scaled(go) : linear_tc_backward(go);
+    else if (out.gated) rc = segments ? linear_tc_gated_segments(go) : linear_tc_gated(go);
+    else rc = segments ? linear_tc_forward_segments(go) : linear_tc_forward(go);
+    if (rc) return rc;
     BOF4_CUDA_TRY(cudaGetLastError());
     return BOF4_OK;
 }

@@ -40,7 +40,7 @@
 // operands go in and out: 832 cycles per k-block, of which the tensor cores need 512.  28672 x 8192: 24 tokens 84 us, 64 89, 128
 // 100, 256 123, 2048 870 (1107 TFLOP/s; the power limit holds the clock down).  Two SMs on one tile (cta_group::2, each decoding
 // half of it) took 1.7 times as long: the producers of both wait for one another at every stage.  24 warps leave a thread 80 registers; every
-// instantiation spills 5 to 11 more, the gated ones 12 to 15.
+// instantiation spills 5 to 11 more, the gated ones 12 to 15, those whose accumulators take segments 11 to 16.
 //
 // Every wait is bounded: a time-out sets the status word, everybody leaves, the kernel frees its tensor memory and returns.
 #pragma once
@@ -59,6 +59,7 @@ constexpr int kLtHalfBytes = 8192;           // half a line of codes: two k-bloc
 constexpr int kLtMaxHalves = 8;
 constexpr int kLtTableN = 64;                // tokens of a tile up to which there is room, and use, for the table of pairs
 constexpr int kLtLongK = 4096;               // K up to which results in fp32 have tiles of any width
+constexpr int kLtSegment = 4;                // lines of an accumulator's segment (1024 of K; accumulators that take turns: as many times more)
 constexpr int kLtMaxParts = 64;              // of a tile
 constexpr int kLtAhead = 6;                  // lines that L2 is asked for before the ring is
 constexpr int kLtSmem = 225 * 1024;          // stages and half lines, with slack to align them to 1024 bytes
@@ -71,6 +72,7 @@ struct LtWork {
     int k;                         // K
     int halves;                    // half lines of codes in the ring (even, at least four)
     int accs;                      // accumulators of a part of a tile, which the instructions of a k-block use in turn: 4, 2 or 1
+    int segment;                   // lines that an accumulator takes at most (SEGMENTS)
     int each, extra;               // lines per CTA, and the remainder
     bool table;                    // half of the codes go through a table
     unsigned long long epoch;
@@ -90,11 +92,77 @@ __device__ __forceinline__ void lt_load16(uint32_t addr, uint32_t (&v)[16])
           "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(addr));
 }
+__device__ __forceinline__ void lt_read16(uint32_t addr, uint32_t (&v)[16])  // with the wait, so that no sum can get between the two
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr)
+        : "memory");
+}
 
-// Sixteen columns of the warp's 32 rows, added over the accumulators in order.
+// Sums of the segments before, which a lane keeps in the part's slab.  Of a part that others will add to theirs, a lane's row goes to its place, column by column, and each segment is
+// added where it lies, without a wait for what is there (nobody else has the place until the part is finished).  Of a tile that the CTA has whole, a warp's four columns of its
+// 32 rows lie row by row instead, sixteen bytes a lane (`at`), and are read again with the last segment: columns q ... q + 31, `count` in all.
+__device__ __forceinline__ void lt_before(const float* at, int q, int count, float (&z)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (at && q + (j & 16) < count) v = __ldcg(reinterpret_cast<const float4*>(at + (q + j) * kLtM));
+        z[j] = v.x, z[j + 1] = v.y, z[j + 2] = v.z, z[j + 3] = v.w;
+    }
+}
+template <int N>
+__device__ __forceinline__ void lt_put(float* p, const float (&v)[N], bool whole, bool add)
+{
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            float* const to = p + j * kLtM;
+            if (add) asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(v[j]), "f"(v[j + 1]), "f"(v[j + 2]), "f"(v[j + 3]) : "memory");
+            else __stcg(reinterpret_cast<float4*>(to), make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (add) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p + j * kLtM), "f"(v[j]) : "memory");
+            else __stcg(p + j * kLtM, v[j]);
+        }
+    }
+}
+
+__device__ __forceinline__ void lt_read32(uint32_t addr, float (&v)[32])
+{
+    uint32_t a[16], b[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=&r"(a[0]), "=&r"(a[1]), "=&r"(a[2]), "=&r"(a[3]), "=&r"(a[4]), "=&r"(a[5]), "=&r"(a[6]), "=&r"(a[7]), "=&r"(a[8]), "=&r"(a[9]), "=&r"(a[10]),
+          "=&r"(a[11]), "=&r"(a[12]), "=&r"(a[13]), "=&r"(a[14]), "=&r"(a[15]), "=&r"(b[0]), "=&r"(b[1]), "=&r"(b[2]), "=&r"(b[3]), "=&r"(b[4]), "=&r"(b[5]),
+          "=&r"(b[6]), "=&r"(b[7]), "=&r"(b[8]), "=&r"(b[9]), "=&r"(b[10]), "=&r"(b[11]), "=&r"(b[12]), "=&r"(b[13]), "=&r"(b[14]), "=&r"(b[15])
+        : "r"(addr), "r"(addr + 16u)
+        : "memory");
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(a[k]), v[16 + k] = __uint_as_float(b[k]);
+}
+
+// Sixteen columns of the warp's 32 rows, added over the accumulators in order (SEGMENTS: to z).
+template <bool SEGMENTS = false>
 __device__ __forceinline__ void lt_sums(uint32_t src, int accs, float (&z)[16])
 {
     uint32_t a[16];
+    if (SEGMENTS) {
+        for (int i = 0; i < accs; ++i) {
+            lt_read16(src + (uint32_t)(i * (kLtMaxN / accs)), a);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) z[k] += __uint_as_float(a[k]);
+        }
+        return;
+    }
     lt_load16(src, a);
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
@@ -104,6 +172,26 @@ __device__ __forceinline__ void lt_sums(uint32_t src, int accs, float (&z)[16])
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
         for (int k = 0; k < 16; ++k) z[k] += __uint_as_float(a[k]);
+    }
+}
+
+// A segment's sums of `count` columns, to their places in the slab.
+__device__ __forceinline__ void lt_segment(uint32_t src, int accs, int count, float* at, bool whole, bool add)
+{
+    int q = 0;
+    if (accs == 1) {
+        for (; q + 16 < count; q += 32) {
+            float z[32];
+            __syncwarp();
+            lt_read32(src + (uint32_t)q, z);
+            lt_put(at + q * kLtM, z, whole, add);
+        }
+    }
+    for (; q < count; q += 16) {
+        float z[16];
+        __syncwarp();
+        lt_sums(src + (uint32_t)q, accs, z);
+        lt_put(at + q * kLtM, z, whole, add);
     }
 }
 
@@ -184,12 +272,8 @@ __device__ __forceinline__ void lt_result(const LinearOut& out, uint32_t src, in
 
 // N tokens of a gated tile: lane pairs have column f of the gate and of the up rows; the even lane takes the even tokens.
 template <int N>
-__device__ __forceinline__ void lt_result_pair(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t f, bool live, int lane)
+__device__ __forceinline__ void lt_pair(const LinearOut& out, float (&z)[N], float b, int64_t t0, int count, int64_t f, bool live, int lane)
 {
-    float z[N];
-    __syncwarp();
-#pragma unroll
-    for (int q = 0; q < N; q += 16) lt_sums(src + (uint32_t)q, accs, *reinterpret_cast<float(*)[16]>(z + q));
     const bool odd = lane & 1;
 #pragma unroll
     for (int k = 0; k < N; ++k) z[k] += b;
@@ -217,10 +301,21 @@ __device__ __forceinline__ void lt_result_pair(const LinearOut& out, uint32_t sr
     }
 }
 
+template <int N>
+__device__ __forceinline__ void lt_result_pair(const LinearOut& out, uint32_t src, int accs, float b, int64_t t0, int count, int64_t f, bool live, int lane)
+{
+    float z[N];
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < N; q += 16) lt_sums(src + (uint32_t)q, accs, *reinterpret_cast<float(*)[16]>(z + q));
+    lt_pair(out, z, b, t0, count, f, live, lane);
+}
+
 // HALF: blocks of 32 weights, two constants per thread and k-block.  LUT: half of the codes are looked up in a table of pairs.
 // GATED (forward): a tile holds 64 gate rows and the 64 up rows of the same columns of the result, in turn.
 // SCALED (backward): a token's sums are multiplied by out.scale; with a test of it in every launch bof4_linear_backward took 4 % longer (200 tokens of 14336 x 4096: 44.6 us, 42.8 without).
-template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT, bool GATED, bool SCALED>
+// SEGMENTS (forward): results in fp32 of a long K, whose accumulators take at most `work.segment` lines; the segments of a part of a tile are added, rounded, in its slab.
+template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT, bool GATED, bool SCALED, bool SEGMENTS>
 __global__ void __launch_bounds__(kLtThreads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap token_map, const void* __restrict__ scales,
                  int64_t cols, int block_shift, int64_t last_scale, const float* __restrict__ levels, const LinearOut out,
@@ -387,7 +482,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             // fp32 accumulator, bf16 x bf16, A M-major (backward) or K-major, B K-major, M = 128, N
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (BWD ? 1u << 15 : 0u) | ((uint32_t)(box_n >> 3) << 17) | ((uint32_t)(kLtM >> 4) << 24);
             constexpr uint64_t a_step = BWD ? 2048 >> 4 : 32 >> 4;  // 16 of K
-            int in = in0, seg = 0;
+            int in = in0, seg = 0, run = 0;
             uint32_t acc = 0u;
             bool ok = true;
             for (int n = 0; n < lines; ++n) {
@@ -422,6 +517,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
                 if (++in == per_tile || n + 1 == lines) {  // the end of a part of a tile
                     tc_commit(&s_acc_full[seg & 1], 1u);
                     in = 0, ++seg, acc = 0u;
+                    if (SEGMENTS) run = 0;
+                } else if (SEGMENTS && ++run == work.segment) {
+                    tc_commit(&s_acc_full[seg & 1], 1u);
+                    ++seg, acc = 0u, run = 0;
                 }
             }
         }
@@ -491,17 +590,61 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_cons
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(ok ? 1u : 0u) : "memory");
             return r != 0u;
         };
+        int done = 0;  // accumulators that were read, but for the last one of each part
+        const int slab_at = (lane >> 3) * kLtM + (warp & 3) * 32 + (lane & 7) * 4;
         for (int seg = 0; seg < segs; ++seg) {
-            const int buf = seg & 1;
-            if (!all4(warp_wait(&s_acc_full[buf], (uint32_t)(seg >> 1) & 1u))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int tile = tile0 + seg, t0 = tile * per_tile;
+            bool summed = false;
+            if (SEGMENTS) {  // the segments of this part of the tile but for the last
+                const int from = begin > t0 ? begin : t0, to = finish < t0 + per_tile ? finish : t0 + per_tile;
+                const bool whole = to - from == per_tile;
+                const int64_t first = (int64_t)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
+                const int count = (int)(out.tokens - first < box_n ? out.tokens - first : box_n);
+                float* const at = parts + (2 * (int64_t)blockIdx.x + (begin <= t0 ? 1 : 0)) * kLtM * box_n + (whole ? slab_at : m);
+                bool ok = true;
+                for (int left = (to - from - 1) / work.segment; left; --left, ++done) {
+                    const int buf = (seg + done) & 1;
+                    if (!(ok = all4(warp_wait(&s_acc_full[buf], (uint32_t)((seg + done) >> 1) & 1u)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    lt_segment(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * kLtMaxN), accs, count, at, whole, summed);
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) tc_arrive(&s_acc_empty[buf]);
+                    summed = true;
+                }
+                if (!ok) break;
+            }
+            const int buf = (seg + done) & 1;
+            if (!all4(warp_wait(&s_acc_full[buf], (uint32_t)((seg + done) >> 1) & 1u))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int64_t o = (int64_t)((uint32_t)tile / (uint32_t)work.tiles_n) * kLtM + m, token0 = (int64_t)((uint32_t)tile % (uint32_t)work.tiles_n) * box_n;
             const int count = (int)(out.tokens - token0 < box_n ? out.tokens - token0 : box_n);
             const bool all = begin <= t0 && finish >= t0 + per_tile, live = (GATED ? o >> 1 : o) < out.n;
             const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * kLtMaxN);
             float* const part = parts + (2 * (int64_t)blockIdx.x + (begin <= t0 ? 1 : 0)) * kLtM * box_n;
-            if (!all) {
+            if (SEGMENTS && summed) {
+                if (!all) {
+                    lt_segment(src, accs, count, part + m, false, true);
+                } else {
+                    const float b = GATED && live ? out.bias_at((o & 1) * out.n + (o >> 1)) : 0.0f;
+                    float* const y = static_cast<float*>(out.y) + token0 * out.ldy + o;
+                    for (int q = 0; q < count; q += 32) {
+                        float z[32];
+                        lt_before(part + slab_at, q, count, z);
+                        __syncwarp();
+#pragma unroll
+                        for (int h = 0; h < 32; h += 16)
+                            if (q + h < count) lt_sums<true>(src + (uint32_t)(q + h), accs, *reinterpret_cast<float(*)[16]>(z + h));
+                        if (GATED) {
+                            lt_pair(out, z, b, token0 + q, count - q, o >> 1, live, lane);
+                        } else {  // logits: nothing but stores
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (live && q + k < count) y[(q + k) * out.ldy] = z[k];
+                        }
+                    }
+                }
+            } else if (!all) {
                 float* to = part + m;
                 for (int q = 0; q < count; q += 16, to += 16 * kLtM) {
                     float z[16];
@@ -616,29 +759,31 @@ int linear_tc_forward(const LtLaunch& go);
 int linear_tc_backward(const LtLaunch& go);
 int linear_tc_scaled(const LtLaunch& go);
 int linear_tc_gated(const LtLaunch& go);
+int linear_tc_forward_segments(const LtLaunch& go);
+int linear_tc_gated_segments(const LtLaunch& go);
 
-template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT, bool GATED, bool SCALED>
+template <bool BWD, class ST, bool HALF, bool OPQ, bool LUT, bool GATED, bool SCALED, bool SEGMENTS>
 int lt_go(const LtLaunch& go)
 {
-    constexpr auto kern = linear_tc_kernel<BWD, ST, HALF, OPQ, LUT, GATED, SCALED>;
+    constexpr auto kern = linear_tc_kernel<BWD, ST, HALF, OPQ, LUT, GATED, SCALED, SEGMENTS>;
     if (const int rc = ensure_dynamic_smem<kern>(kLtSmem)) return rc;
     const LinearW& w = *go.w;
     launch_after(kern, go.ctas, kLtThreads, kLtSmem, go.st, *go.code_map, *go.token_map, w.scales, w.cols, w.block_shift, w.rows * w.cols / w.block_size - 1,
                  w.levels, *go.out, go.status, go.heads, go.nodes, *go.work, go.ws, go.parts);
     return BOF4_OK;
 }
-template <bool BWD, bool GATED, bool SCALED, class ST, bool HALF>
+template <bool BWD, bool GATED, bool SCALED, bool SEGMENTS, class ST, bool HALF>
 int lt_pick(const LtLaunch& go)
 {
-    if (go.heads) return go.work->table ? lt_go<BWD, ST, HALF, true, true, GATED, SCALED>(go) : lt_go<BWD, ST, HALF, true, false, GATED, SCALED>(go);
-    return go.work->table ? lt_go<BWD, ST, HALF, false, true, GATED, SCALED>(go) : lt_go<BWD, ST, HALF, false, false, GATED, SCALED>(go);
+    if (go.heads) return go.work->table ? lt_go<BWD, ST, HALF, true, true, GATED, SCALED, SEGMENTS>(go) : lt_go<BWD, ST, HALF, true, false, GATED, SCALED, SEGMENTS>(go);
+    return go.work->table ? lt_go<BWD, ST, HALF, false, true, GATED, SCALED, SEGMENTS>(go) : lt_go<BWD, ST, HALF, false, false, GATED, SCALED, SEGMENTS>(go);
 }
-template <bool BWD, bool GATED, bool SCALED = false>
+template <bool BWD, bool GATED, bool SCALED = false, bool SEGMENTS = false>
 int lt_launch(const LtLaunch& go)
 {
     const bool half = go.w->block_size == 32;
-    if (go.w->scale_dtype == BOF4_F32) return half ? lt_pick<BWD, GATED, SCALED, F32, true>(go) : lt_pick<BWD, GATED, SCALED, F32, false>(go);
-    return half ? lt_pick<BWD, GATED, SCALED, BF16, true>(go) : lt_pick<BWD, GATED, SCALED, BF16, false>(go);
+    if (go.w->scale_dtype == BOF4_F32) return half ? lt_pick<BWD, GATED, SCALED, SEGMENTS, F32, true>(go) : lt_pick<BWD, GATED, SCALED, SEGMENTS, F32, false>(go);
+    return half ? lt_pick<BWD, GATED, SCALED, SEGMENTS, BF16, true>(go) : lt_pick<BWD, GATED, SCALED, SEGMENTS, BF16, false>(go);
 }
 
 }  // namespace bof4
